@@ -296,6 +296,119 @@ segattn_status seg_attn_gather_context_rope(int32_t B, int32_t Hkv, int32_t d, i
                                             const int32_t* idx, void* K_ctx, void* V_ctx, const float* table,
                                             int32_t n_pos, void* stream);
 
+/* ---- Rotary positions in general form.  The paper's "standard RoPE" above rotates the whole head in the half pairing at
+ * consecutive positions; models that are served through the paged cache below also come with neighbouring elements
+ * paired, with only the first rot_dim elements of a head rotated, with frequencies scaled for contexts longer than the
+ * trained one, and with rows at positions of their own.
+ *   seg_rope_table_scaled  fills `table` (DEVICE, 16-byte aligned, fp32 [n_pos][rot_dim/2][2] = a (cos, sin)(pos w_i)) with
+ *                          w_i = base^(-2i/rot_dim), a = amplitude, and by `kind`
+ *                            SEGATTN_ROPE_PLAIN      w_i as it is;
+ *                            SEGATTN_ROPE_LINEAR     w_i / factor (positions interpolated);
+ *                            SEGATTN_ROPE_BY_PARTS   (1 - g_i) w_i / factor + g_i w_i with the ramp
+ *                                                    g_i = clamp((t_i - turns_lo) / (turns_hi - turns_lo), 0, 1) over the
+ *                                                    turns t_i = trained_len w_i / (2 pi) that pair i makes in the trained
+ *                                                    length: slow pairs are interpolated, fast ones kept.
+ *                          Angles, cosines and sines in double precision, rounded to fp32.  A table that seg_rope_table
+ *                          filled serves as well (rot_dim = d).
+ *   seg_rope_rotate        Y[b][r][h][:] = Rot(p) X[b][r][h][:] with p = positions[b*L + r] (DEVICE int32 [B][L]) or, where
+ *                          `positions` is NULL, pos0 + r.  Pairs are (x[i], x[i + rot_dim/2]) for SEGATTN_ROPE_HALF and
+ *                          (x[2i], x[2i+1]) for SEGATTN_ROPE_INTERLEAVED, i < rot_dim/2; elements from rot_dim on are
+ *                          copied.  bf16, element strides (batch, row, head), multiples of 8; Y may be X (with its strides)
+ *                          and may not overlap it otherwise.  inverse != 0 applies the transposed map (times the amplitude
+ *                          again): the backward pass, which takes dY to dX.  fp32 arithmetic with separately rounded
+ *                          products, one rounding to bf16.  A position outside [0, n_pos) is not looked up: its row comes
+ *                          out zero and the next seg_attn_poll_status returns SEGATTN_ERR_INVALID.
+ * d and rot_dim are multiples of 16, 16 <= rot_dim <= d <= 256, n_pos <= 2^24. */
+#define SEGATTN_ROPE_PLAIN 0
+#define SEGATTN_ROPE_LINEAR 1
+#define SEGATTN_ROPE_BY_PARTS 2
+#define SEGATTN_ROPE_HALF 0
+#define SEGATTN_ROPE_INTERLEAVED 1
+typedef struct {
+    int32_t kind;
+    double base;                              /* > 1 */
+    double factor;                            /* LINEAR, BY_PARTS: > 0 */
+    double trained_len, turns_lo, turns_hi;   /* BY_PARTS: trained_len > 0, 0 <= turns_lo < turns_hi */
+    double amplitude;                         /* > 0; 1 for a pure rotation */
+} seg_rope_scaling;
+segattn_status seg_rope_table_scaled(int32_t n_pos, int32_t rot_dim, const seg_rope_scaling* sc, float* table, void* stream);
+segattn_status seg_rope_rotate(int32_t B, int32_t L, int32_t H, int32_t d, int32_t rot_dim, int32_t layout, const void* X,
+                               const int64_t x_stride[3], void* Y, const int64_t y_stride[3], const int32_t* positions,
+                               int32_t pos0, int32_t inverse, const float* table, int32_t n_pos, void* stream);
+
+/* ---- Serving: a paged key/value cache, the attention of new tokens over it, and its eviction.  The paper stops at the
+ * prefill; these continue it token by token under the same mask.  A sequence's rows lie in pages of page_size rows, slot j
+ * in row j % page_size of page block_table[b][j / page_size]; a page belongs to one sequence.  kv_len[b] counts the rows
+ * including the call's new ones: new row t of sequence b (t < q_len[b]) has slot kv_len[b] - q_len[b] + t and the global
+ * position slot + pos_shift[b], where pos_shift counts the rows that evictions have taken out.
+ * Everything the kernels read per sequence is in device memory, so a captured graph follows the lengths as they grow.
+ * Numbers are checked where they are read: a page number outside [0, n_pages), a length outside [0, max_pages*page_size]
+ * or a q_len outside [0, Lq] makes the next seg_attn_poll_status return SEGATTN_ERR_INVALID; such a page's rows are neither
+ * read (they count as not visible) nor written, such a length is cut to its range. */
+#define SEGATTN_KV_BF16 0
+#define SEGATTN_KV_E4M3 1 /* 8-bit values, 1 + 4 + 3 bits, times a scale per KV head */
+typedef struct {
+    int32_t B, Hkv, d;           /* sequences; KV heads, at most 64; head dimension, 64 or 128 */
+    int32_t dtype;               /* SEGATTN_KV_* */
+    int32_t page_size, n_pages;  /* rows in a page, >= 1; pages in K and in V */
+    int32_t max_pages;           /* entries of a sequence's row of the block table; max_pages*page_size <= 2^30 */
+    int32_t table_stride;        /* elements between rows of the block table, >= max_pages */
+    void *K, *V;                 /* DEVICE, 16-byte aligned */
+    int64_t k_stride[3], v_stride[3]; /* elements, for (page, row, head); multiples of 16 bytes; the last dimension is contiguous */
+    const float *k_scale, *v_scale;   /* E4M3: DEVICE [Hkv], finite and > 0 (not checked); BF16: NULL */
+    const int32_t* block_table;  /* DEVICE [B][max_pages]; entries past a sequence's last page are not read */
+    const int32_t* kv_len;       /* DEVICE [B] */
+    const int32_t* q_len;        /* DEVICE [B], new rows of each sequence, or NULL: Lq for all */
+    const int32_t* pos_shift;    /* DEVICE [B], >= 0, or NULL: 0 for all */
+} seg_kv_cache;
+
+/* Writes the new rows K_new, V_new (bf16 [B][Lq][Hkv][d]) into the cache.  With `table` (see seg_rope_rotate; rot_dim, layout
+ * and n_pos as there) the keys are rotated by their positions first, and so are the queries Q (bf16 [B][Lq][Hq][d], may
+ * be NULL; Q_out may be Q) into Q_out; without a table keys are copied and Q must be NULL.  An e4m3 cache stores x / scale
+ * rounded to nearest even and saturated at +-448.  Rows t >= q_len[b] are neither read nor written.  A new row
+ * whose slot or position is out of range is not written (status as above).  One kernel. */
+segattn_status seg_kv_append(const seg_kv_cache* c, int32_t Lq, const void* K_new, const int64_t kn_stride[3],
+                             const void* V_new, const int64_t vn_stride[3], int32_t Hq, const void* Q,
+                             const int64_t q_stride[3], void* Q_out, const int64_t qo_stride[3], const float* table,
+                             int32_t n_pos, int32_t rot_dim, int32_t layout, void* stream);
+
+/* Attention of the new rows over the cache (which already holds them): for row t of sequence b at slot e and position p,
+ * and KV head h of class head_past_mask[h] (HOST array, read before the call returns), slot j is visible when
+ * lo <= j <= e, lo = 0 (PAST), max(0, max(0, i S - T) - pos_shift) (LOCAL), max(0, i S - pos_shift) (OWN), i = p / S: the
+ * mask of seg_attn_fwd on what the cache retains.  (After an eviction that kept at least the last S + T rows, local and
+ * own-segment heads see what they would have seen without it.)  S = 2^30 makes every head plainly causal.
+ *   O bf16 [B][Lq][Hq][d], LSE fp32 contiguous [B][Hq][Lq] as in seg_attn_fwd; rows t >= q_len[b] are left as they were; a
+ *   row that sees no key gets O = 0, LSE = -inf.  A row's result does not depend on rows it does not see, whatever they hold.
+ *   weights_out (NULL: none): fp32 contiguous [B][Hkv][W]; for every slot j < kv_len[b] of sequences with new rows
+ *     weights_out[b][h][j] = (weights_in ? weights_in[b][h][j] : 0) + sum over the new rows and the query heads of h of the
+ *     row's attention weight on j;
+ *   other entries are left as they were.  weights_in may be weights_out.  W >= max_pages*page_size.
+ * `workspace`: DEVICE, 256-byte aligned, seg_attn_decode_workspace_bytes(...) bytes, scratch (0 = invalid parameters); calls
+ * that may run at the same time, captured ones too, need one each.  Results do not change from run to run.
+ * fp32 scores, statistics and accumulators; the weights are rounded to 16 bits before the product with V (bf16, or fp16
+ * beside an e4m3 cache). */
+size_t seg_attn_decode_workspace_bytes(const seg_kv_cache* c, int32_t Lq, int32_t Hq, int32_t with_weights);
+segattn_status seg_attn_decode(const seg_kv_cache* c, int32_t Lq, int32_t Hq, int32_t S, int32_t T, float sm_scale,
+                               const uint8_t* head_past_mask, const void* Q, const int64_t q_stride[3], void* O,
+                               const int64_t o_stride[3], float* LSE, const float* weights_in, float* weights_out, int32_t W,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Eviction by accumulated attention weight.  With n = kv_len[b] and budget = sink + recent + heavy: a sequence of n <= budget
+ * keeps all its rows; otherwise each KV head keeps the first `sink` slots, the last `recent` ones, and of those between them
+ * the `heavy` ones of largest weights[b][h][.] (fp32 contiguous [B][Hkv][W]; equal weights: lower slot first; NaN ranks
+ * lowest).  The kept rows of K and V are copied in ascending order to slots 0, 1, ... of the pages that dst_table (DEVICE
+ * [B][dst_max_pages], row stride dst_stride) names in the same K and V, which must be none of the sequence's present pages.
+ *   idx          int32 contiguous [B][Hkv][budget]: the slots kept, ascending, then -1
+ *   kv_len_out   int32 [B]: min(n, budget);  pos_shift_out int32 [B]: pos_shift + n - kv_len_out.  Either may be the cache's own.
+ *   weights_out  fp32 contiguous [B][Hkv][W]: the kept slots' weights, then zeros; may not overlap weights
+ * W >= max_pages*page_size, 1 <= budget <= dst_max_pages*page_size and budget <= W.  q_len is ignored.
+ * `workspace`: DEVICE, 256-byte aligned, seg_kv_evict_workspace_bytes(c) bytes (0 = invalid parameters), scratch. */
+size_t seg_kv_evict_workspace_bytes(const seg_kv_cache* c);
+segattn_status seg_kv_evict(const seg_kv_cache* c, const float* weights, int32_t W, int32_t sink, int32_t recent,
+                            int32_t heavy, const int32_t* dst_table, int32_t dst_max_pages, int32_t dst_stride, int32_t* idx,
+                            int32_t* kv_len_out, int32_t* pos_shift_out, float* weights_out, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 /* ---- Whole training-step call with HOST buffers (pinned or pageable): copies Q, K, V, dO to
  * the device arena, runs forward and backward, copies O, LSE, dQ, dK, dV back, and
  * synchronises `stream` before returning.  Host tensors are contiguous in the layouts

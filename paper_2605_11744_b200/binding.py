@@ -82,6 +82,17 @@ def lib():
         L.seg_attn_gather_context.argtypes = [ctypes.c_int32] * 6 + [vp, vp, ctypes.POINTER(ctypes.c_int64), vp, vp,
                                                                      ctypes.POINTER(ctypes.c_int64), vp, vp, vp, vp]
         L.seg_attn_selftest_wait_timeout.argtypes = [vp]
+        i32 = ctypes.c_int32
+        L.seg_rope_table_scaled.argtypes = [i32, i32, vp, vp, vp]
+        L.seg_rope_rotate.argtypes = [i32] * 6 + [vp, vp, vp, vp, vp, i32, i32, vp, i32, vp]
+        L.seg_kv_append.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, i32, i32, vp]
+        L.seg_attn_decode_workspace_bytes.restype = ctypes.c_size_t
+        L.seg_attn_decode_workspace_bytes.argtypes = [vp, i32, i32, i32]
+        L.seg_attn_decode.argtypes = [vp, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp,
+                                      ctypes.c_size_t, vp]
+        L.seg_kv_evict_workspace_bytes.restype = ctypes.c_size_t
+        L.seg_kv_evict_workspace_bytes.argtypes = [vp]
+        L.seg_kv_evict.argtypes = [vp, vp, i32, i32, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.seg_attn_status_string.restype = ctypes.c_char_p
         L.seg_attn_status_string.argtypes = [ctypes.c_int]
         L.seg_attn_last_cuda_error.restype = ctypes.c_int
