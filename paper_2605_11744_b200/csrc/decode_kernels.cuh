@@ -1,17 +1,21 @@
 // Attention of a sequence's newest rows over its paged cache.
 //
 // The work is a stream over the visible K and V rows (HBM bound: 4 g flops per byte for g query heads to a KV head), so the
-// kernel is built around the loads.  Its unit is a tile of 64 slots of one item, an item being up to 16 WM rows (new row,
+// kernel is built around the loads.  Its unit is a tile of 64 slots of one item, an item being up to 8 NT WM rows (new row,
 // query head) of one (sequence, KV head).  All tiles of all items form one list, which the grid - two blocks to an SM -
 // cuts into equal ranges by the lengths found in device memory: whatever the batch's mix of lengths and head classes, every
 // SM reads the same number of bytes.  Where a range ends inside an item the block leaves an unnormalised part (O, running
-// maximum, sum) in the workspace, and decode_join_kernel adds the parts up in the order of the ranges.
+// base, sum) in the workspace, and decode_join_kernel adds the parts up in the order of the ranges.
 //
 // Inside a block four warps load 16 slots of a tile each with cp.async into a ring of their own, several tiles ahead and
-// across item borders.  For up to 16 rows (WM = 1) each warp attends over its own 16 slots with its own running maximum
-// and sum and needs no block barrier until an item ends; for more rows WM = 2 or 4 warps share 32 or 64 slots, so that a
-// row of K is read once for 32 or 64 rows.  Products run on mma.sync: 16 rows fill one of its tiles, while tcgen05.mma
-// starts at 64 and would leave nine tenths of its rows empty for the same bytes.
+// across item borders.  For up to 16 rows (WM = 1) each warp attends over its own 16 slots with its own base and sum and
+// needs no block barrier until an item ends; for more rows WM = 2 or 4 warps share 32 or 64 slots, so that a row of K is
+// read once for 32 or 64 rows.
+//
+// Products run on mma.sync with the slots in M and the query rows in N: S^T = K Q^T (16 slots x 8 rows) and O^T = V^T P^T
+// (16 dims x 8 rows).  Eight query heads fill a tile of that shape; with the rows in M half of it would be padding, and
+// tcgen05.mma, which starts at 64 (the slots could fill that, but P^T would have to pass through shared memory for every
+// tile), buys nothing where four tenths of the issue slots are free.
 #pragma once
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -35,14 +39,15 @@ struct DecodeParams {
     float* w_out;                    // or null
     const float *k_scale, *v_scale;  // e4m3 only
     // workspace
-    float* part_o;                   // [grid][2][16 WM][D]
-    float2* part_ml;                 // [grid][2][16 WM] (maximum in log2 units, sum)
+    float* part_o;                   // [grid][2][rows of an item][D]
+    float2* part_ml;                 // [grid][2][rows of an item] (base in log2 units, sum)
     int2* item_blocks;               // [B][Hkv][row blocks]: first and last block of the item's tiles
     float* scores;                   // [B][Hkv][g Lq][pitch], log2 units; null unless weights are asked for
     long long q_stride[3], o_stride[3];
     FastDiv f_S, f_g;
     int S, T, W, Hq, g;
-    int row_blocks;                  // ceil(g Lq / (16 WM))
+    int row_blocks;                  // ceil(g Lq / (rows of an item))
+    int page_whole;                  // page_size is a multiple of 16: a warp's slots lie in one page
     int pitch;                       // slots in a row of scores
     int min_tiles;                   // a block's range has at least this many tiles
     float scale_log2;                // sm_scale * log2(e)
@@ -196,9 +201,12 @@ template <int RB>
 __device__ __forceinline__ uint32_t swizzled(int r, int c) {
     return (uint32_t)(r * RB + ((c ^ (RB == 64 ? (r >> 1) & 3 : r & 7)) << 4));
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async16_if(uint32_t dst, const void* src, bool there) {
     // without `there` nothing is read and the 16 bytes become zero
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -211,6 +219,11 @@ __device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t (&r)[4]) {
 }
 __device__ __forceinline__ void ldsm_x4_t(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// two 16 x 16 blocks of bytes, transposed: lane l gets column l/4 (then l/4 + 8), rows 4 (l%4) .. + 3, of each
+__device__ __forceinline__ void ldsm8_x2_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
@@ -244,38 +257,40 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
     return pack_bf16(lo, hi);
 }
 
-template <int D, bool FP8, int WM>
+__device__ __forceinline__ uint32_t movm_t(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+template <int D, bool FP8, int NT, int WM>
 struct DecodeShape {
     static constexpr int RB = D * (FP8 ? 1 : 2);           // bytes of a cache row
     static constexpr int kStages = RB == 256 ? 3 : RB == 128 ? 6 : 8;
     static constexpr int kWarpStage = 2 * 16 * RB;         // a warp's 16 K rows and 16 V rows
-    static constexpr int kRing = kStages * 4 * kWarpStage;
-    static constexpr int MB = 16 * WM;                     // rows of an item
-    static constexpr int kMergeRows = WM == 4 ? 0 : 32;    // rows handed over between warps at an item's end
-    static constexpr int kMergePitch = D + 4;              // floats
-    static constexpr int kMerge = kMergeRows * kMergePitch * 4;
-    static constexpr int kDynamic = kRing + kMerge + 128;
+    static constexpr int kWR = 8 * NT;                     // rows of a warp
+    static constexpr int MB = kWR * WM;                    // rows of an item
+    static constexpr int kDynamic = kStages * 4 * kWarpStage + 128;
+    static_assert(8 * D * 4 <= kWarpStage, "eight rows of an item's end go through a warp's free stage");
 };
 
-// One warp's running state for 16 rows.  Lane l holds rows l/4 and l/4 + 8 in the layout of an mma accumulator.
-template <int D>
-struct RowState {
-    float o[D / 8][4];
-    float m[2], l[2];  // maximum in log2 units; sum over this lane's columns
-};
+// A weight of exp2(score - base) may exceed 1 by this power of two before the base is moved up to the row's maximum: most
+// tiles then need no maximum across lanes and no rescaling, and a weight in fp16 or bf16 keeps its relative precision.
+constexpr float kDecSlack = 8.f;
 
-template <int D, bool FP8, int WM>
+template <int D, bool FP8, int NT, int WM>
 __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
-    using Sh = DecodeShape<D, FP8, WM>;
-    constexpr int RB = Sh::RB, C = RB / 16, MB = Sh::MB, ST = Sh::kStages, KS = D / 16;
+    using Sh = DecodeShape<D, FP8, NT, WM>;
+    constexpr int RB = Sh::RB, C = RB / 16, MB = Sh::MB, WR = Sh::kWR, ST = Sh::kStages, KS = D / 16, MT = D / 16;
     extern __shared__ uint8_t smem_raw[];
     __shared__ BlockRange range;
     __shared__ int warp_sum[4];
     __shared__ uint32_t there[ST][4];  // which of a warp's 16 slots were loaded, per stage
+    __shared__ float2 end_ml[4][8];    // an item's end: base and sum of eight rows of each warp
     const uint32_t ring = (smem_u32(smem_raw) + 127u) & ~127u;
-    float* merge = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + Sh::kRing);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q4 = lane & 3;
-    const int group = warp / WM, wrow = warp % WM;  // key group of this warp, and its 16 rows of the item
+    uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q4 = lane & 3, l4 = lane >> 2;
+    const int group = warp / WM, wrow = warp % WM;  // key group of this warp, and its rows of the item
 
     find_range<MB>(p, &range, warp_sum);
     if (range.begin >= range.end) return;
@@ -289,32 +304,61 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
     put = get;
     int put_left = range.end - range.begin, get_left = put_left;
 
-    // One tile's 16 slots of this warp into stage s.
+    // ---- one tile's 16 slots of this warp into stage s ----
+    constexpr int RPI = 32 / C;  // rows that one instruction of the warp covers
+    const int r0 = lane / C, ch = lane % C;
+    const uint32_t put_lane = swizzled<RB>(r0, ch);
     auto load_tile = [&](int s) {
         if (put_left > 0) {
             if (put.tile == put.end) put.next_item(p);
-            const int r = lane & 15, slot = put.first_slot() + warp * 16 + r;
-            long long off = -1;  // of row r: lanes 0-15 in K, 16-31 in V
-            if (slot >= put.lo && slot < put.hi) {
-                int prow;
-                const int page = page_of(p.c, put.b, slot, &prow);
-                const long long* st = lane < 16 ? p.c.k_stride : p.c.v_stride;
-                if (page >= 0) off = page * st[0] + prow * st[1] + put.h * st[2];
-            }
-            const uint32_t loaded = __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
-            if (lane == 0) there[s][warp] = loaded;
-            const uint32_t dst = ring + (uint32_t)(s * 4 + warp) * Sh::kWarpStage;
-            constexpr int RPI = 32 / C;  // rows one instruction covers
-            const int r0 = lane / C, ch = lane % C;
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-                for (int i = 0; i < 16 / RPI; ++i) {
-                    const int row = i * RPI + r0;
-                    const long long o = __shfl_sync(0xffffffffu, off, kv * 16 + row);
-                    const char* src = (kv ? p.c.V : p.c.K) + (o >= 0 ? o + ch * 16 : 0);
-                    cp_async16(dst + kv * 16 * RB + swizzled<RB>(row, ch), src, o >= 0);
+            const int slot0 = put.first_slot() + warp * 16;
+            const uint32_t dst = ring + (uint32_t)(s * 4 + warp) * Sh::kWarpStage + put_lane;
+            if (p.page_whole) {
+                // the 16 slots lie in one page: one look-up, and rows a stride apart
+                int prow = 0, page = -1;
+                if (slot0 + 16 > put.lo && slot0 < put.hi) page = page_of(p.c, put.b, slot0, &prow);
+                const long long pg = max(page, 0);
+                const char* k = p.c.K + pg * p.c.k_stride[0] + (prow + r0) * p.c.k_stride[1] + put.h * p.c.k_stride[2] + ch * 16;
+                const char* v = p.c.V + pg * p.c.v_stride[0] + (prow + r0) * p.c.v_stride[1] + put.h * p.c.v_stride[2] + ch * 16;
+                const bool whole = slot0 >= put.lo && slot0 + 16 <= put.hi && page >= 0;
+                uint32_t loaded = 0xffffu;
+                if (!whole) {
+                    const int a = min(max(put.lo - slot0, 0), 16), z = min(max(put.hi - slot0, 0), 16);
+                    loaded = page >= 0 ? ((1u << z) - 1) & ~((1u << a) - 1) : 0u;
                 }
+                if (lane == 0) there[s][warp] = loaded;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    const char* src = kv ? v : k;
+                    const long long step = RPI * (kv ? p.c.v_stride[1] : p.c.k_stride[1]);
+#pragma unroll
+                    for (int i = 0; i < 16 / RPI; ++i) {
+                        const uint32_t to = (dst ^ swizzled<RB>(i * RPI, 0) % RB) + kv * 16 * RB + i * RPI * RB;
+                        if (whole) cp_async16(to, src);
+                        else cp_async16_if(to, src, (loaded >> (i * RPI + r0)) & 1);
+                        src += step;
+                    }
+                }
+            } else {
+                const int slot = slot0 + (lane & 15);
+                long long off = -1;  // of one row: lanes 0-15 in K, 16-31 in V
+                if (slot >= put.lo && slot < put.hi) {
+                    int prow;
+                    const int page = page_of(p.c, put.b, slot, &prow);
+                    const long long* st = lane < 16 ? p.c.k_stride : p.c.v_stride;
+                    if (page >= 0) off = page * st[0] + prow * st[1] + put.h * st[2];
+                }
+                const uint32_t loaded = __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
+                if (lane == 0) there[s][warp] = loaded;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+                    for (int i = 0; i < 16 / RPI; ++i) {
+                        const long long o = __shfl_sync(0xffffffffu, off, kv * 16 + i * RPI + r0);
+                        const uint32_t to = (dst ^ swizzled<RB>(i * RPI, 0) % RB) + kv * 16 * RB + i * RPI * RB;
+                        cp_async16_if(to, (kv ? p.c.V : p.c.K) + (o >= 0 ? o + ch * 16 : 0), o >= 0);
+                    }
+            }
             ++put.tile;
             --put_left;
         }
@@ -323,24 +367,34 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
 
 #pragma unroll
     for (int s = 0; s < ST - 1; ++s) load_tile(s);
-    int stage = 0, slot_stage = ST - 1;
+    int stage = 0, free_stage = ST - 1;
 
-    RowState<D> st;
-    uint32_t qf[KS][4];
-    float qscale[2];     // score scale of the lane's two rows, log2 units
-    int rlo[2], rhi[2];  // their visible slots
+    // Which slot of its 16 the row m of an S^T tile stands for.  The transposing 8-bit load of V hands a lane four
+    // neighbouring slots, so with an e4m3 cache rows 2q, 2q + 1, 8 + 2q, 9 + 2q stand for slots 4q .. 4q + 3.
+    auto slot_of = [](int m) { return FP8 ? 4 * ((m & 7) >> 1) + (m & 1) + 2 * (m >> 3) : m; };
+    const int js[2] = {slot_of(l4), slot_of(l4 + 8)};  // slots of this lane's scores
+    // byte offsets of this lane's operand pieces within a 16-slot block; piece 2c is reached by XOR with 32 c
+    const uint32_t k_lane = FP8 ? 0u : swizzled<RB>(lane & 15, lane >> 4);
+    const uint32_t k8_lane[2] = {swizzled<RB>(js[0], q4 * (D / 64)), swizzled<RB>(js[1], q4 * (D / 64))};
+    const uint32_t v_lane = 16 * RB + (FP8 ? swizzled<RB>(lane & 15, lane >> 4) : swizzled<RB>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1));
+
+    float o[MT][NT][4];        // O^T: (dim l4, row 2 q4), (dim l4, row 2 q4 + 1), (dim l4 + 8, ...) of 16-dim tiles
+    float m[NT][2], l[NT][2];  // base in log2 units; sum over this lane's slots
+    uint32_t qf[KS][NT][2];
+    float qscale[NT][2];       // score scale of the lane's rows, log2 units
+    int rlo[NT][2], rhi[NT][2];  // their visible slots
     while (get_left > 0) {
         // ---- a piece: this block's tiles of one item ----
         const int first = get.tile, count = min(get.end - first, get_left);
         const int cls = p.head_class[get.h], rows = get.rows * p.g;
         const float vs = FP8 ? p.v_scale[get.h] : 1.f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = get.rb * MB + wrow * 16 + (lane >> 2) + 8 * i;
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = get.rb * MB + wrow * WR + nt * 8 + l4;  // the row whose elements this lane holds
             const bool real = r < rows;
             const int t = (int)fdiv((uint32_t)(real ? r : 0), p.f_g), qh = get.h * p.g + (real ? r - t * p.g : 0);
-            visible_slots(p, get.n, get.rows, get.shift, t, cls, &rlo[i], &rhi[i]);
             const __nv_bfloat16* q = p.Q + get.b * p.q_stride[0] + t * p.q_stride[1] + qh * p.q_stride[2];
+            float scale = p.scale_log2;
             if (FP8) {
                 // Lane q4 of a row takes D/4 consecutive elements, in the order in which it meets the bytes of K.  They go
                 // to fp16 after a division by a power of two that brings the row's largest below 2: what a bf16 value
@@ -364,27 +418,34 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 const int e = big > 0.f ? min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126) : 0;
                 const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-                qscale[i] = p.scale_log2 * p.k_scale[get.h] * __uint_as_float((uint32_t)(127 + e) << 23);
+                scale *= p.k_scale[get.h] * __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
-                    qf[k][i] = real ? pack16<true>(x[4 * k] * down, x[4 * k + 1] * down) : 0u;
-                    qf[k][2 + i] = real ? pack16<true>(x[4 * k + 2] * down, x[4 * k + 3] * down) : 0u;
+                    qf[k][nt][0] = real ? pack16<true>(x[4 * k] * down, x[4 * k + 1] * down) : 0u;
+                    qf[k][nt][1] = real ? pack16<true>(x[4 * k + 2] * down, x[4 * k + 3] * down) : 0u;
                 }
             } else {
-                qscale[i] = p.scale_log2;
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
-                    qf[k][i] = real ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 2 * q4) : 0u;
-                    qf[k][2 + i] = real ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 + 2 * q4) : 0u;
+                    qf[k][nt][0] = real ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 2 * q4) : 0u;
+                    qf[k][nt][1] = real ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 + 2 * q4) : 0u;
                 }
             }
-            st.m[i] = -INFINITY;
-            st.l[i] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int rc = get.rb * MB + wrow * WR + nt * 8 + 2 * q4 + e;  // a row whose scores this lane holds
+                qscale[nt][e] = FP8 ? __shfl_sync(0xffffffffu, scale, (2 * q4 + e) * 4) : scale;
+                visible_slots(p, get.n, get.rows, get.shift, (int)fdiv((uint32_t)min(rc, rows - 1), p.f_g), cls, &rlo[nt][e], &rhi[nt][e]);
+                m[nt][e] = -INFINITY;
+                l[nt][e] = 0.f;
+            }
         }
 #pragma unroll
-        for (int k = 0; k < D / 8; ++k)
+        for (int k = 0; k < MT; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) st.o[k][e] = 0.f;
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[k][nt][e] = 0.f;
         // slots that every row of the item sees: no mask there
         int all_lo, all_hi;
         {
@@ -393,138 +454,125 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
             visible_slots(p, get.n, get.rows, get.shift, (int)fdiv((uint32_t)r_last, p.f_g), cls, &all_lo, &x);
             visible_slots(p, get.n, get.rows, get.shift, (int)fdiv((uint32_t)(get.rb * MB), p.f_g), cls, &x, &all_hi);
         }
-        float* score_row[2];
-        if (p.scores) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = get.rb * MB + wrow * 16 + (lane >> 2) + 8 * i;
-                score_row[i] = r < rows ? p.scores + (((long long)get.b * p.c.Hkv + get.h) * p.g * p.c.Lq + r) * p.pitch : nullptr;
-            }
-        }
+        float* scores = p.scores;
+        if (scores) scores += (((long long)get.b * p.c.Hkv + get.h) * p.g * p.c.Lq + get.rb * MB + wrow * WR) * p.pitch;
 
         for (int left = count; left > 0; --left) {
             cp_async_wait<ST - 2>();
             if (WM == 1) __syncwarp();
             else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(32 * WM) : "memory");
-            load_tile(slot_stage);
-            slot_stage = stage;
+            load_tile(free_stage);
             // this warp's key group: 16 WM slots, loaded by the group's WM warps
-            const int slot0 = get.first_slot() + group * 16 * WM;
-            float s[WM][2][4];
-#pragma unroll
+#pragma unroll 1
             for (int k = 0; k < WM; ++k) {
-                const uint32_t kb = ring + (uint32_t)(stage * 4 + group * WM + k) * Sh::kWarpStage;
+                const int slot0 = get.first_slot() + (group * WM + k) * 16;
+                const uint32_t blk = ring + (uint32_t)(stage * 4 + group * WM + k) * Sh::kWarpStage;
+                const uint32_t have = there[stage][group * WM + k];
+                float s[NT][4];
 #pragma unroll
-                for (int n8 = 0; n8 < 2; ++n8)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[k][n8][e] = 0.f;
+                    for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
                 if (FP8) {
 #pragma unroll
-                    for (int n8 = 0; n8 < 2; ++n8) {
-                        const int row = n8 * 8 + (lane >> 2);
+                    for (int v = 0; v < D / 64; ++v) {
+                        const uint4 w0 = lds128(blk + (k8_lane[0] ^ (v << 4))), w1 = lds128(blk + (k8_lane[1] ^ (v << 4)));
+                        const uint32_t a0[4] = {w0.x, w0.y, w0.z, w0.w}, a1[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-                        for (int v = 0; v < D / 64; ++v) {
-                            const uint4 w = lds128(kb + swizzled<RB>(row, q4 * (D / 64) + v));
-                            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t a[4] = {e4m3x2_to_half2(a0[j]), e4m3x2_to_half2(a1[j]), e4m3x2_to_half2(a0[j] >> 16),
+                                                   e4m3x2_to_half2(a1[j] >> 16)};
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                mma16816<true>(s[k][n8], qf[v * 4 + j], e4m3x2_to_half2(ww[j]), e4m3x2_to_half2(ww[j] >> 16));
+                            for (int nt = 0; nt < NT; ++nt) mma16816<true>(s[nt], a, qf[v * 4 + j][nt][0], qf[v * 4 + j][nt][1]);
                         }
                     }
                 } else {
 #pragma unroll
-                    for (int c2 = 0; c2 < KS; ++c2) {
-                        // matrices: (slots 0-7, piece 2 c2), (slots 0-7, next piece), (slots 8-15, ...) x 2
-                        uint32_t b[4];
-                        ldsm_x4(kb + swizzled<RB>((lane & 7) + ((lane >> 4) << 3), 2 * c2 + ((lane >> 3) & 1)), b);
-                        mma16816<false>(s[k][0], qf[c2], b[0], b[1]);
-                        mma16816<false>(s[k][1], qf[c2], b[2], b[3]);
+                    for (int c = 0; c < KS; ++c) {
+                        uint32_t a[4];
+                        ldsm_x4(blk + (k_lane ^ (c << 5)), a);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma16816<false>(s[nt], a, qf[c][nt][0], qf[c][nt][1]);
                     }
                 }
-            }
-            // scores in log2 units, masked where this tile is not seen whole by every row
-            const bool edge_range = slot0 < all_lo || slot0 + 16 * WM > all_hi;
-            bool edge = edge_range;
+                // element e of s[nt]: slot js[e >> 1], row 2 q4 + (e & 1) of the warp's eight
+                const bool edge_range = slot0 < all_lo || slot0 + 16 > all_hi;
 #pragma unroll
-            for (int k = 0; k < WM; ++k) edge |= there[stage][group * WM + k] != 0xffffu;
-            float mx[2] = {-INFINITY, -INFINITY};
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int k = 0; k < WM; ++k)
+                    for (int e = 0; e < 4; ++e) s[nt][e] *= qscale[nt][e & 1];
+                if (edge_range || have != 0xffffu) {
 #pragma unroll
-                for (int n8 = 0; n8 < 2; ++n8)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float x = s[k][n8][e] * qscale[e >> 1];
-                        if (edge) {
-                            const int j = n8 * 8 + q4 * 2 + (e & 1), slot = slot0 + k * 16 + j;
-                            if (slot < rlo[e >> 1] || slot >= rhi[e >> 1] || !((there[stage][group * WM + k] >> j) & 1)) x = -INFINITY;
+                        for (int e = 0; e < 4; ++e) {
+                            const int j = js[e >> 1];
+                            if (slot0 + j < rlo[nt][e & 1] || slot0 + j >= rhi[nt][e & 1] || !((have >> j) & 1)) s[nt][e] = -INFINITY;
                         }
-                        s[k][n8][e] = x;
-                        mx[e >> 1] = fmaxf(mx[e >> 1], x);
-                    }
-            if (p.scores) {
-#pragma unroll
-                for (int k = 0; k < WM; ++k)
-#pragma unroll
-                    for (int n8 = 0; n8 < 2; ++n8)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            if (score_row[i])
-                                *reinterpret_cast<float2*>(score_row[i] + slot0 + k * 16 + n8 * 8 + q4 * 2) =
-                                    make_float2(s[k][n8][2 * i], s[k][n8][2 * i + 1]);
-            }
-            float base[2];
-            bool grows = false;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
-                grows |= mx[i] > st.m[i];
-            }
-            if (__any_sync(0xffffffffu, grows)) {
-                float f[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float mn = fmaxf(st.m[i], mx[i]);
-                    f[i] = mn == -INFINITY ? 1.f : ex2(st.m[i] - mn);
-                    st.m[i] = mn;
-                    st.l[i] *= f[i];
                 }
+                if (scores) {
 #pragma unroll
-                for (int k = 0; k < D / 8; ++k)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) st.o[k][e] *= f[e >> 1];
-            }
+                        for (int e = 0; e < 4; ++e) {
+                            const int r = nt * 8 + 2 * q4 + (e & 1);
+                            if (get.rb * MB + wrow * WR + r < rows) scores[(long long)r * p.pitch + slot0 + js[e >> 1]] = s[nt][e];
+                        }
+                }
+                bool grows = false;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) base[i] = st.m[i] == -INFINITY ? 0.f : st.m[i];
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int k = 0; k < WM; ++k) {
-                const uint32_t vb = ring + (uint32_t)(stage * 4 + group * WM + k) * Sh::kWarpStage + 16 * RB;
+                    for (int e = 0; e < 4; ++e) grows |= s[nt][e] > m[nt][e & 1] + kDecSlack;
+                if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
-                for (int n8 = 0; n8 < 2; ++n8)
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float f[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float mx = fmaxf(s[nt][e], s[nt][e + 2]);
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                            // row by row: what one row sees must not move another row's base (and with it its rounding)
+                            if (!(mx > m[nt][e] + kDecSlack)) mx = m[nt][e];
+                            f[e] = mx == m[nt][e] ? 1.f : ex2(m[nt][e] - mx);
+                            m[nt][e] = mx;
+                            l[nt][e] *= f[e];
+                        }
+#pragma unroll
+                        for (int k2 = 0; k2 < MT; ++k2)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[k2][nt][e] *= f[e & 1];
+                    }
+                }
+                uint32_t pf[NT][2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        s[k][n8][e] = ex2(s[k][n8][e] - base[e >> 1]);
-                        st.l[e >> 1] += s[k][n8][e];
+                        const float base = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1];
+                        s[nt][e] = ex2(s[nt][e] - base);
+                        l[nt][e & 1] += s[nt][e];
                     }
-                const uint32_t a[4] = {pack16<FP8>(s[k][0][0], s[k][0][1]), pack16<FP8>(s[k][0][2], s[k][0][3]),
-                                       pack16<FP8>(s[k][1][0], s[k][1][1]), pack16<FP8>(s[k][1][2], s[k][1][3])};
+                    pf[nt][0] = movm_t(pack16<FP8>(s[nt][0], s[nt][1]));
+                    pf[nt][1] = movm_t(pack16<FP8>(s[nt][2], s[nt][3]));
+                }
                 // A weight of zero does not undo an infinite or NaN V: slots that some rows of the item see and others do not
                 // (rows behind a row, slots across a segment's border) are looked at, and where V is not finite its product is
                 // taken out of the mma and added to the rows that see it one by one.
                 uint32_t bad = 0;
                 if (edge_range) {
-                    const int b0 = slot0 + k * 16;
                     uint32_t part = 0;
                     for (int j = 0; j < 16; ++j)
-                        if (b0 + j < all_lo || b0 + j >= all_hi) part |= 1u << j;
-                    part &= there[stage][group * WM + k];
+                        if (slot0 + j < all_lo || slot0 + j >= all_hi) part |= 1u << j;
+                    part &= have;
                     while (part) {
                         const int j = __ffs(part) - 1;
                         part &= part - 1;
                         bool odd = false;
                         if (lane < C) {
-                            const uint4 w = lds128(vb + swizzled<RB>(j, lane));
+                            const uint4 w = lds128(blk + 16 * RB + swizzled<RB>(j, lane));
                             const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
@@ -539,157 +587,142 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
                         if (__any_sync(0xffffffffu, odd)) bad |= 1u << j;
                     }
                 }
-                uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;  // of the lane's V fragments: slots 2 q4, 2 q4 + 1 and 8 on
-                if (bad) {
-                    const uint32_t t0 = bad >> (2 * q4), t1 = bad >> (2 * q4 + 8);
-                    keep0 = (t0 & 1 ? 0u : 0xffffu) | (t0 & 2 ? 0u : 0xffff0000u);
-                    keep1 = (t1 & 1 ? 0u : 0xffffu) | (t1 & 2 ? 0u : 0xffff0000u);
-                }
+                auto add_values = [&](uint32_t keep0, uint32_t keep1) {
 #pragma unroll
-                for (int c2 = 0; c2 < C / 2; ++c2) {
-                    if (FP8) {
-                        // (slots 0-7, piece 2 c2), (slots 8-15, same), and the next piece: 16 dims of V to a piece; even and odd
-                        // dims of it go to two mma tiles
+                    for (int c = 0; c < (FP8 ? MT / 2 : MT); ++c) {
                         uint32_t b[4];
-                        ldsm_x4_t(vb + swizzled<RB>(lane & 15, 2 * c2 + (lane >> 4)), b);
+                        if (FP8) {
+                            ldsm8_x2_t(blk + (v_lane ^ (c << 5)), b);
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const uint32_t l0 = e4m3x2_to_half2(b[2 * x]), h0 = e4m3x2_to_half2(b[2 * x] >> 16);
-                            const uint32_t l1 = e4m3x2_to_half2(b[2 * x + 1]), h1 = e4m3x2_to_half2(b[2 * x + 1] >> 16);
-                            mma16816<true>(st.o[4 * c2 + 2 * x], a, __byte_perm(l0, h0, 0x5410) & keep0, __byte_perm(l1, h1, 0x5410) & keep1);
-                            mma16816<true>(st.o[4 * c2 + 2 * x + 1], a, __byte_perm(l0, h0, 0x7632) & keep0, __byte_perm(l1, h1, 0x7632) & keep1);
+                            for (int x = 0; x < 2; ++x) {
+                                const uint32_t a[4] = {e4m3x2_to_half2(b[2 * x]) & keep0, e4m3x2_to_half2(b[2 * x + 1]) & keep0,
+                                                       e4m3x2_to_half2(b[2 * x] >> 16) & keep1, e4m3x2_to_half2(b[2 * x + 1] >> 16) & keep1};
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) mma16816<true>(o[2 * c + x][nt], a, pf[nt][0], pf[nt][1]);
+                            }
+                        } else {
+                            ldsm_x4_t(blk + (v_lane ^ (c << 5)), b);
+                            const uint32_t a[4] = {b[0] & keep0, b[1] & keep0, b[2] & keep1, b[3] & keep1};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma16816<false>(o[c][nt], a, pf[nt][0], pf[nt][1]);
                         }
-                    } else {
-                        uint32_t b[4];
-                        ldsm_x4_t(vb + swizzled<RB>(lane & 15, 2 * c2 + (lane >> 4)), b);
-                        mma16816<false>(st.o[2 * c2], a, b[0] & keep0, b[1] & keep1);
-                        mma16816<false>(st.o[2 * c2 + 1], a, b[2] & keep0, b[3] & keep1);
                     }
-                }
-                while (bad) {
-                    const int j = __ffs(bad) - 1;
-                    bad &= bad - 1;
-                    const int slot = slot0 + k * 16 + j;
+                };
+                if (bad == 0) {
+                    add_values(0xffffffffu, 0xffffffffu);
+                } else {
+                    // the lane's V fragments hold slots slot_of(2 q4), slot_of(2 q4 + 1) and slot_of(8 + 2 q4), slot_of(9 + 2 q4)
+                    add_values(((bad >> slot_of(2 * q4)) & 1 ? 0u : 0xffffu) | ((bad >> slot_of(2 * q4 + 1)) & 1 ? 0u : 0xffff0000u),
+                               ((bad >> slot_of(8 + 2 * q4)) & 1 ? 0u : 0xffffu) | ((bad >> slot_of(9 + 2 * q4)) & 1 ? 0u : 0xffff0000u));
+#pragma unroll 1
+                    for (; bad; bad &= bad - 1) {
+                        const int j = __ffs(bad) - 1, slot = slot0 + j;
+                        const int mrow = FP8 ? (j >> 2) * 2 + (j & 1) + ((j >> 1) & 1) * 8 : j;  // slot_of(mrow) = j
+                        const uint32_t vrow = blk + 16 * RB;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        // the weight of (row, j): column j & 7 of n8 = j / 8, held by lane (row, (j & 7) / 2)
-                        const float x0 = j & 8 ? s[k][1][2 * i] : s[k][0][2 * i], x1 = j & 8 ? s[k][1][2 * i + 1] : s[k][0][2 * i + 1];
-                        const float w = __shfl_sync(0xffffffffu, j & 1 ? x1 : x0, (lane & ~3) | ((j & 7) >> 1));
-                        if (slot < rlo[i] || slot >= rhi[i]) continue;
-#pragma unroll
-                        for (int nt = 0; nt < D / 8; ++nt)
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const int dim = FP8 ? (nt >> 1) * 16 + 4 * q4 + 2 * e + (nt & 1) : nt * 8 + 2 * q4 + e;
-                                const uint32_t at = vb + swizzled<RB>(j, dim * (FP8 ? 1 : 2) / 16) + dim * (FP8 ? 1 : 2) % 16;
-                                float v;
-                                if (FP8) {
-                                    uint32_t byte;
-                                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(at));
-                                    v = __half2float(__ushort_as_half((unsigned short)(e4m3x2_to_half2(byte) & 0xffffu)));
-                                } else {
-                                    uint16_t h16;
-                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h16) : "r"(at));
-                                    v = __uint_as_float((uint32_t)h16 << 16);
-                                }
-                                st.o[nt][2 * i + e] += w * v;
+                                const float w = __shfl_sync(0xffffffffu, mrow & 8 ? s[nt][2 + e] : s[nt][e], (mrow & 7) * 4 + q4);
+                                if (slot < rlo[nt][e] || slot >= rhi[nt][e]) continue;
+#pragma unroll
+                                for (int k2 = 0; k2 < MT; ++k2)
+#pragma unroll
+                                    for (int hh = 0; hh < 2; ++hh) {
+                                        const int byte = (k2 * 16 + l4 + 8 * hh) * (FP8 ? 1 : 2);
+                                        const uint32_t at = vrow + swizzled<RB>(j, byte >> 4) + (byte & 15);
+                                        float x;
+                                        if (FP8) {
+                                            uint32_t raw;
+                                            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(raw) : "r"(at));
+                                            x = __half2float(__ushort_as_half((unsigned short)(e4m3x2_to_half2(raw) & 0xffffu)));
+                                        } else {
+                                            uint16_t raw;
+                                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(raw) : "r"(at));
+                                            x = __uint_as_float((uint32_t)raw << 16);
+                                        }
+                                        o[k2][nt][2 * hh + e] += w * x;
+                                    }
                             }
                     }
                 }
             }
+            free_stage = stage;
             stage = stage + 1 == ST ? 0 : stage + 1;
             ++get.tile;
         }
         get_left -= count;
 
-        // ---- the piece's rows: over the lanes of a row, then over the key groups ----
+        // ---- the item's end: sums over the lanes of a row, then over the key groups, eight rows of each warp at a time
+        // through the stage that was computed last (the next load into it comes after the barriers here) ----
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            st.l[i] += __shfl_xor_sync(0xffffffffu, st.l[i], 1);
-            st.l[i] += __shfl_xor_sync(0xffffffffu, st.l[i], 2);
-        }
-        // warps [half, 2 half) hand their state to warps [0, half); only rows that are there
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int half = 2; half >= WM; half >>= 1) {
-            if (WM == 4) break;
-            float* mine = merge + ((warp % half) * 16 + (lane >> 2)) * Sh::kMergePitch;
-            if (warp >= half && warp < 2 * half) {
+            for (int e = 0; e < 2; ++e) {
+                l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 4);
+                l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 8);
+                l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 16);
+            }
+        // the item's tiles are numbered from list0 on in the list of all tiles
+        const int list0 = range.end - get_left - count - first;
+        const int b_first = list0 / per, b_last = (list0 + get.end - 1) / per;
+        if (first == 0 && threadIdx.x == 0)
+            p.item_blocks[((long long)get.b * p.c.Hkv + get.h) * p.row_blocks + get.rb] = make_int2(b_first, b_last);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float* to = mine + 8 * i * Sh::kMergePitch;
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt > 0 && get.rb * MB + nt * 8 >= rows) break;  // none of the warps' rows from here on is there (WM = 1)
+            float* mine = reinterpret_cast<float*>(ring_ptr + (size_t)(free_stage * 4 + warp) * Sh::kWarpStage);
+            __syncthreads();
+            // row r8 at r8 D, its dims XORed with the row so that the lanes' writes fall into different banks
 #pragma unroll
-                    for (int nt = 0; nt < D / 8; ++nt)
-                        *reinterpret_cast<float2*>(to + nt * 8 + 2 * q4) = make_float2(st.o[nt][2 * i], st.o[nt][2 * i + 1]);
-                    if (q4 == 0) *reinterpret_cast<float2*>(to + D) = make_float2(st.m[i], st.l[i]);
-                }
+            for (int k2 = 0; k2 < MT; ++k2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mine[(2 * q4 + (e & 1)) * D + ((k2 * 16 + l4 + 8 * (e >> 1)) ^ (q4 << 3))] = o[k2][nt][e];
+            if (l4 == 0) {
+                end_ml[warp][2 * q4] = make_float2(m[nt][0], l[nt][0]);
+                end_ml[warp][2 * q4 + 1] = make_float2(m[nt][1], l[nt][1]);
             }
             __syncthreads();
-            if (warp < half) {
+            constexpr int TPR = D / 4;  // threads to a row
+            const int d0 = (threadIdx.x % TPR) * 4;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float* from = mine + 8 * i * Sh::kMergePitch;
-                    const float2 ml = *reinterpret_cast<const float2*>(from + D);
-                    const float mn = fmaxf(st.m[i], ml.x), zero = mn == -INFINITY ? 0.f : mn;
-                    const float fa = ex2(st.m[i] - zero), fb = ex2(ml.x - zero);
-                    st.m[i] = mn;
-                    st.l[i] = st.l[i] * fa + ml.y * fb;
-#pragma unroll
-                    for (int nt = 0; nt < D / 8; ++nt) {
-                        const float2 v = *reinterpret_cast<const float2*>(from + nt * 8 + 2 * q4);
-                        st.o[nt][2 * i] = st.o[nt][2 * i] * fa + v.x * fb;
-                        st.o[nt][2 * i + 1] = st.o[nt][2 * i + 1] * fa + v.y * fb;
-                    }
-                }
-            }
-            __syncthreads();
-        }
-        if (group == 0) {
-            // the item's tiles are numbered from here on in the list of all tiles
-            const int list0 = range.end - get_left - count - first;
-            const int b_first = list0 / per, b_last = (list0 + get.end - 1) / per;
-            if (first == 0 && wrow == 0 && lane == 0)
-                p.item_blocks[((long long)get.b * p.c.Hkv + get.h) * p.row_blocks + get.rb] = make_int2(b_first, b_last);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int rl = wrow * 16 + (lane >> 2) + 8 * i, r = get.rb * MB + rl;
+            for (int pass = 0; pass < WM * 8 * TPR / kDecThreads; ++pass) {
+                const int i = pass * (kDecThreads / TPR) + threadIdx.x / TPR, w0 = i >> 3, r8 = i & 7;
+                const int rl = w0 * WR + nt * 8 + r8, r = get.rb * MB + rl;
                 if (r >= rows) continue;
+                float mm = -INFINITY, ll = 0.f;
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int g = 0; g < 4 / WM; ++g) mm = fmaxf(mm, end_ml[g * WM + w0][r8].x);
+                const float base = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+                for (int g = 0; g < 4 / WM; ++g) {
+                    const float2 ml = end_ml[g * WM + w0][r8];
+                    const float f = ex2(ml.x - base);
+                    const float4 y = *reinterpret_cast<const float4*>(
+                        ring_ptr + (size_t)(free_stage * 4 + g * WM + w0) * Sh::kWarpStage + (r8 * D + (d0 ^ ((r8 >> 1) << 3))) * 4);
+                    ll += ml.y * f;
+                    x.x += y.x * f;
+                    x.y += y.y * f;
+                    x.z += y.z * f;
+                    x.w += y.w * f;
+                }
                 if (b_first == b_last) {
                     const int t = (int)fdiv((uint32_t)r, p.f_g), qh = get.h * p.g + r - t * p.g;
-                    const float inv = st.l[i] == 0.f ? 0.f : vs / st.l[i];
-                    __nv_bfloat16* o = p.O + get.b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2];
-                    if (FP8) {
-#pragma unroll
-                        for (int x = 0; x < D / 16; ++x) {
-                            const uint32_t lo2 = pack_bf16(st.o[2 * x][2 * i] * inv, st.o[2 * x + 1][2 * i] * inv);
-                            const uint32_t hi2 = pack_bf16(st.o[2 * x][2 * i + 1] * inv, st.o[2 * x + 1][2 * i + 1] * inv);
-                            *reinterpret_cast<uint2*>(o + 16 * x + 4 * q4) = make_uint2(lo2, hi2);
-                        }
-                    } else {
-#pragma unroll
-                        for (int nt = 0; nt < D / 8; ++nt)
-                            *reinterpret_cast<uint32_t*>(o + nt * 8 + 2 * q4) = pack_bf16(st.o[nt][2 * i] * inv, st.o[nt][2 * i + 1] * inv);
-                    }
-                    if (q4 == 0)
-                        p.LSE[((long long)get.b * p.Hq + qh) * p.c.Lq + t] =
-                            st.l[i] == 0.f ? -INFINITY : (st.m[i] + log2f(st.l[i])) * 0.6931471805599453f;
+                    const float inv = ll == 0.f ? 0.f : vs / ll;
+                    *reinterpret_cast<uint2*>(p.O + get.b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + d0) =
+                        make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+                    if (d0 == 0)
+                        p.LSE[((long long)get.b * p.Hq + qh) * p.c.Lq + t] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
                 } else {
                     // a part: slot 0 where the block's range begins inside the item, else slot 1
                     const long long at = ((long long)blockIdx.x * 2 + (first == 0 ? 1 : 0)) * MB + rl;
-                    float* o = p.part_o + at * D;
-#pragma unroll
-                    for (int nt = 0; nt < D / 8; ++nt) {
-                        if (FP8) {
-                            if (nt & 1) continue;
-                            *reinterpret_cast<float4*>(o + nt * 8 + 4 * q4) = make_float4(
-                                st.o[nt][2 * i] * vs, st.o[nt + 1][2 * i] * vs, st.o[nt][2 * i + 1] * vs, st.o[nt + 1][2 * i + 1] * vs);
-                        } else {
-                            *reinterpret_cast<float2*>(o + nt * 8 + 2 * q4) = make_float2(st.o[nt][2 * i], st.o[nt][2 * i + 1]);
-                        }
-                    }
-                    if (q4 == 0) p.part_ml[at] = make_float2(st.m[i], st.l[i]);
+                    *reinterpret_cast<float4*>(p.part_o + at * D + d0) = make_float4(x.x * vs, x.y * vs, x.z * vs, x.w * vs);
+                    if (d0 == 0) p.part_ml[at] = make_float2(mm, ll);
                 }
             }
         }
+        __syncthreads();
         if (get_left > 0) get.next_item(p);
     }
     cp_async_wait<0>();
