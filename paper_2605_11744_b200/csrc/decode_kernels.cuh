@@ -2,7 +2,7 @@
 //
 // The work is a stream over the visible K and V rows (HBM bound: 4 g flops per byte for g query heads to a KV head), so the
 // kernel is built around the loads.  Its unit is a tile of 64 slots of one item, an item being up to 8 NT WM rows (new row,
-// query head) of one (sequence, KV head).  All tiles of all items form one list, which the grid - two blocks to an SM -
+// query head) of one (sequence, KV head).  All tiles of all items form one list, which the grid - two or three blocks to an SM -
 // cuts into equal ranges by the lengths found in device memory: whatever the batch's mix of lengths and head classes, every
 // SM reads the same number of bytes.  Where a range ends inside an item the block leaves an unnormalised part (O, running
 // base, sum) in the workspace, and decode_join_kernel adds the parts up in the order of the ranges.
@@ -27,8 +27,6 @@
 namespace segattn {
 
 constexpr int kDecThreads = 128;
-constexpr int kDecTile = 64;     // slots in a tile
-constexpr int kDecBlocksPerSm = 2;
 
 struct DecodeParams {
     PagedView c;
@@ -39,8 +37,8 @@ struct DecodeParams {
     float* w_out;                    // or null
     const float *k_scale, *v_scale;  // e4m3 only
     // workspace
-    float* part_o;                   // [grid][2][rows of an item][D]
-    float2* part_ml;                 // [grid][2][rows of an item] (base in log2 units, sum)
+    float* part_o;                   // [grid][2][rows of a unit][D]
+    float2* part_ml;                 // [grid][2][rows of a unit] (base in log2 units, sum)
     int2* item_blocks;               // [B][Hkv][row blocks]: first and last block of the item's tiles
     float* scores;                   // [B][Hkv][g Lq][pitch], log2 units; null unless weights are asked for
     long long q_stride[3], o_stride[3];
@@ -51,8 +49,11 @@ struct DecodeParams {
     int pitch;                       // slots in a row of scores
     int min_tiles;                   // a block's range has at least this many tiles
     float scale_log2;                // sm_scale * log2(e)
-    int n_class[3];                  // KV heads of each class
+    // KV heads are taken in units of one class: 1, 2 or 4 of them, side by side in the block's warps
+    int unit_log[3], units[3];       // by class: heads to a unit (log2), and units
     uint8_t head_class[64];
+    uint8_t head_order[64];          // the heads by class, unit after unit
+    uint8_t head_in_unit[64];        // by head
 };
 
 // Slots [lo, hi) that new row t of a sequence sees through a KV head of class cls.
@@ -70,47 +71,63 @@ __device__ __forceinline__ void visible_slots(const DecodeParams& p, int n, int 
 
 // ---- the list of tiles -------------------------------------------------------------------------------------------
 // Slots the rows of one row block see between them (their lower and upper ends both grow with the row), and its tiles:
-// whole tiles of 64 slots, at least one, so that rows that see nothing are written too.
+// whole tiles of 2^tile_log slots, at least one, so that rows that see nothing are written too.
 template <int MB>
-__device__ __forceinline__ int item_tiles(const DecodeParams& p, int n, int rows, int shift, int cls, int rb, int* lo, int* hi) {
+__device__ __forceinline__ int item_tiles(const DecodeParams& p, int n, int rows, int shift, int cls, int tile_log, int rb, int* lo, int* hi) {
     const int last = min((rb + 1) * MB, rows * p.g) - 1;
     int l0, h0, l1, h1;
     visible_slots(p, n, rows, shift, (int)fdiv((uint32_t)(rb * MB), p.f_g), cls, &l0, &h0);
     visible_slots(p, n, rows, shift, (int)fdiv((uint32_t)last, p.f_g), cls, &l1, &h1);
     *lo = l0;
     *hi = max(h1, l0);
-    return max(1, (*hi + kDecTile - 1) / kDecTile - l0 / kDecTile);
+    return max(1, ((*hi + (1 << tile_log) - 1) >> tile_log) - (l0 >> tile_log));
 }
 
-// Tiles of one sequence's heads of class cls (one head).
-template <int MB>
-__device__ __forceinline__ int class_tiles(const DecodeParams& p, int n, int rows, int shift, int cls) {
+// Tiles of one unit of class cls of a sequence.  A unit's tile has 2^(TILE_LOG - unit_log) slots: the same bytes for all.
+template <int MB, int TILE_LOG>
+__device__ __forceinline__ int unit_tiles(const DecodeParams& p, int n, int rows, int shift, int cls) {
     int sum = 0, lo, hi;
-    for (int rb = 0; rb * MB < rows * p.g; ++rb) sum += item_tiles<MB>(p, n, rows, shift, cls, rb, &lo, &hi);
+    for (int rb = 0; rb * MB < rows * p.g; ++rb) sum += item_tiles<MB>(p, n, rows, shift, cls, TILE_LOG - p.unit_log[cls], rb, &lo, &hi);
     return sum;
 }
 
-// A place in the list: an item and a tile of it.
-template <int MB>
+__device__ __forceinline__ int class_of_unit(const DecodeParams& p, int u, int* first_head) {
+    int cls = 0, first = 0;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+        if (cls == c && u >= p.units[c]) {
+            u -= p.units[c];
+            first += p.units[c] << p.unit_log[c];
+            cls = c + 1;
+        }
+    *first_head = first + (u << p.unit_log[cls]);
+    return cls;
+}
+
+// A place in the list: an item (a row block of a unit of a sequence) and a tile of it.
+template <int MB, int TILE_LOG>
 struct TileCursor {
-    int b, h, rb, n, rows, shift;
-    int lo, hi;     // visible slots of the item
-    int tile, end;  // next tile of the item and the number of its tiles
+    int b, u, rb, n, rows, shift;
+    int cls, log, first_head;    // of the unit; it has 2^log heads
+    int lo, hi;                  // visible slots of the item
+    int tile, end;               // next tile of the item and the number of its tiles
     __device__ __forceinline__ void read_sequence(const DecodeParams& p) {
         n = seq_len(p.c, b);
         rows = new_rows(p.c, b);
         shift = shift_of(p.c, b);
     }
     __device__ __forceinline__ void enter(const DecodeParams& p, int at) {
-        end = item_tiles<MB>(p, n, rows, shift, p.head_class[h], rb, &lo, &hi);
+        cls = class_of_unit(p, u, &first_head);
+        log = p.unit_log[cls];
+        end = item_tiles<MB>(p, n, rows, shift, cls, TILE_LOG - log, rb, &lo, &hi);
         tile = at;
     }
     // the item after this one; the caller knows that there is one
     __device__ __forceinline__ void next_item(const DecodeParams& p) {
         if (++rb * MB >= rows * p.g) {
             rb = 0;
-            if (++h == p.c.Hkv) {
-                h = 0;
+            if (++u == p.units[0] + p.units[1] + p.units[2]) {
+                u = 0;
                 do {
                     ++b;
                     read_sequence(p);
@@ -119,15 +136,17 @@ struct TileCursor {
         }
         enter(p, 0);
     }
-    __device__ __forceinline__ int first_slot() const { return (lo / kDecTile + tile) * kDecTile; }
+    __device__ __forceinline__ int first_slot() const {
+        return ((lo >> (TILE_LOG - log)) + tile) << (TILE_LOG - log);
+    }
 };
 
 // This block's range of tiles, and the item it begins in.  Every block counts the tiles of all sequences: they are read
 // from device memory, so that a captured call follows the lengths.
 struct BlockRange {
-    int begin, end, per, b, h, rb, tile;
+    int begin, end, per, b, u, rb, tile;
 };
-template <int MB>
+template <int MB, int TILE_LOG>
 __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* out, int* warp_sum) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int seg = (p.c.B + kDecThreads - 1) / kDecThreads;
@@ -139,7 +158,7 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
         int sum = 0;
 #pragma unroll
         for (int cls = 0; cls < 3; ++cls)
-            if (p.n_class[cls]) sum += p.n_class[cls] * class_tiles<MB>(p, n, rows, shift, cls);
+            if (p.units[cls]) sum += p.units[cls] * unit_tiles<MB, TILE_LOG>(p, n, rows, shift, cls);
         return sum;
     };
     int mine = 0;
@@ -169,17 +188,20 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
             off -= t;
         }
         const int n = seq_len(p.c, b), rows = new_rows(p.c, b), shift = shift_of(p.c, b);
-        int of_class[3], h = 0, rb = 0;
-#pragma unroll
-        for (int cls = 0; cls < 3; ++cls) of_class[cls] = p.n_class[cls] ? class_tiles<MB>(p, n, rows, shift, cls) : 0;
-        for (;; ++h) {
-            const int c = p.head_class[h], t = c == 0 ? of_class[0] : c == 1 ? of_class[1] : of_class[2];
-            if (off < t) break;
-            off -= t;
+        int u = 0, rb = 0, cls = 0;
+        for (;; ++cls) {
+            const int t = p.units[cls] ? unit_tiles<MB, TILE_LOG>(p, n, rows, shift, cls) : 0;
+            if (off < t * p.units[cls]) {
+                u += off / t;
+                off %= t;
+                break;
+            }
+            off -= t * p.units[cls];
+            u += p.units[cls];
         }
         for (;; ++rb) {
             int lo, hi;
-            const int t = item_tiles<MB>(p, n, rows, shift, p.head_class[h], rb, &lo, &hi);
+            const int t = item_tiles<MB>(p, n, rows, shift, cls, TILE_LOG - p.unit_log[cls], rb, &lo, &hi);
             if (off < t) break;
             off -= t;
         }
@@ -187,7 +209,7 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
         out->end = end;
         out->per = per;
         out->b = b;
-        out->h = h;
+        out->u = u;
         out->rb = rb;
         out->tile = off;
     }
@@ -243,10 +265,10 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// two e4m3 values to two fp16 ones (exact)
-__device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xffffu), __NV_E4M3);
-    return (uint32_t)h.x | ((uint32_t)h.y << 16);
+// four e4m3 values to four fp16 ones (exact): the lower two bytes to lo, the upper two to hi
+__device__ __forceinline__ void e4m3x4_to_half(uint32_t x, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=r"(lo), "=r"(hi) : "r"(x));
 }
 template <bool HALF>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
@@ -263,13 +285,23 @@ __device__ __forceinline__ uint32_t movm_t(uint32_t x) {
     return y;
 }
 
+template <bool V>
+struct Flag {
+    static constexpr bool value = V;
+};
+
 template <int D, bool FP8, int NT, int WM>
 struct DecodeShape {
     static constexpr int RB = D * (FP8 ? 1 : 2);           // bytes of a cache row
-    static constexpr int kStages = RB == 256 ? 3 : RB == 128 ? 6 : 8;
-    static constexpr int kWarpStage = 2 * 16 * RB;         // a warp's 16 K rows and 16 V rows
+    static constexpr int KG = RB == 256 ? 1 : 2;           // blocks of 16 slots of a warp in a tile
+    static constexpr int kTileLog = KG == 1 ? 6 : 7;       // log2 of 64 KG, slots of a tile of one head
+    static constexpr int kBlock = 2 * 16 * RB;             // 16 K rows and 16 V rows
+    static constexpr int kWarpStage = KG * kBlock;
+    static constexpr int kBlocksPerSm = RB == 64 && NT == 1 ? 3 : 2;
+    static constexpr int kStages = RB == 64 ? (NT == 1 ? 4 : 6) : 3;
     static constexpr int kWR = 8 * NT;                     // rows of a warp
-    static constexpr int MB = kWR * WM;                    // rows of an item
+    static constexpr int MB = kWR * WM;                    // rows of an item, of each of its heads
+    static constexpr int kPartRows = WM == 1 ? 4 * kWR : MB;  // rows of a unit's item
     static constexpr int kDynamic = kStages * 4 * kWarpStage + 128;
     static_assert(8 * D * 4 <= kWarpStage, "eight rows of an item's end go through a warp's free stage");
 };
@@ -279,88 +311,110 @@ struct DecodeShape {
 constexpr float kDecSlack = 8.f;
 
 template <int D, bool FP8, int NT, int WM>
-__global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
+__global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
     using Sh = DecodeShape<D, FP8, NT, WM>;
-    constexpr int RB = Sh::RB, C = RB / 16, MB = Sh::MB, WR = Sh::kWR, ST = Sh::kStages, KS = D / 16, MT = D / 16;
+    constexpr int RB = Sh::RB, C = RB / 16, MB = Sh::MB, WR = Sh::kWR, ST = Sh::kStages, KS = D / 16, MT = D / 16, KG = Sh::KG;
     extern __shared__ uint8_t smem_raw[];
     __shared__ BlockRange range;
     __shared__ int warp_sum[4];
-    __shared__ uint32_t there[ST][4];  // which of a warp's 16 slots were loaded, per stage
+    __shared__ uint32_t there[ST][4];  // which of a warp's 16 KG slots were loaded, per stage
     __shared__ float2 end_ml[4][8];    // an item's end: base and sum of eight rows of each warp
     const uint32_t ring = (smem_u32(smem_raw) + 127u) & ~127u;
     uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q4 = lane & 3, l4 = lane >> 2;
-    const int group = warp / WM, wrow = warp % WM;  // key group of this warp, and its rows of the item
+    const int wrow = WM == 1 ? 0 : warp % WM;  // this warp's eight NT rows of the item
+    // with one head to a unit warps WM g .. WM g + WM - 1 share the slots of key group g; with several heads each warp has a
+    // head and a key group of its own
+    auto key_group = [&](int log) { return WM == 1 ? warp >> log : warp / WM; };
+    auto head_of = [&](int first_head, int log) { return (int)p.head_order[first_head + (WM == 1 ? warp & ((1 << log) - 1) : 0)]; };
 
-    find_range<MB>(p, &range, warp_sum);
+    find_range<MB, Sh::kTileLog>(p, &range, warp_sum);
     if (range.begin >= range.end) return;
     const int per = range.per;
-    TileCursor<MB> put, get;  // what is loaded next, and what is computed next
+    TileCursor<MB, Sh::kTileLog> put, get;  // what is loaded next, and what is computed next
     get.b = range.b;
-    get.h = range.h;
+    get.u = range.u;
     get.rb = range.rb;
     get.read_sequence(p);
     get.enter(p, range.tile);
     put = get;
     int put_left = range.end - range.begin, get_left = put_left;
 
-    // ---- one tile's 16 slots of this warp into stage s ----
+    // ---- one tile's 16 KG slots of this warp into stage s ----
     constexpr int RPI = 32 / C;  // rows that one instruction of the warp covers
     const int r0 = lane / C, ch = lane % C;
     const uint32_t put_lane = swizzled<RB>(r0, ch);
+    const char *k_item, *v_item;  // of the item being loaded: this lane's piece of row r0 of page 0
+    auto enter_item = [&]() {
+        const int h = head_of(put.first_head, put.log);
+        k_item = p.c.K + r0 * p.c.k_stride[1] + h * p.c.k_stride[2] + ch * 16;
+        v_item = p.c.V + r0 * p.c.v_stride[1] + h * p.c.v_stride[2] + ch * 16;
+    };
+    // The pages of the tile to be loaded next, looked up one tile ahead: the look-up is a load of its own, and the loads of the
+    // rows wait for it.  An entry of the table outside the visible slots is not read.
+    int page_next[KG];
+    auto look_up = [&]() {
+        const int slot0 = put.first_slot() + (WM == 1 ? key_group(put.log) : warp) * 16 * KG;
+#pragma unroll
+        for (int k = 0; k < KG; ++k) {
+            const int s0 = slot0 + 16 * k;
+            page_next[k] = -1;
+            if (p.page_whole && s0 >= put.lo && s0 + 16 <= put.hi) page_next[k] = table_entry(p.c, put.b, s0);
+        }
+    };
+    enter_item();
+    look_up();
     auto load_tile = [&](int s) {
         if (put_left > 0) {
-            if (put.tile == put.end) put.next_item(p);
-            const int slot0 = put.first_slot() + warp * 16;
-            const uint32_t dst = ring + (uint32_t)(s * 4 + warp) * Sh::kWarpStage + put_lane;
-            if (p.page_whole) {
-                // the 16 slots lie in one page: one look-up, and rows a stride apart
-                int prow = 0, page = -1;
-                if (slot0 + 16 > put.lo && slot0 < put.hi) page = page_of(p.c, put.b, slot0, &prow);
-                const long long pg = max(page, 0);
-                const char* k = p.c.K + pg * p.c.k_stride[0] + (prow + r0) * p.c.k_stride[1] + put.h * p.c.k_stride[2] + ch * 16;
-                const char* v = p.c.V + pg * p.c.v_stride[0] + (prow + r0) * p.c.v_stride[1] + put.h * p.c.v_stride[2] + ch * 16;
-                const bool whole = slot0 >= put.lo && slot0 + 16 <= put.hi && page >= 0;
-                uint32_t loaded = 0xffffu;
-                if (!whole) {
-                    const int a = min(max(put.lo - slot0, 0), 16), z = min(max(put.hi - slot0, 0), 16);
-                    loaded = page >= 0 ? ((1u << z) - 1) & ~((1u << a) - 1) : 0u;
-                }
-                if (lane == 0) there[s][warp] = loaded;
+            const int slot0 = put.first_slot() + (WM == 1 ? key_group(put.log) : warp) * 16 * KG;
+            uint32_t loaded = 0;
 #pragma unroll
-                for (int kv = 0; kv < 2; ++kv) {
-                    const char* src = kv ? v : k;
-                    const long long step = RPI * (kv ? p.c.v_stride[1] : p.c.k_stride[1]);
+            for (int k = 0; k < KG; ++k) {
+                const int s0 = slot0 + 16 * k;
+                const uint32_t dst = ring + (uint32_t)((s * 4 + warp) * KG + k) * Sh::kBlock + put_lane;
+                int prow, page = page_next[k];
+                if ((unsigned)page < (unsigned)p.c.n_pages) {
+                    // 16 visible slots in one page: one look-up, and rows a stride apart
+                    prow = row_in_page(p.c, s0);
+                    const char* src = k_item + page * p.c.k_stride[0] + prow * p.c.k_stride[1];
 #pragma unroll
                     for (int i = 0; i < 16 / RPI; ++i) {
-                        const uint32_t to = (dst ^ swizzled<RB>(i * RPI, 0) % RB) + kv * 16 * RB + i * RPI * RB;
-                        if (whole) cp_async16(to, src);
-                        else cp_async16_if(to, src, (loaded >> (i * RPI + r0)) & 1);
-                        src += step;
+                        cp_async16((dst ^ swizzled<RB>(i * RPI, 0) % RB) + i * RPI * RB, src);
+                        src += RPI * p.c.k_stride[1];
                     }
-                }
-            } else {
-                const int slot = slot0 + (lane & 15);
-                long long off = -1;  // of one row: lanes 0-15 in K, 16-31 in V
-                if (slot >= put.lo && slot < put.hi) {
-                    int prow;
-                    const int page = page_of(p.c, put.b, slot, &prow);
-                    const long long* st = lane < 16 ? p.c.k_stride : p.c.v_stride;
-                    if (page >= 0) off = page * st[0] + prow * st[1] + put.h * st[2];
-                }
-                const uint32_t loaded = __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
-                if (lane == 0) there[s][warp] = loaded;
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv)
+                    src = v_item + page * p.c.v_stride[0] + prow * p.c.v_stride[1];
 #pragma unroll
                     for (int i = 0; i < 16 / RPI; ++i) {
-                        const long long o = __shfl_sync(0xffffffffu, off, kv * 16 + i * RPI + r0);
-                        const uint32_t to = (dst ^ swizzled<RB>(i * RPI, 0) % RB) + kv * 16 * RB + i * RPI * RB;
-                        cp_async16_if(to, (kv ? p.c.V : p.c.K) + (o >= 0 ? o + ch * 16 : 0), o >= 0);
+                        cp_async16((dst ^ swizzled<RB>(i * RPI, 0) % RB) + (16 + i * RPI) * RB, src);
+                        src += RPI * p.c.v_stride[1];
                     }
+                    loaded |= 0xffffu << (16 * k);
+                } else {
+                    const int slot = s0 + (lane & 15);
+                    long long off = -1;  // of one row: lanes 0-15 in K, 16-31 in V
+                    if (slot >= put.lo && slot < put.hi && (page = page_of(p.c, put.b, slot, &prow)) >= 0) {
+                        const long long* st = lane < 16 ? p.c.k_stride : p.c.v_stride;
+                        off = page * st[0] + prow * st[1] + head_of(put.first_head, put.log) * st[2];
+                    }
+                    loaded |= (__ballot_sync(0xffffffffu, off >= 0) & 0xffffu) << (16 * k);
+#pragma unroll 1
+                    for (int i = 0; i < 32 / RPI; ++i) {
+                        const int row = i * RPI + r0;  // 0-15 of K, then of V
+                        const long long o = __shfl_sync(0xffffffffu, off, row);
+                        cp_async16_if(dst - put_lane + (row >> 4) * 16 * RB + swizzled<RB>(row & 15, ch),
+                                      (row & 16 ? p.c.V : p.c.K) + (o >= 0 ? o + ch * 16 : 0), o >= 0);
+                    }
+                }
             }
+            if (lane == 0) there[s][warp] = loaded;
             ++put.tile;
-            --put_left;
+            if (--put_left > 0) {
+                if (put.tile == put.end) {
+                    put.next_item(p);
+                    enter_item();
+                }
+                look_up();
+            }
         }
         cp_async_commit();
     };
@@ -379,20 +433,21 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
     const uint32_t v_lane = 16 * RB + (FP8 ? swizzled<RB>(lane & 15, lane >> 4) : swizzled<RB>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1));
 
     float o[MT][NT][4];        // O^T: (dim l4, row 2 q4), (dim l4, row 2 q4 + 1), (dim l4 + 8, ...) of 16-dim tiles
-    float m[NT][2], l[NT][2];  // base in log2 units; sum over this lane's slots
+    // A row's weights are exp2(score - base) so far: the base (0 until the row has seen a key), the sum over this lane's slots,
+    // and how far over the base a score has to be for the base to move (-inf until the row has seen a key).
+    float base[NT][2], l[NT][2], slack[NT][2];
     uint32_t qf[KS][NT][2];
     float qscale[NT][2];       // score scale of the lane's rows, log2 units
     int rlo[NT][2], rhi[NT][2];  // their visible slots
     while (get_left > 0) {
         // ---- a piece: this block's tiles of one item ----
         const int first = get.tile, count = min(get.end - first, get_left);
-        const int cls = p.head_class[get.h], rows = get.rows * p.g;
-        const float vs = FP8 ? p.v_scale[get.h] : 1.f;
+        const int cls = get.cls, rows = get.rows * p.g, group = key_group(get.log), head = head_of(get.first_head, get.log);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = get.rb * MB + wrow * WR + nt * 8 + l4;  // the row whose elements this lane holds
             const bool real = r < rows;
-            const int t = (int)fdiv((uint32_t)(real ? r : 0), p.f_g), qh = get.h * p.g + (real ? r - t * p.g : 0);
+            const int t = (int)fdiv((uint32_t)(real ? r : 0), p.f_g), qh = head * p.g + (real ? r - t * p.g : 0);
             const __nv_bfloat16* q = p.Q + get.b * p.q_stride[0] + t * p.q_stride[1] + qh * p.q_stride[2];
             float scale = p.scale_log2;
             if (FP8) {
@@ -418,7 +473,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 const int e = big > 0.f ? min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126) : 0;
                 const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-                scale *= p.k_scale[get.h] * __uint_as_float((uint32_t)(127 + e) << 23);
+                scale *= p.k_scale[head] * __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     qf[k][nt][0] = real ? pack16<true>(x[4 * k] * down, x[4 * k + 1] * down) : 0u;
@@ -436,8 +491,8 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
                 const int rc = get.rb * MB + wrow * WR + nt * 8 + 2 * q4 + e;  // a row whose scores this lane holds
                 qscale[nt][e] = FP8 ? __shfl_sync(0xffffffffu, scale, (2 * q4 + e) * 4) : scale;
                 visible_slots(p, get.n, get.rows, get.shift, (int)fdiv((uint32_t)min(rc, rows - 1), p.f_g), cls, &rlo[nt][e], &rhi[nt][e]);
-                m[nt][e] = -INFINITY;
-                l[nt][e] = 0.f;
+                base[nt][e] = l[nt][e] = 0.f;
+                slack[nt][e] = -INFINITY;
             }
         }
 #pragma unroll
@@ -455,89 +510,120 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
             visible_slots(p, get.n, get.rows, get.shift, (int)fdiv((uint32_t)(get.rb * MB), p.f_g), cls, &x, &all_hi);
         }
         float* scores = p.scores;
-        if (scores) scores += (((long long)get.b * p.c.Hkv + get.h) * p.g * p.c.Lq + get.rb * MB + wrow * WR) * p.pitch;
+        if (scores) scores += (((long long)get.b * p.c.Hkv + head) * p.g * p.c.Lq + get.rb * MB + wrow * WR) * p.pitch;
 
         for (int left = count; left > 0; --left) {
             cp_async_wait<ST - 2>();
             if (WM == 1) __syncwarp();
-            else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(32 * WM) : "memory");
+            else asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / WM), "n"(32 * WM) : "memory");
             load_tile(free_stage);
-            // this warp's key group: 16 WM slots, loaded by the group's WM warps
+            // this warp's key group: 16 KG WM slots, loaded by the group's WM warps
 #pragma unroll 1
-            for (int k = 0; k < WM; ++k) {
-                const int slot0 = get.first_slot() + (group * WM + k) * 16;
-                const uint32_t blk = ring + (uint32_t)(stage * 4 + group * WM + k) * Sh::kWarpStage;
-                const uint32_t have = there[stage][group * WM + k];
-                float s[NT][4];
+            for (int w = 0; w < WM; ++w) {
+                const int slot0 = get.first_slot() + (group * WM + w) * 16 * KG;
+                const int from = WM == 1 ? warp : group * WM + w;  // the warp that loaded them
+                const uint32_t blk = ring + (uint32_t)(stage * 4 + from) * Sh::kWarpStage;
+                const uint32_t have = there[stage][from];
+                float s[KG][NT][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
-                if (FP8) {
-#pragma unroll
-                    for (int v = 0; v < D / 64; ++v) {
-                        const uint4 w0 = lds128(blk + (k8_lane[0] ^ (v << 4))), w1 = lds128(blk + (k8_lane[1] ^ (v << 4)));
-                        const uint32_t a0[4] = {w0.x, w0.y, w0.z, w0.w}, a1[4] = {w1.x, w1.y, w1.z, w1.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t a[4] = {e4m3x2_to_half2(a0[j]), e4m3x2_to_half2(a1[j]), e4m3x2_to_half2(a0[j] >> 16),
-                                                   e4m3x2_to_half2(a1[j] >> 16)};
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma16816<true>(s[nt], a, qf[v * 4 + j][nt][0], qf[v * 4 + j][nt][1]);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < KS; ++c) {
-                        uint32_t a[4];
-                        ldsm_x4(blk + (k_lane ^ (c << 5)), a);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16816<false>(s[nt], a, qf[c][nt][0], qf[c][nt][1]);
-                    }
-                }
-                // element e of s[nt]: slot js[e >> 1], row 2 q4 + (e & 1) of the warp's eight
-                const bool edge_range = slot0 < all_lo || slot0 + 16 > all_hi;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[nt][e] *= qscale[nt][e & 1];
-                if (edge_range || have != 0xffffu) {
+                for (int k = 0; k < KG; ++k)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int j = js[e >> 1];
-                            if (slot0 + j < rlo[nt][e & 1] || slot0 + j >= rhi[nt][e & 1] || !((have >> j) & 1)) s[nt][e] = -INFINITY;
+                        for (int e = 0; e < 4; ++e) s[k][nt][e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < KG; ++k) {
+                    if (FP8) {
+#pragma unroll
+                        for (int v = 0; v < D / 64; ++v) {
+                            const uint4 w0 = lds128(blk + k * Sh::kBlock + (k8_lane[0] ^ (v << 4)));
+                            const uint4 w1 = lds128(blk + k * Sh::kBlock + (k8_lane[1] ^ (v << 4)));
+                            const uint32_t a0[4] = {w0.x, w0.y, w0.z, w0.w}, a1[4] = {w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t a[4];
+                                e4m3x4_to_half(a0[j], a[0], a[2]);
+                                e4m3x4_to_half(a1[j], a[1], a[3]);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) mma16816<true>(s[k][nt], a, qf[v * 4 + j][nt][0], qf[v * 4 + j][nt][1]);
+                            }
                         }
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < KS; ++c) {
+                            uint32_t a[4];
+                            ldsm_x4(blk + k * Sh::kBlock + (k_lane ^ (c << 5)), a);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma16816<false>(s[k][nt], a, qf[c][nt][0], qf[c][nt][1]);
+                        }
+                    }
                 }
+                // element e of s[k][nt]: slot 16 k + js[e >> 1], row 2 q4 + (e & 1) of the warp's eight; log2 units over the base
+                const bool edge_range = slot0 < all_lo || slot0 + 16 * KG > all_hi;
                 if (scores) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int r = nt * 8 + 2 * q4 + (e & 1);
-                            if (get.rb * MB + wrow * WR + r < rows) scores[(long long)r * p.pitch + slot0 + js[e >> 1]] = s[nt][e];
+                            if (get.rb * MB + wrow * WR + r < rows)
+#pragma unroll
+                                for (int k = 0; k < KG; ++k)
+                                    scores[(long long)r * p.pitch + slot0 + 16 * k + js[e >> 1]] =
+                                        (have >> (16 * k + js[e >> 1])) & 1 ? s[k][nt][e] * qscale[nt][e & 1] : -INFINITY;
                         }
                 }
                 bool grows = false;
 #pragma unroll
+                for (int k = 0; k < KG; ++k)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[k][nt][e] = fmaf(s[k][nt][e], qscale[nt][e & 1], -base[nt][e & 1]);
+                if (edge_range || have != (KG == 1 ? 0xffffu : 0xffffffffu)) {
+#pragma unroll
+                    for (int k = 0; k < KG; ++k)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int j = 16 * k + js[e >> 1];
+                                if (slot0 + j < rlo[nt][e & 1] || slot0 + j >= rhi[nt][e & 1] || !((have >> j) & 1)) s[k][nt][e] = -INFINITY;
+                            }
+                }
+#pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) grows |= s[nt][e] > m[nt][e & 1] + kDecSlack;
+                    for (int e = 0; e < 2; ++e) {
+                        float mx = fmaxf(s[0][nt][e], s[0][nt][e + 2]);
+                        if (KG > 1) mx = fmaxf(mx, fmaxf(s[KG - 1][nt][e], s[KG - 1][nt][e + 2]));
+                        grows |= mx > slack[nt][e];
+                    }
                 if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float f[2];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float mx = fmaxf(s[nt][e], s[nt][e + 2]);
+                            float mx = fmaxf(s[0][nt][e], s[0][nt][e + 2]);
+                            if (KG > 1) mx = fmaxf(mx, fmaxf(s[KG - 1][nt][e], s[KG - 1][nt][e + 2]));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
                             // row by row: what one row sees must not move another row's base (and with it its rounding)
-                            if (!(mx > m[nt][e] + kDecSlack)) mx = m[nt][e];
-                            f[e] = mx == m[nt][e] ? 1.f : ex2(m[nt][e] - mx);
-                            m[nt][e] = mx;
+                            f[e] = 1.f;
+                            if (mx > slack[nt][e]) {
+                                const float moved = base[nt][e] + mx;
+                                mx = moved - base[nt][e];  // by what the rounded base has moved: scores and sums follow it
+                                f[e] = slack[nt][e] == -INFINITY ? 0.f : ex2(-mx);
+                                base[nt][e] = moved;
+                                slack[nt][e] = kDecSlack;
+#pragma unroll
+                                for (int k = 0; k < KG; ++k) {
+                                    s[k][nt][e] -= mx;
+                                    s[k][nt][e + 2] -= mx;
+                                }
+                            }
                             l[nt][e] *= f[e];
                         }
 #pragma unroll
@@ -546,34 +632,36 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
                             for (int e = 0; e < 4; ++e) o[k2][nt][e] *= f[e & 1];
                     }
                 }
-                uint32_t pf[NT][2];
+                uint32_t pf[KG][NT][2];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
+                for (int k = 0; k < KG; ++k)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float base = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1];
-                        s[nt][e] = ex2(s[nt][e] - base);
-                        l[nt][e & 1] += s[nt][e];
+                    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            s[k][nt][e] = ex2(s[k][nt][e]);
+                            l[nt][e & 1] += s[k][nt][e];
+                        }
+                        pf[k][nt][0] = movm_t(pack16<FP8>(s[k][nt][0], s[k][nt][1]));
+                        pf[k][nt][1] = movm_t(pack16<FP8>(s[k][nt][2], s[k][nt][3]));
                     }
-                    pf[nt][0] = movm_t(pack16<FP8>(s[nt][0], s[nt][1]));
-                    pf[nt][1] = movm_t(pack16<FP8>(s[nt][2], s[nt][3]));
-                }
                 // A weight of zero does not undo an infinite or NaN V: slots that some rows of the item see and others do not
                 // (rows behind a row, slots across a segment's border) are looked at, and where V is not finite its product is
                 // taken out of the mma and added to the rows that see it one by one.
                 uint32_t bad = 0;
                 if (edge_range) {
                     uint32_t part = 0;
-                    for (int j = 0; j < 16; ++j)
+#pragma unroll 1
+                    for (int j = 0; j < 16 * KG; ++j)
                         if (slot0 + j < all_lo || slot0 + j >= all_hi) part |= 1u << j;
                     part &= have;
-                    while (part) {
+#pragma unroll 1
+                    for (; part; part &= part - 1) {
                         const int j = __ffs(part) - 1;
-                        part &= part - 1;
                         bool odd = false;
                         if (lane < C) {
-                            const uint4 w = lds128(blk + 16 * RB + swizzled<RB>(j, lane));
-                            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+                            const uint4 w4 = lds128(blk + (j >> 4) * Sh::kBlock + 16 * RB + swizzled<RB>(j & 15, lane));
+                            const uint32_t ww[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 if (FP8) {
@@ -587,61 +675,79 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
                         if (__any_sync(0xffffffffu, odd)) bad |= 1u << j;
                     }
                 }
-                auto add_values = [&](uint32_t keep0, uint32_t keep1) {
+                auto add_values = [&](auto masked) {
 #pragma unroll
-                    for (int c = 0; c < (FP8 ? MT / 2 : MT); ++c) {
-                        uint32_t b[4];
-                        if (FP8) {
-                            ldsm8_x2_t(blk + (v_lane ^ (c << 5)), b);
-#pragma unroll
-                            for (int x = 0; x < 2; ++x) {
-                                const uint32_t a[4] = {e4m3x2_to_half2(b[2 * x]) & keep0, e4m3x2_to_half2(b[2 * x + 1]) & keep0,
-                                                       e4m3x2_to_half2(b[2 * x] >> 16) & keep1, e4m3x2_to_half2(b[2 * x + 1] >> 16) & keep1};
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) mma16816<true>(o[2 * c + x][nt], a, pf[nt][0], pf[nt][1]);
+                    for (int k = 0; k < KG; ++k) {
+                        // the lane's V fragments hold slots slot_of(2 q4), slot_of(2 q4 + 1) and slot_of(8 + 2 q4), slot_of(9 + 2 q4)
+                        uint32_t keep0 = 0, keep1 = 0;
+                        if (masked.value) {
+                            const uint32_t b16 = bad >> (16 * k);
+                            keep0 = ((b16 >> slot_of(2 * q4)) & 1 ? 0u : 0xffffu) | ((b16 >> slot_of(2 * q4 + 1)) & 1 ? 0u : 0xffff0000u);
+                            keep1 = ((b16 >> slot_of(8 + 2 * q4)) & 1 ? 0u : 0xffffu) | ((b16 >> slot_of(9 + 2 * q4)) & 1 ? 0u : 0xffff0000u);
+                        }
+                        auto product = [&](float (&acc)[NT][4], uint32_t (&a)[4]) {
+                            if (masked.value) {
+                                a[0] &= keep0;
+                                a[1] &= keep0;
+                                a[2] &= keep1;
+                                a[3] &= keep1;
                             }
-                        } else {
-                            ldsm_x4_t(blk + (v_lane ^ (c << 5)), b);
-                            const uint32_t a[4] = {b[0] & keep0, b[1] & keep0, b[2] & keep1, b[3] & keep1};
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma16816<false>(o[c][nt], a, pf[nt][0], pf[nt][1]);
+                            for (int nt = 0; nt < NT; ++nt) mma16816<FP8>(acc[nt], a, pf[k][nt][0], pf[k][nt][1]);
+                        };
+#pragma unroll
+                        for (int c = 0; c < (FP8 ? MT / 2 : MT); ++c) {
+                            uint32_t b[4];
+                            if (FP8) {
+                                ldsm8_x2_t(blk + k * Sh::kBlock + (v_lane ^ (c << 5)), b);
+#pragma unroll
+                                for (int x = 0; x < 2; ++x) {
+                                    uint32_t a[4];
+                                    e4m3x4_to_half(b[2 * x], a[0], a[2]);
+                                    e4m3x4_to_half(b[2 * x + 1], a[1], a[3]);
+                                    product(o[2 * c + x], a);
+                                }
+                            } else {
+                                ldsm_x4_t(blk + k * Sh::kBlock + (v_lane ^ (c << 5)), b);
+                                product(o[c], b);
+                            }
                         }
                     }
                 };
                 if (bad == 0) {
-                    add_values(0xffffffffu, 0xffffffffu);
+                    add_values(Flag<false>());
                 } else {
-                    // the lane's V fragments hold slots slot_of(2 q4), slot_of(2 q4 + 1) and slot_of(8 + 2 q4), slot_of(9 + 2 q4)
-                    add_values(((bad >> slot_of(2 * q4)) & 1 ? 0u : 0xffffu) | ((bad >> slot_of(2 * q4 + 1)) & 1 ? 0u : 0xffff0000u),
-                               ((bad >> slot_of(8 + 2 * q4)) & 1 ? 0u : 0xffffu) | ((bad >> slot_of(9 + 2 * q4)) & 1 ? 0u : 0xffff0000u));
+                    add_values(Flag<true>());
 #pragma unroll 1
                     for (; bad; bad &= bad - 1) {
-                        const int j = __ffs(bad) - 1, slot = slot0 + j;
-                        const int mrow = FP8 ? (j >> 2) * 2 + (j & 1) + ((j >> 1) & 1) * 8 : j;  // slot_of(mrow) = j
-                        const uint32_t vrow = blk + 16 * RB;
+                        const int j = __ffs(bad) - 1, slot = slot0 + j, j16 = j & 15;
+                        const int mrow = FP8 ? (j16 >> 2) * 2 + (j16 & 1) + ((j16 >> 1) & 1) * 8 : j16;  // slot_of(mrow) = j16
+                        const uint32_t vrow = blk + (j >> 4) * Sh::kBlock + 16 * RB;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const float w = __shfl_sync(0xffffffffu, mrow & 8 ? s[nt][2 + e] : s[nt][e], (mrow & 7) * 4 + q4);
+                                const float lo_w = j & 16 ? s[KG - 1][nt][e] : s[0][nt][e], hi_w = j & 16 ? s[KG - 1][nt][2 + e] : s[0][nt][2 + e];
+                                const float wt = __shfl_sync(0xffffffffu, mrow & 8 ? hi_w : lo_w, (mrow & 7) * 4 + q4);
                                 if (slot < rlo[nt][e] || slot >= rhi[nt][e]) continue;
 #pragma unroll
                                 for (int k2 = 0; k2 < MT; ++k2)
 #pragma unroll
                                     for (int hh = 0; hh < 2; ++hh) {
                                         const int byte = (k2 * 16 + l4 + 8 * hh) * (FP8 ? 1 : 2);
-                                        const uint32_t at = vrow + swizzled<RB>(j, byte >> 4) + (byte & 15);
+                                        const uint32_t at = vrow + swizzled<RB>(j16, byte >> 4) + (byte & 15);
                                         float x;
                                         if (FP8) {
-                                            uint32_t raw;
+                                            uint32_t raw, h0, h1;
                                             asm volatile("ld.shared.u8 %0, [%1];" : "=r"(raw) : "r"(at));
-                                            x = __half2float(__ushort_as_half((unsigned short)(e4m3x2_to_half2(raw) & 0xffffu)));
+                                            e4m3x4_to_half(raw, h0, h1);
+                                            x = __half2float(__ushort_as_half((unsigned short)(h0 & 0xffffu)));
                                         } else {
                                             uint16_t raw;
                                             asm volatile("ld.shared.u16 %0, [%1];" : "=h"(raw) : "r"(at));
                                             x = __uint_as_float((uint32_t)raw << 16);
                                         }
-                                        o[k2][nt][2 * hh + e] += w * x;
+                                        o[k2][nt][2 * hh + e] += wt * x;
                                     }
                             }
                     }
@@ -666,8 +772,10 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
         // the item's tiles are numbered from list0 on in the list of all tiles
         const int list0 = range.end - get_left - count - first;
         const int b_first = list0 / per, b_last = (list0 + get.end - 1) / per;
-        if (first == 0 && threadIdx.x == 0)
-            p.item_blocks[((long long)get.b * p.c.Hkv + get.h) * p.row_blocks + get.rb] = make_int2(b_first, b_last);
+        if (first == 0 && threadIdx.x < 1 << get.log)
+            p.item_blocks[((long long)get.b * p.c.Hkv + p.head_order[get.first_head + threadIdx.x]) * p.row_blocks + get.rb] =
+                make_int2(b_first, b_last);
+        const int side = WM == 1 ? 1 << get.log : WM;  // warps w, w + side, ... hold parts of the same rows
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             if (nt > 0 && get.rb * MB + nt * 8 >= rows) break;  // none of the warps' rows from here on is there (WM = 1)
@@ -679,28 +787,27 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
 #pragma unroll
                 for (int e = 0; e < 4; ++e) mine[(2 * q4 + (e & 1)) * D + ((k2 * 16 + l4 + 8 * (e >> 1)) ^ (q4 << 3))] = o[k2][nt][e];
             if (l4 == 0) {
-                end_ml[warp][2 * q4] = make_float2(m[nt][0], l[nt][0]);
-                end_ml[warp][2 * q4 + 1] = make_float2(m[nt][1], l[nt][1]);
+                end_ml[warp][2 * q4] = make_float2(slack[nt][0] == -INFINITY ? -INFINITY : base[nt][0], l[nt][0]);
+                end_ml[warp][2 * q4 + 1] = make_float2(slack[nt][1] == -INFINITY ? -INFINITY : base[nt][1], l[nt][1]);
             }
             __syncthreads();
             constexpr int TPR = D / 4;  // threads to a row
             const int d0 = (threadIdx.x % TPR) * 4;
-#pragma unroll
-            for (int pass = 0; pass < WM * 8 * TPR / kDecThreads; ++pass) {
-                const int i = pass * (kDecThreads / TPR) + threadIdx.x / TPR, w0 = i >> 3, r8 = i & 7;
-                const int rl = w0 * WR + nt * 8 + r8, r = get.rb * MB + rl;
+            for (int i = threadIdx.x / TPR; i < side * 8; i += kDecThreads / TPR) {
+                const int w0 = i >> 3, r8 = i & 7;
+                const int rl = (WM == 1 ? 0 : w0 * WR) + nt * 8 + r8, r = get.rb * MB + rl;
                 if (r >= rows) continue;
+                const int h = p.head_order[get.first_head + (WM == 1 ? w0 : 0)];
+                const float vs = FP8 ? p.v_scale[h] : 1.f;
                 float mm = -INFINITY, ll = 0.f;
                 float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int g = 0; g < 4 / WM; ++g) mm = fmaxf(mm, end_ml[g * WM + w0][r8].x);
-                const float base = mm == -INFINITY ? 0.f : mm;
-#pragma unroll
-                for (int g = 0; g < 4 / WM; ++g) {
-                    const float2 ml = end_ml[g * WM + w0][r8];
-                    const float f = ex2(ml.x - base);
+                for (int w = w0; w < 4; w += side) mm = fmaxf(mm, end_ml[w][r8].x);
+                const float top = mm == -INFINITY ? 0.f : mm;
+                for (int w = w0; w < 4; w += side) {
+                    const float2 ml = end_ml[w][r8];
+                    const float f = ex2(ml.x - top);
                     const float4 y = *reinterpret_cast<const float4*>(
-                        ring_ptr + (size_t)(free_stage * 4 + g * WM + w0) * Sh::kWarpStage + (r8 * D + (d0 ^ ((r8 >> 1) << 3))) * 4);
+                        ring_ptr + (size_t)(free_stage * 4 + w) * Sh::kWarpStage + (r8 * D + (d0 ^ ((r8 >> 1) << 3))) * 4);
                     ll += ml.y * f;
                     x.x += y.x * f;
                     x.y += y.y * f;
@@ -708,7 +815,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
                     x.w += y.w * f;
                 }
                 if (b_first == b_last) {
-                    const int t = (int)fdiv((uint32_t)r, p.f_g), qh = get.h * p.g + r - t * p.g;
+                    const int t = (int)fdiv((uint32_t)r, p.f_g), qh = h * p.g + r - t * p.g;
                     const float inv = ll == 0.f ? 0.f : vs / ll;
                     *reinterpret_cast<uint2*>(p.O + get.b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + d0) =
                         make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
@@ -716,7 +823,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
                         p.LSE[((long long)get.b * p.Hq + qh) * p.c.Lq + t] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
                 } else {
                     // a part: slot 0 where the block's range begins inside the item, else slot 1
-                    const long long at = ((long long)blockIdx.x * 2 + (first == 0 ? 1 : 0)) * MB + rl;
+                    const long long at = ((long long)blockIdx.x * 2 + (first == 0 ? 1 : 0)) * Sh::kPartRows + w0 * WR + nt * 8 + r8;
                     *reinterpret_cast<float4*>(p.part_o + at * D + d0) = make_float4(x.x * vs, x.y * vs, x.z * vs, x.w * vs);
                     if (d0 == 0) p.part_ml[at] = make_float2(mm, ll);
                 }
@@ -730,14 +837,14 @@ __global__ void __launch_bounds__(kDecThreads, kDecBlocksPerSm) decode_kernel(co
 
 // Adds the parts of one row of an item that several blocks share; block.x = the row, block.y = the item.
 template <int D>
-__global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ DecodeParams p, int MB) {
+__global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ DecodeParams p, int MB, int part_rows) {
     const int rb = blockIdx.y % p.row_blocks, u = blockIdx.y / p.row_blocks, h = u % p.c.Hkv, b = u / p.c.Hkv;
     const int rl = blockIdx.x, r = rb * MB + rl;
     if (r >= new_rows(p.c, b) * p.g) return;
     const int2 blocks = p.item_blocks[blockIdx.y];
     if (blocks.x == blocks.y) return;
     // the item's first block holds its part in slot 1 (its range began at or before the item), the others in slot 0
-    auto at = [&](int k) { return ((long long)k * 2 + (k == blocks.x ? 1 : 0)) * MB + rl; };
+    auto at = [&](int k) { return ((long long)k * 2 + (k == blocks.x ? 1 : 0)) * part_rows + p.head_in_unit[h] * MB + rl; };
     float m = -INFINITY, l = 0.f, o = 0.f;
     for (int k = blocks.x; k <= blocks.y; ++k) m = fmaxf(m, p.part_ml[at(k)].x);
     const float base = m == -INFINITY ? 0.f : m;

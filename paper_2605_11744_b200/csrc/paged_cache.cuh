@@ -44,11 +44,17 @@ __device__ __forceinline__ int shift_of(const PagedView& c, int b) {
     if (s < 0) refuse_input(32);
     return max(s, 0);
 }
+// The block table's entry for a slot in [0, cap), unchecked, and the slot's row in its page.
+__device__ __forceinline__ int table_entry(const PagedView& c, int b, int slot) {
+    return __ldg(c.block_table + (long long)b * c.table_stride + fdiv((uint32_t)slot, c.f_page));
+}
+__device__ __forceinline__ int row_in_page(const PagedView& c, int slot) {
+    return slot - (int)(fdiv((uint32_t)slot, c.f_page) * c.f_page.d);
+}
 // Page of a slot in [0, cap) and the row in it; -1 for a page number out of range.
 __device__ __forceinline__ int page_of(const PagedView& c, int b, int slot, int* row) {
-    const int e = (int)fdiv((uint32_t)slot, c.f_page);
-    *row = slot - e * (int)c.f_page.d;
-    const int page = __ldg(c.block_table + (long long)b * c.table_stride + e);
+    *row = row_in_page(c, slot);
+    const int page = table_entry(c, b, slot);
     if ((unsigned)page >= (unsigned)c.n_pages) {
         refuse_input(33);
         return -1;
