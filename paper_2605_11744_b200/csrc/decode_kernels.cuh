@@ -27,6 +27,7 @@
 namespace segattn {
 
 constexpr int kDecThreads = 128;
+constexpr int kDecMaxBlocks = 480;  // blocks a launch has at most: what the parts in the workspace are laid out for
 
 struct DecodeParams {
     PagedView c;
@@ -257,11 +258,11 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 template <bool HALF>
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if (HALF)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -298,6 +299,7 @@ struct DecodeShape {
     static constexpr int kBlock = 2 * 16 * RB;             // 16 K rows and 16 V rows
     static constexpr int kWarpStage = KG * kBlock;
     static constexpr int kBlocksPerSm = RB == 64 && NT == 1 ? 3 : 2;
+    static constexpr int KP = KG == 2 || WM > 1 ? 2 : 1;   // blocks of 16 slots taken through the products at once
     static constexpr int kStages = RB == 64 ? (NT == 1 ? 4 : 6) : 3;
     static constexpr int kWR = 8 * NT;                     // rows of a warp
     static constexpr int MB = kWR * WM;                    // rows of an item, of each of its heads
@@ -313,7 +315,7 @@ constexpr float kDecSlack = 8.f;
 template <int D, bool FP8, int NT, int WM>
 __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
     using Sh = DecodeShape<D, FP8, NT, WM>;
-    constexpr int RB = Sh::RB, C = RB / 16, MB = Sh::MB, WR = Sh::kWR, ST = Sh::kStages, KS = D / 16, MT = D / 16, KG = Sh::KG;
+    constexpr int RB = Sh::RB, C = RB / 16, MB = Sh::MB, WR = Sh::kWR, ST = Sh::kStages, KS = D / 16, MT = D / 16, KG = Sh::KG, KP = Sh::KP;
     extern __shared__ uint8_t smem_raw[];
     __shared__ BlockRange range;
     __shared__ int warp_sum[4];
@@ -519,47 +521,64 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
             load_tile(free_stage);
             // this warp's key group: 16 KG WM slots, loaded by the group's WM warps
 #pragma unroll 1
-            for (int w = 0; w < WM; ++w) {
-                const int slot0 = get.first_slot() + (group * WM + w) * 16 * KG;
-                const int from = WM == 1 ? warp : group * WM + w;  // the warp that loaded them
+            for (int w = 0; w < WM * KG; w += KP) {
+                const int slot0 = get.first_slot() + group * WM * KG * 16 + w * 16;
+                const int from = WM == 1 ? warp : group * WM + w / KG;  // the warp that loaded them, or the first of two
                 const uint32_t blk = ring + (uint32_t)(stage * 4 + from) * Sh::kWarpStage;
-                const uint32_t have = there[stage][from];
-                float s[KG][NT][4];
+                uint32_t have = there[stage][from];
+                if (KP > KG) have |= there[stage][from + 1] << 16;
+                // Products with an accumulator wait for one another, some 30 cycles each: four chains are kept going, over blocks of
+                // slots, rows, and where those are too few over even and odd pieces of the head.
+                constexpr int CH = KP * NT >= 4 ? 1 : 2;
+                float s[KP][NT][4], s2[CH][KP][NT][4];
 #pragma unroll
-                for (int k = 0; k < KG; ++k)
+                for (int x = 0; x < CH; ++x)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int k = 0; k < KP; ++k)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[k][nt][e] = 0.f;
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int k = 0; k < KG; ++k) {
-                    if (FP8) {
+                            for (int e = 0; e < 4; ++e) s2[x][k][nt][e] = 0.f;
+                if (FP8) {
 #pragma unroll
-                        for (int v = 0; v < D / 64; ++v) {
-                            const uint4 w0 = lds128(blk + k * Sh::kBlock + (k8_lane[0] ^ (v << 4)));
-                            const uint4 w1 = lds128(blk + k * Sh::kBlock + (k8_lane[1] ^ (v << 4)));
-                            const uint32_t a0[4] = {w0.x, w0.y, w0.z, w0.w}, a1[4] = {w1.x, w1.y, w1.z, w1.w};
+                    for (int v = 0; v < D / 64; ++v) {
+                        uint4 w0[KP], w1[KP];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                uint32_t a[4];
-                                e4m3x4_to_half(a0[j], a[0], a[2]);
-                                e4m3x4_to_half(a1[j], a[1], a[3]);
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) mma16816<true>(s[k][nt], a, qf[v * 4 + j][nt][0], qf[v * 4 + j][nt][1]);
-                            }
+                        for (int k = 0; k < KP; ++k) {
+                            w0[k] = lds128(blk + k * Sh::kBlock + (k8_lane[0] ^ (v << 4)));
+                            w1[k] = lds128(blk + k * Sh::kBlock + (k8_lane[1] ^ (v << 4)));
                         }
-                    } else {
 #pragma unroll
-                        for (int c = 0; c < KS; ++c) {
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int k = 0; k < KP; ++k) {
+                                uint32_t a[4];
+                                e4m3x4_to_half(j == 0 ? w0[k].x : j == 1 ? w0[k].y : j == 2 ? w0[k].z : w0[k].w, a[0], a[2]);
+                                e4m3x4_to_half(j == 0 ? w1[k].x : j == 1 ? w1[k].y : j == 2 ? w1[k].z : w1[k].w, a[1], a[3]);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+                                    mma16816<true>(s2[j % CH][k][nt], a, qf[v * 4 + j][nt][0], qf[v * 4 + j][nt][1]);
+                            }
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < KS; ++c)
+#pragma unroll
+                        for (int k = 0; k < KP; ++k) {
                             uint32_t a[4];
                             ldsm_x4(blk + k * Sh::kBlock + (k_lane ^ (c << 5)), a);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma16816<false>(s[k][nt], a, qf[c][nt][0], qf[c][nt][1]);
+                            for (int nt = 0; nt < NT; ++nt) mma16816<false>(s2[c % CH][k][nt], a, qf[c][nt][0], qf[c][nt][1]);
                         }
-                    }
                 }
+#pragma unroll
+                for (int k = 0; k < KP; ++k)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[k][nt][e] = CH == 1 ? s2[0][k][nt][e] : s2[0][k][nt][e] + s2[CH - 1][k][nt][e];
                 // element e of s[k][nt]: slot 16 k + js[e >> 1], row 2 q4 + (e & 1) of the warp's eight; log2 units over the base
-                const bool edge_range = slot0 < all_lo || slot0 + 16 * KG > all_hi;
+                const bool edge_range = slot0 < all_lo || slot0 + 16 * KP > all_hi;
                 if (scores) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -568,21 +587,21 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                             const int r = nt * 8 + 2 * q4 + (e & 1);
                             if (get.rb * MB + wrow * WR + r < rows)
 #pragma unroll
-                                for (int k = 0; k < KG; ++k)
+                                for (int k = 0; k < KP; ++k)
                                     scores[(long long)r * p.pitch + slot0 + 16 * k + js[e >> 1]] =
                                         (have >> (16 * k + js[e >> 1])) & 1 ? s[k][nt][e] * qscale[nt][e & 1] : -INFINITY;
                         }
                 }
                 bool grows = false;
 #pragma unroll
-                for (int k = 0; k < KG; ++k)
+                for (int k = 0; k < KP; ++k)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[k][nt][e] = fmaf(s[k][nt][e], qscale[nt][e & 1], -base[nt][e & 1]);
-                if (edge_range || have != (KG == 1 ? 0xffffu : 0xffffffffu)) {
+                if (edge_range || have != (KP == 1 ? 0xffffu : 0xffffffffu)) {
 #pragma unroll
-                    for (int k = 0; k < KG; ++k)
+                    for (int k = 0; k < KP; ++k)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -596,7 +615,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         float mx = fmaxf(s[0][nt][e], s[0][nt][e + 2]);
-                        if (KG > 1) mx = fmaxf(mx, fmaxf(s[KG - 1][nt][e], s[KG - 1][nt][e + 2]));
+                        if (KP > 1) mx = fmaxf(mx, fmaxf(s[KP - 1][nt][e], s[KP - 1][nt][e + 2]));
                         grows |= mx > slack[nt][e];
                     }
                 if (__any_sync(0xffffffffu, grows)) {
@@ -606,7 +625,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             float mx = fmaxf(s[0][nt][e], s[0][nt][e + 2]);
-                            if (KG > 1) mx = fmaxf(mx, fmaxf(s[KG - 1][nt][e], s[KG - 1][nt][e + 2]));
+                            if (KP > 1) mx = fmaxf(mx, fmaxf(s[KP - 1][nt][e], s[KP - 1][nt][e + 2]));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -619,7 +638,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                                 base[nt][e] = moved;
                                 slack[nt][e] = kDecSlack;
 #pragma unroll
-                                for (int k = 0; k < KG; ++k) {
+                                for (int k = 0; k < KP; ++k) {
                                     s[k][nt][e] -= mx;
                                     s[k][nt][e + 2] -= mx;
                                 }
@@ -632,9 +651,9 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                             for (int e = 0; e < 4; ++e) o[k2][nt][e] *= f[e & 1];
                     }
                 }
-                uint32_t pf[KG][NT][2];
+                uint32_t pf[KP][NT][2];
 #pragma unroll
-                for (int k = 0; k < KG; ++k)
+                for (int k = 0; k < KP; ++k)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -652,7 +671,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                 if (edge_range) {
                     uint32_t part = 0;
 #pragma unroll 1
-                    for (int j = 0; j < 16 * KG; ++j)
+                    for (int j = 0; j < 16 * KP; ++j)
                         if (slot0 + j < all_lo || slot0 + j >= all_hi) part |= 1u << j;
                     part &= have;
 #pragma unroll 1
@@ -677,7 +696,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                 }
                 auto add_values = [&](auto masked) {
 #pragma unroll
-                    for (int k = 0; k < KG; ++k) {
+                    for (int k = 0; k < KP; ++k) {
                         // the lane's V fragments hold slots slot_of(2 q4), slot_of(2 q4 + 1) and slot_of(8 + 2 q4), slot_of(9 + 2 q4)
                         uint32_t keep0 = 0, keep1 = 0;
                         if (masked.value) {
@@ -727,7 +746,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const float lo_w = j & 16 ? s[KG - 1][nt][e] : s[0][nt][e], hi_w = j & 16 ? s[KG - 1][nt][2 + e] : s[0][nt][2 + e];
+                                const float lo_w = j & 16 ? s[KP - 1][nt][e] : s[0][nt][e], hi_w = j & 16 ? s[KP - 1][nt][2 + e] : s[0][nt][2 + e];
                                 const float wt = __shfl_sync(0xffffffffu, mrow & 8 ? hi_w : lo_w, (mrow & 7) * 4 + q4);
                                 if (slot < rlo[nt][e] || slot >= rhi[nt][e]) continue;
 #pragma unroll
@@ -835,49 +854,95 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
     cp_async_wait<0>();
 }
 
-// Adds the parts of one row of an item that several blocks share; block.x = the row, block.y = the item.
+// Adds the parts of one row of an item that several blocks share; block.x = the row, block.y = the item, a thread one dim.
+// A row has at most as many parts as the grid has blocks: their bases and sums are read by all threads at once, and the first
+// values of O beside them, so that two dependent reads are all the latency there is.
 template <int D>
 __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ DecodeParams p, int MB, int part_rows) {
+    constexpr int AHEAD = 8;
     const int rb = blockIdx.y % p.row_blocks, u = blockIdx.y / p.row_blocks, h = u % p.c.Hkv, b = u / p.c.Hkv;
-    const int rl = blockIdx.x, r = rb * MB + rl;
+    const int rl = blockIdx.x, r = rb * MB + rl, tid = threadIdx.x;
     if (r >= new_rows(p.c, b) * p.g) return;
     const int2 blocks = p.item_blocks[blockIdx.y];
     if (blocks.x == blocks.y) return;
+    __shared__ float weight[kDecMaxBlocks];
+    __shared__ float red[2][D / 32];
+    const int n = blocks.y - blocks.x + 1;
     // the item's first block holds its part in slot 1 (its range began at or before the item), the others in slot 0
-    auto at = [&](int k) { return ((long long)k * 2 + (k == blocks.x ? 1 : 0)) * part_rows + p.head_in_unit[h] * MB + rl; };
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int k = blocks.x; k <= blocks.y; ++k) m = fmaxf(m, p.part_ml[at(k)].x);
+    auto at = [&](int k) { return ((long long)(blocks.x + k) * 2 + (k == 0 ? 1 : 0)) * part_rows + p.head_in_unit[h] * MB + rl; };
+    float ahead[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) ahead[k] = k < n ? p.part_o[at(k) * D + tid] : 0.f;
+    float m = -INFINITY;
+    for (int k = tid; k < n; k += D) m = fmaxf(m, p.part_ml[at(k)].x);
+#pragma unroll
+    for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+    if ((tid & 31) == 0) red[0][tid >> 5] = m;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) m = fmaxf(m, red[0][k]);
     const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll 4
-    for (int k = blocks.x; k <= blocks.y; ++k) {
+    float l = 0.f;
+    for (int k = tid; k < n; k += D) {
         const float2 ml = p.part_ml[at(k)];
-        const float f = ex2(ml.x - base);
-        l += ml.y * f;
-        o += p.part_o[at(k) * D + threadIdx.x] * f;
+        weight[k] = ex2(ml.x - base);
+        l += ml.y * weight[k];
     }
+#pragma unroll
+    for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+    if ((tid & 31) == 0) red[1][tid >> 5] = l;
+    __syncthreads();
+    l = 0.f;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) l += red[1][k];
+    float o = 0.f;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+        if (k < n) o += ahead[k] * weight[k];
+#pragma unroll 8
+    for (int k = AHEAD; k < n; ++k) o += p.part_o[at(k) * D + tid] * weight[k];
     const int t = (int)fdiv((uint32_t)r, p.f_g), qh = h * p.g + r - t * p.g;
-    p.O[b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + threadIdx.x] = __float2bfloat16(l == 0.f ? 0.f : o / l);
-    if (threadIdx.x == 0) p.LSE[((long long)b * p.Hq + qh) * p.c.Lq + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    p.O[b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + tid] = __float2bfloat16(l == 0.f ? 0.f : o / l);
+    if (tid == 0) p.LSE[((long long)b * p.Hq + qh) * p.c.Lq + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// Attention weight of every slot, from the scores and the finished LSE: one thread per slot.
+// Attention weight of every slot, from the scores and the finished LSE: a block takes 256 slots of one (sequence, KV head), a
+// thread one slot, over the rows in chunks whose LSE and visible slots lie in shared memory.  A stream over the scores: eight
+// loads are in flight per thread (a slot a row does not see is loaded and dropped: the workspace has room for every slot).
+constexpr int kWeightRows = 128;
 __global__ void __launch_bounds__(256) decode_weights_kernel(const __grid_constant__ DecodeParams p) {
     const int j = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y, b = blockIdx.z;
     const int rows = new_rows(p.c, b), n = seq_len(p.c, b);
-    if (j >= n || rows == 0) return;
+    if (blockIdx.x * 256 >= n || rows == 0) return;
+    __shared__ float lse2[kWeightRows];
+    __shared__ int lo[kWeightRows], hi[kWeightRows];
     const int shift = shift_of(p.c, b), cls = p.head_class[h];
     const long long unit = (long long)b * p.c.Hkv + h;
-    const float* s = p.scores + unit * p.g * p.c.Lq * p.pitch + j;
     float sum = 0.f;
-    for (int t = 0; t < rows; ++t) {
-        int lo, hi;
-        visible_slots(p, n, rows, shift, t, cls, &lo, &hi);
-        if (j < lo || j >= hi) continue;
-        for (int k = 0; k < p.g; ++k) {
-            const float lse = p.LSE[((long long)b * p.Hq + h * p.g + k) * p.c.Lq + t];
-            if (lse != -INFINITY) sum += ex2(s[(long long)(t * p.g + k) * p.pitch] - lse * 1.4426950408889634f);
+    for (int r0 = 0; r0 < rows * p.g; r0 += kWeightRows) {
+        const int m = min(kWeightRows, rows * p.g - r0);
+        if (threadIdx.x < m) {
+            const int r = r0 + threadIdx.x, t = (int)fdiv((uint32_t)r, p.f_g);
+            const float x = p.LSE[((long long)b * p.Hq + h * p.g + r - t * p.g) * p.c.Lq + t];
+            visible_slots(p, n, rows, shift, t, cls, &lo[threadIdx.x], &hi[threadIdx.x]);
+            lse2[threadIdx.x] = x * 1.4426950408889634f;
+            if (x == -INFINITY) hi[threadIdx.x] = lo[threadIdx.x];
         }
+        __syncthreads();
+        if (j < n && j >= lo[0]) {  // the rows' lower ends only grow
+            const float* s = p.scores + (unit * p.g * p.c.Lq + r0) * p.pitch + j;
+            for (int r = 0; r < m; r += 8) {
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = r + k < m ? s[(long long)(r + k) * p.pitch] : 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (r + k < m && j >= lo[r + k] && j < hi[r + k]) sum += ex2(x[k] - lse2[r + k]);
+            }
+        }
+        __syncthreads();
     }
+    if (j >= n) return;
     const long long at = unit * p.W + j;
     p.w_out[at] = (p.w_in ? p.w_in[at] : 0.f) + sum;
 }
