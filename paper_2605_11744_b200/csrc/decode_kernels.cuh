@@ -57,6 +57,11 @@ struct DecodeParams {
     uint8_t head_in_unit[64];        // by head
 };
 
+// Programmatic launch: the next kernel of the stream may be set up from here on, and this kernel waits for the end (and the
+// writes) of the one before it.
+__device__ __forceinline__ void next_kernel_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void after_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Slots [lo, hi) that new row t of a sequence sees through a KV head of class cls.
 __device__ __forceinline__ void visible_slots(const DecodeParams& p, int n, int rows, int shift, int t, int cls, int* lo, int* hi) {
     const int slot = n - rows + t;
@@ -330,6 +335,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
     auto key_group = [&](int log) { return WM == 1 ? warp >> log : warp / WM; };
     auto head_of = [&](int first_head, int log) { return (int)p.head_order[first_head + (WM == 1 ? warp & ((1 << log) - 1) : 0)]; };
 
+    next_kernel_may_start();
     find_range<MB, Sh::kTileLog>(p, &range, warp_sum);
     if (range.begin >= range.end) return;
     const int per = range.per;
@@ -862,6 +868,7 @@ __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ 
     constexpr int AHEAD = 8;
     const int rb = blockIdx.y % p.row_blocks, u = blockIdx.y / p.row_blocks, h = u % p.c.Hkv, b = u / p.c.Hkv;
     const int rl = blockIdx.x, r = rb * MB + rl, tid = threadIdx.x;
+    after_previous_kernel();
     if (r >= new_rows(p.c, b) * p.g) return;
     const int2 blocks = p.item_blocks[blockIdx.y];
     if (blocks.x == blocks.y) return;
@@ -912,6 +919,7 @@ __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ 
 constexpr int kWeightRows = 128;
 __global__ void __launch_bounds__(256) decode_weights_kernel(const __grid_constant__ DecodeParams p) {
     const int j = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y, b = blockIdx.z;
+    after_previous_kernel();
     const int rows = new_rows(p.c, b), n = seq_len(p.c, b);
     if (blockIdx.x * 256 >= n || rows == 0) return;
     __shared__ float lse2[kWeightRows];

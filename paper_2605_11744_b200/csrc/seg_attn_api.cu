@@ -62,22 +62,40 @@ segattn_status cuda_fail(cudaError_t e) {
     return SEGATTN_ERR_CUDA;
 }
 
-segattn_status check_arch() {
-    int dev = 0, major = 0;
+// What the launches need to know of a device, asked for once: compute capability and number of SMs, packed as
+// major << 16 | SMs; 0 = not asked yet.
+constexpr int kMaxDevices = 64;
+std::atomic<int> g_device_facts[kMaxDevices];
+
+segattn_status device_facts(int* facts) {
+    int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return cuda_fail(e);
+    if (dev < 0 || dev >= kMaxDevices) return SEGATTN_ERR_INVALID;
+    *facts = g_device_facts[dev].load(std::memory_order_relaxed);
+    if (*facts) return SEGATTN_OK;
+    int major = 0, sms = 0;
     e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return cuda_fail(e);
-    return major == 10 ? SEGATTN_OK : SEGATTN_ERR_UNSUPPORTED_ARCH;
+    *facts = (major << 16) | (sms & 0xffff);
+    g_device_facts[dev].store(*facts, std::memory_order_relaxed);
+    return SEGATTN_OK;
+}
+
+segattn_status check_arch() {
+    int facts = 0;
+    const segattn_status st = device_facts(&facts);
+    if (st != SEGATTN_OK) return st;
+    return (facts >> 16) == 10 ? SEGATTN_OK : SEGATTN_ERR_UNSUPPORTED_ARCH;
 }
 
 // number of SMs of the current device
 segattn_status sm_count(int* n) {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return cuda_fail(e);
-    e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return cuda_fail(e);
+    int facts = 0;
+    const segattn_status st = device_facts(&facts);
+    if (st != SEGATTN_OK) return st;
+    *n = facts & 0xffff;
     return *n > 0 ? SEGATTN_OK : SEGATTN_ERR_CUDA;
 }
 
@@ -385,7 +403,6 @@ static __device__ __align__(256) float g_static_row_dots[SEG_ATTN_STATIC_MAX_ROW
 
 namespace {
 
-constexpr int kMaxDevices = 64;
 std::mutex g_static_mu;
 float* g_static_ptr[kMaxDevices] = {};  // per device: address of g_static_row_dots on that device
 

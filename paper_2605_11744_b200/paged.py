@@ -27,6 +27,11 @@ _STRIDE3 = struct.Struct("3q")
 _SCALING = struct.Struct("i4x6d")      # seg_rope_scaling
 _LAYOUTS = {"half": 0, "interleaved": 1}
 _KINDS = {"plain": 0, "linear": 1, "by_parts": 2}
+_BF16, _E4M3, _I32, _F32 = torch.bfloat16, torch.float8_e4m3fn, torch.int32, torch.float32
+# A decoding step's calls last a few microseconds on the device, so their way there counts: devices are compared by number,
+# structures packed in one go, and the current stream is asked for as torch's own generated code asks for it (a Stream object
+# costs as much as a launch).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
 
 
 def _check(status: int, where: str):
@@ -44,75 +49,89 @@ def _layout(name) -> int:
     return _LAYOUTS[name]
 
 
-def _rows4(t: torch.Tensor, shape, what: str) -> bytes:
-    """The (batch, row, head) strides of a bf16 CUDA tensor of this shape, the last dimension contiguous."""
-    if t.dtype is not torch.bfloat16 or not t.is_cuda or t.shape != shape:
-        raise ValueError("%s must be a bf16 CUDA tensor of shape %s" % (what, tuple(shape)))
+def _rows4(t: torch.Tensor, shape, what: str, dev: int) -> bytes:
+    """The (batch, row, head) strides of a bf16 tensor of this shape on CUDA device `dev`, the last dimension contiguous."""
+    if t.dtype is not _BF16 or dev < 0 or t.get_device() != dev or t.shape != shape:
+        raise ValueError("%s must be a bf16 CUDA tensor of shape %s on the device of the others" % (what, tuple(shape)))
     s = t.stride()
     if s[3] != 1:
         raise ValueError("%s must have a contiguous last dimension" % what)
     return _STRIDE3.pack(s[0], s[1], s[2])
 
 
-def _flat(t, dtype, shape, what: str, device):
-    """A contiguous CUDA tensor of this type and shape on this device, or None."""
-    if t is not None and (t.dtype is not dtype or t.device != device or t.shape != shape or not t.is_contiguous()):
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
+def _flat(t, dtype, shape, what: str, dev: int):
+    """A contiguous tensor of this type and shape on CUDA device `dev`."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on CUDA device %d" % (what, dtype, tuple(shape), dev))
     return t
 
 
-def _on(device, stream):
-    """The stream to launch on: the given one, or the tensors' device's current one."""
+def _call(dev: int, stream, fn, where: str, *args):
+    """One C call with the tensors' device current, on the given stream of that device or its current one."""
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    elif stream.device != device:
+        stream = _raw_stream(dev)
+    elif stream.device_index != dev:
         raise ValueError("the stream belongs to another device than the tensors")
-    return stream.cuda_stream
-
-
-def _call(device, fn, where, *args):
-    """One C call with the tensors' device current."""
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args), where)
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args), where)
+        stream = stream.cuda_stream
+    if torch.cuda.current_device() == dev:
+        _check(fn(*args, stream), where)
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, stream), where)
+
+
+def _mask_bytes(head_past_mask, Hkv: int) -> bytes:
+    """One head class per KV head, as seg_attn_fwd takes them."""
+    if type(head_past_mask) in (list, tuple) and len(head_past_mask) == Hkv:
+        try:
+            return bytes(head_past_mask)
+        except (TypeError, ValueError):
+            pass
+    return _mask_arr(head_past_mask, Hkv).tobytes()
 
 
 def _cache(K, V, block_table, kv_len, q_len, pos_shift, k_scale, v_scale):
-    """seg_kv_cache of these tensors as bytes, and (B, Hkv, d, page_size, max_pages)."""
-    dev = K.device
-    if K.dim() != 4 or K.shape != V.shape or not K.is_cuda or V.device != dev or K.dtype is not V.dtype:
+    """seg_kv_cache of these tensors as bytes, and (B, Hkv, d, page_size, max_pages, CUDA device)."""
+    dev, kind = K.get_device(), K.dtype
+    shape = K.shape
+    if dev < 0 or len(shape) != 4 or shape != V.shape or V.get_device() != dev or V.dtype is not kind:
         raise ValueError("K_pages and V_pages must be CUDA tensors [n_pages, page_size, Hkv, d] of one shape, type and device")
-    if K.dtype is torch.bfloat16:
-        kind = 0
-        if k_scale is not None or v_scale is not None:
-            raise ValueError("scales belong to an 8-bit cache")
-    elif K.dtype is torch.float8_e4m3fn:
-        kind = 1
+    n_pages, page, Hkv, d = shape
+    ks_ptr = vs_ptr = 0
+    if kind is _E4M3:
         if k_scale is None or v_scale is None:
             raise ValueError("an 8-bit cache needs k_scale and v_scale")
-    else:
+        ks_ptr = _flat(k_scale, _F32, (Hkv,), "k_scale", dev).data_ptr()
+        vs_ptr = _flat(v_scale, _F32, (Hkv,), "v_scale", dev).data_ptr()
+    elif kind is not _BF16:
         raise ValueError("the cache must be bf16 or float8_e4m3fn")
-    n_pages, page, Hkv, d = K.shape
-    ks, vs = K.stride(), V.stride()
-    if ks[3] != 1 or vs[3] != 1:
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("scales belong to an 8-bit cache")
+    k, v = K.stride(), V.stride()
+    if k[3] != 1 or v[3] != 1:
         raise ValueError("the pages must have a contiguous last dimension")
-    if block_table.dim() != 2 or block_table.dtype is not torch.int32 or block_table.device != dev or block_table.stride(1) != 1:
-        raise ValueError("block_table must be an int32 tensor [B, max_pages] on %s with contiguous rows" % dev)
-    B, max_pages = block_table.shape
-    if kv_len is None:
-        raise ValueError("kv_len is needed")
-    for t, what in ((kv_len, "kv_len"), (q_len, "q_len"), (pos_shift, "pos_shift")):
-        _flat(t, torch.int32, (B,), what, dev)
-    _flat(k_scale, torch.float32, (Hkv,), "k_scale", dev)
-    _flat(v_scale, torch.float32, (Hkv,), "v_scale", dev)
-    c = _CACHE.pack(B, Hkv, d, kind, page, n_pages, max_pages, max(block_table.stride(0), max_pages) if B > 1 else max_pages,
-                    K.data_ptr(), V.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], _p(k_scale) or 0, _p(v_scale) or 0,
-                    block_table.data_ptr(), kv_len.data_ptr(), _p(q_len) or 0, _p(pos_shift) or 0)
-    if B > 1 and block_table.stride(0) < max_pages:
-        raise ValueError("the rows of block_table overlap")
-    return c, B, Hkv, d, page, max_pages
+    table = _pages(block_table, None, "block_table", dev)
+    B = table[0]
+    _flat(kv_len, _I32, (B,), "kv_len", dev)
+    if q_len is not None:
+        _flat(q_len, _I32, (B,), "q_len", dev)
+    if pos_shift is not None:
+        _flat(pos_shift, _I32, (B,), "pos_shift", dev)
+    c = _CACHE.pack(B, Hkv, d, kind is _E4M3, page, n_pages, table[1], table[2], K.data_ptr(), V.data_ptr(), k[0], k[1], k[2], v[0],
+                    v[1], v[2], ks_ptr, vs_ptr, block_table.data_ptr(), kv_len.data_ptr(), _p(q_len) or 0, _p(pos_shift) or 0)
+    return c, B, Hkv, d, page, table[1], dev
+
+
+def _pages(t, B, what: str, dev: int):
+    """(B, entries of a row, elements between rows) of a table of page numbers."""
+    if t.dtype is not _I32 or t.get_device() != dev or t.dim() != 2 or (B is not None and t.shape[0] != B):
+        raise ValueError("%s must be an int32 tensor [B, pages] on CUDA device %d" % (what, dev))
+    rows, n = t.shape
+    s = t.stride()
+    if (n > 1 and s[1] != 1) or (rows > 1 and s[0] < n):
+        raise ValueError("%s must have contiguous rows that do not overlap" % what)
+    return rows, n, s[0] if rows > 1 else n
 
 
 def rope_table_scaled(n_pos: int, rot_dim: int, base: float = 10000.0, kind: str = "plain", factor: float = 1.0,
@@ -125,17 +144,17 @@ def rope_table_scaled(n_pos: int, rot_dim: int, base: float = 10000.0, kind: str
         raise ValueError("kind must be 'plain', 'linear' or 'by_parts'")
     if n_pos < 0 or rot_dim < 0:
         raise SegAttnError(1, "seg_rope_table_scaled")
-    table = torch.empty((n_pos, rot_dim // 2, 2), dtype=torch.float32, device=device)
+    table = torch.empty((n_pos, rot_dim // 2, 2), dtype=_F32, device=device)
+    if not table.is_cuda:
+        raise ValueError("the table lies on a CUDA device")
     sc = _SCALING.pack(_KINDS[kind], base, factor, trained_len, turns_lo, turns_hi, amplitude)
-    _call(table.device, lib().seg_rope_table_scaled, "seg_rope_table_scaled", n_pos, rot_dim, sc, table.data_ptr(),
-          _on(table.device, stream))
+    _call(table.get_device(), stream, lib().seg_rope_table_scaled, "seg_rope_table_scaled", n_pos, rot_dim, sc, table.data_ptr())
     return table
 
 
-def _table(table, device):
-    if (table.dim() != 3 or table.shape[2] != 2 or table.dtype is not torch.float32 or table.device != device or
-            not table.is_contiguous()):
-        raise ValueError("table must be a contiguous fp32 tensor [n_pos, rot_dim/2, 2] on %s" % device)
+def _table(table, dev: int):
+    if table.dim() != 3 or table.shape[2] != 2 or table.dtype is not _F32 or table.get_device() != dev or not table.is_contiguous():
+        raise ValueError("table must be a contiguous fp32 tensor [n_pos, rot_dim/2, 2] on CUDA device %d" % dev)
     return table.shape[0], 2 * table.shape[1]
 
 
@@ -145,22 +164,23 @@ def rope_rotate(X, table, positions: Optional[torch.Tensor] = None, pos0: int = 
     rope_table_scaled, whose width is the part of the head that turns - the C entry point `seg_rope_rotate`.  `layout` names
     the pairs: "half" (x[i], x[i + rot/2]) or "interleaved" (x[2i], x[2i+1]).  inverse=True applies the transposed map, which
     takes the gradient of the output to that of X.  `out` may be X."""
-    if X.dim() != 4:
+    shape, dev = X.shape, X.get_device()
+    if len(shape) != 4:
         raise ValueError("X must be [B, L, H, d]")
-    xs = _rows4(X, X.shape, "X")
-    Y = torch.empty(X.shape, dtype=X.dtype, device=X.device) if out is None else out
-    ys = _rows4(Y, X.shape, "out") if out is not None else _STRIDE3.pack(*Y.stride()[:3])
-    dev = X.device
-    if Y.device != dev:
-        raise ValueError("out must be on the device of X")
-    if Y.data_ptr() == X.data_ptr() and X.numel() and xs != ys:
+    xs = _rows4(X, shape, "X", dev)
+    if out is None:
+        out = torch.empty_like(X)
+    ys = _rows4(out, shape, "out", dev)
+    x, y = X.data_ptr(), out.data_ptr()
+    if x == y and x and xs != ys:
         raise ValueError("a rotation in place needs the strides of X")
     n_pos, rot = _table(table, dev)
-    B, L, H, d = X.shape
-    _flat(positions, torch.int32, (B, L), "positions", dev)
-    _call(dev, lib().seg_rope_rotate, "seg_rope_rotate", B, L, H, d, rot, _layout(layout), X.data_ptr(), xs, Y.data_ptr(), ys,
-          _p(positions), pos0, int(bool(inverse)), table.data_ptr(), n_pos, _on(dev, stream))
-    return Y
+    B, L, H, d = shape
+    if positions is not None:
+        _flat(positions, _I32, (B, L), "positions", dev)
+    _call(dev, stream, lib().seg_rope_rotate, "seg_rope_rotate", B, L, H, d, rot, _layout(layout), x, xs, y, ys, _p(positions), pos0,
+          1 if inverse else 0, table.data_ptr(), n_pos)
+    return out
 
 
 def kv_append(K_new, V_new, K_pages, V_pages, block_table, kv_len, table: Optional[torch.Tensor] = None, layout: str = "half",
@@ -169,12 +189,11 @@ def kv_append(K_new, V_new, K_pages, V_pages, block_table, kv_len, table: Option
     """New rows K_new, V_new [B, Lq, Hkv, d] into the cache; with a table the keys, and the queries Q [B, Lq, Hq, d] if given,
     are rotated at their positions - the C entry point `seg_kv_append`.  Returns the rotated queries (q_out, which may be Q),
     or None.  kv_len counts the new rows already."""
-    c, B, Hkv, d, _, _ = _cache(K_pages, V_pages, block_table, kv_len, q_len, pos_shift, k_scale, v_scale)
-    dev = K_pages.device
-    if K_new.dim() != 4 or K_new.device != dev or V_new.device != dev:
-        raise ValueError("K_new and V_new must be [B, Lq, Hkv, d] on the cache's device")
+    c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, q_len, pos_shift, k_scale, v_scale)
+    if K_new.dim() != 4:
+        raise ValueError("K_new and V_new must be [B, Lq, Hkv, d]")
     Lq = K_new.shape[1]
-    kn, vn = _rows4(K_new, (B, Lq, Hkv, d), "K_new"), _rows4(V_new, (B, Lq, Hkv, d), "V_new")
+    kn, vn = _rows4(K_new, (B, Lq, Hkv, d), "K_new", dev), _rows4(V_new, (B, Lq, Hkv, d), "V_new", dev)
     n_pos = rot = Hq = 0
     if table is not None:
         n_pos, rot = _table(table, dev)
@@ -183,18 +202,16 @@ def kv_append(K_new, V_new, K_pages, V_pages, block_table, kv_len, table: Option
         if table is None:
             raise ValueError("queries are rotated by a table")
         Hq = Q.shape[2] if Q.dim() == 4 else 0
-        qs = _rows4(Q, (B, Lq, Hq, d), "Q")
+        qs = _rows4(Q, (B, Lq, Hq, d), "Q", dev)
         if q_out is None:
-            q_out = torch.empty(Q.shape, dtype=Q.dtype, device=dev)
-        qo = _rows4(q_out, (B, Lq, Hq, d), "q_out")
-        if Q.device != dev or q_out.device != dev:
-            raise ValueError("Q and q_out must be on the cache's device")
-        if q_out.data_ptr() == Q.data_ptr() and Q.numel() and qs != qo:
+            q_out = torch.empty_like(Q)
+        qo = _rows4(q_out, (B, Lq, Hq, d), "q_out", dev)
+        if q_out.data_ptr() == Q.data_ptr() and qs != qo and Q.numel():
             raise ValueError("a rotation in place needs the strides of Q")
     elif q_out is not None:
         raise ValueError("q_out needs Q")
-    _call(dev, lib().seg_kv_append, "seg_kv_append", c, Lq, K_new.data_ptr(), kn, V_new.data_ptr(), vn, Hq, _p(Q), qs, _p(q_out),
-          qo, _p(table), n_pos, rot, _layout(layout), _on(dev, stream))
+    _call(dev, stream, lib().seg_kv_append, "seg_kv_append", c, Lq, K_new.data_ptr(), kn, V_new.data_ptr(), vn, Hq, _p(Q), qs,
+          _p(q_out), qo, _p(table), n_pos, rot, _layout(layout))
     return q_out
 
 
@@ -206,39 +223,36 @@ def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, he
     (segments of S, tail T, one head class per KV head).  weights_out [B, Hkv, W] fp32, W >= max_pages * page_size, takes
     every slot's attention weight summed over the rows and query heads of its KV head, added to `weights` if given (which may
     be the same tensor).  Rows from q_len on, in O and in LSE, are left as they were."""
-    c, B, Hkv, d, page, max_pages = _cache(K_pages, V_pages, block_table, kv_len, q_len, pos_shift, k_scale, v_scale)
-    dev = K_pages.device
-    if Q.dim() != 4 or Q.device != dev:
-        raise ValueError("Q must be [B, Lq, Hq, d] on the cache's device")
+    c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, q_len, pos_shift, k_scale, v_scale)
+    if Q.dim() != 4:
+        raise ValueError("Q must be [B, Lq, Hq, d]")
     Lq, Hq = Q.shape[1], Q.shape[2]
-    qs = _rows4(Q, (B, Lq, Hq, d), "Q")
+    shape = (B, Lq, Hq, d)
+    qs = _rows4(Q, shape, "Q", dev)
     if out is None:
-        out = torch.empty((B, Lq, Hq, d), dtype=torch.bfloat16, device=dev)
-    elif out.device != dev:
-        raise ValueError("out must be on the cache's device")
-    os_ = _rows4(out, (B, Lq, Hq, d), "out")
+        out = torch.empty_like(Q)
+    os_ = _rows4(out, shape, "out", dev)
     if lse is None:
-        lse = torch.empty((B, Hq, Lq), dtype=torch.float32, device=dev)
+        lse = Q.new_empty((B, Hq, Lq), dtype=_F32)
     else:
-        _flat(lse, torch.float32, (B, Hq, Lq), "lse", dev)
+        _flat(lse, _F32, (B, Hq, Lq), "lse", dev)
     W = 0
     if weights_out is not None:
         W = weights_out.shape[-1] if weights_out.dim() == 3 else 0
-        _flat(weights_out, torch.float32, (B, Hkv, W), "weights_out", dev)
-        _flat(weights, torch.float32, (B, Hkv, W), "weights", dev)
+        _flat(weights_out, _F32, (B, Hkv, W), "weights_out", dev)
+        if weights is not None:
+            _flat(weights, _F32, (B, Hkv, W), "weights", dev)
     elif weights is not None:
         raise ValueError("weights are added to in weights_out: pass that too (it may be the same tensor)")
-    m = _mask_arr(head_past_mask, Hkv)
     L = lib()
-    need = L.seg_attn_decode_workspace_bytes(c, Lq, Hq, int(weights_out is not None))
-    ws = workspace
-    if ws is None:
-        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-    elif ws.device != dev:
+    if workspace is None:
+        need = L.seg_attn_decode_workspace_bytes(c, Lq, Hq, 0 if weights_out is None else 1)
+        workspace = Q.new_empty((max(need, 256),), dtype=torch.uint8)
+    elif workspace.get_device() != dev:
         raise ValueError("workspace must be on the cache's device")
-    _call(dev, L.seg_attn_decode, "seg_attn_decode", c, Lq, Hq, S, T, float(sm_scale if sm_scale is not None else d ** -0.5),
-          m.ctypes.data, Q.data_ptr(), qs, out.data_ptr(), os_, lse.data_ptr(), _p(weights), _p(weights_out), W, ws.data_ptr(),
-          ws.numel() * ws.element_size(), _on(dev, stream))
+    _call(dev, stream, L.seg_attn_decode, "seg_attn_decode", c, Lq, Hq, S, T, d ** -0.5 if sm_scale is None else sm_scale,
+          _mask_bytes(head_past_mask, Hkv), Q.data_ptr(), qs, out.data_ptr(), os_, lse.data_ptr(), _p(weights), _p(weights_out), W,
+          workspace.data_ptr(), workspace.nbytes)
     return out, lse
 
 
@@ -249,30 +263,23 @@ def kv_evict(weights, K_pages, V_pages, block_table, kv_len, dst_table, sink: in
     [B, pages], none of them a page the sequence has now) - the C entry point `seg_kv_evict`.  weights is fp32 [B, Hkv, W] as
     seg_attn_decode gathers it.  Returns (idx int32 [B, Hkv, budget] (the slots kept, then -1), kv_len, pos_shift, weights) of
     the evicted cache, whose block table is dst_table; kv_len_out may be kv_len and pos_shift_out pos_shift."""
-    c, B, Hkv, d, page, max_pages = _cache(K_pages, V_pages, block_table, kv_len, None, pos_shift, k_scale, v_scale)
-    dev = K_pages.device
-    if (dst_table.dim() != 2 or dst_table.dtype is not torch.int32 or dst_table.device != dev or dst_table.shape[0] != B or
-            dst_table.stride(1) != 1 or (B > 1 and dst_table.stride(0) < dst_table.shape[1])):
-        raise ValueError("dst_table must be an int32 tensor [B, pages] on %s with contiguous rows" % dev)
+    c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, None, pos_shift, k_scale, v_scale)
+    _, dst_pages, dst_stride = _pages(dst_table, B, "dst_table", dev)
     W = weights.shape[-1] if weights.dim() == 3 else 0
-    _flat(weights, torch.float32, (B, Hkv, W), "weights", dev)
+    _flat(weights, _F32, (B, Hkv, W), "weights", dev)
     budget = sink + recent + heavy
     if min(sink, recent, heavy) < 0 or budget < 1:
         raise SegAttnError(1, "seg_kv_evict")
-    idx = torch.empty((B, Hkv, budget), dtype=torch.int32, device=dev)
-    weights_out = torch.empty((B, Hkv, W), dtype=torch.float32, device=dev) if weights_out is None else \
-        _flat(weights_out, torch.float32, (B, Hkv, W), "weights_out", dev)
-    kv_len_out = torch.empty((B,), dtype=torch.int32, device=dev) if kv_len_out is None else \
-        _flat(kv_len_out, torch.int32, (B,), "kv_len_out", dev)
-    pos_shift_out = torch.empty((B,), dtype=torch.int32, device=dev) if pos_shift_out is None else \
-        _flat(pos_shift_out, torch.int32, (B,), "pos_shift_out", dev)
+    idx = kv_len.new_empty((B, Hkv, budget))
+    weights_out = torch.empty_like(weights) if weights_out is None else _flat(weights_out, _F32, (B, Hkv, W), "weights_out", dev)
+    kv_len_out = torch.empty_like(kv_len) if kv_len_out is None else _flat(kv_len_out, _I32, (B,), "kv_len_out", dev)
+    pos_shift_out = torch.empty_like(kv_len) if pos_shift_out is None else _flat(pos_shift_out, _I32, (B,), "pos_shift_out", dev)
     L = lib()
-    ws = workspace
-    if ws is None:
-        ws = torch.empty(max(L.seg_kv_evict_workspace_bytes(c), 256), dtype=torch.uint8, device=dev)
-    elif ws.device != dev:
+    if workspace is None:
+        workspace = kv_len.new_empty((max(L.seg_kv_evict_workspace_bytes(c), 256),), dtype=torch.uint8)
+    elif workspace.get_device() != dev:
         raise ValueError("workspace must be on the cache's device")
-    _call(dev, L.seg_kv_evict, "seg_kv_evict", c, weights.data_ptr(), W, sink, recent, heavy, dst_table.data_ptr(),
-          dst_table.shape[1], dst_table.stride(0) if B > 1 else dst_table.shape[1], idx.data_ptr(), kv_len_out.data_ptr(),
-          pos_shift_out.data_ptr(), weights_out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), _on(dev, stream))
+    _call(dev, stream, L.seg_kv_evict, "seg_kv_evict", c, weights.data_ptr(), W, sink, recent, heavy, dst_table.data_ptr(), dst_pages,
+          dst_stride, idx.data_ptr(), kv_len_out.data_ptr(), pos_shift_out.data_ptr(), weights_out.data_ptr(), workspace.data_ptr(),
+          workspace.nbytes)
     return idx, kv_len_out, pos_shift_out, weights_out
