@@ -355,7 +355,7 @@ typedef struct {
     int32_t table_stride;        /* elements between rows of the block table, >= max_pages */
     void *K, *V;                 /* DEVICE, 16-byte aligned */
     int64_t k_stride[3], v_stride[3]; /* elements, for (page, row, head); multiples of 16 bytes; the last dimension is contiguous */
-    const float *k_scale, *v_scale;   /* E4M3: DEVICE [Hkv], finite and > 0 (not checked); BF16: NULL */
+    const float *k_scale, *v_scale;   /* E4M3: DEVICE [Hkv], > 0, finite, with finite inverses (not checked); BF16: NULL */
     const int32_t* block_table;  /* DEVICE [B][max_pages]; entries past a sequence's last page are not read */
     const int32_t* kv_len;       /* DEVICE [B] */
     const int32_t* q_len;        /* DEVICE [B], new rows of each sequence, or NULL: Lq for all */
@@ -364,8 +364,8 @@ typedef struct {
 
 /* Writes the new rows K_new, V_new (bf16 [B][Lq][Hkv][d]) into the cache.  With `table` (see seg_rope_rotate; rot_dim, layout
  * and n_pos as there) the keys are rotated by their positions first, and so are the queries Q (bf16 [B][Lq][Hq][d], may
- * be NULL; Q_out may be Q) into Q_out; without a table keys are copied and Q must be NULL.  An e4m3 cache stores x / scale
- * rounded to nearest even and saturated at +-448.  Rows t >= q_len[b] are neither read nor written.  A new row
+ * be NULL; Q_out may be Q) into Q_out; without a table keys are copied and Q must be NULL.  An e4m3 cache stores x times
+ * the scale's inverse (both rounded to fp32), rounded to nearest even and saturated at +-448.  Rows t >= q_len[b] are neither read nor written.  A new row
  * whose slot or position is out of range is not written (status as above).  One kernel. */
 segattn_status seg_kv_append(const seg_kv_cache* c, int32_t Lq, const void* K_new, const int64_t kn_stride[3],
                              const void* V_new, const int64_t vn_stride[3], int32_t Hq, const void* Q,

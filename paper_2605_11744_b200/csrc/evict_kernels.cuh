@@ -16,7 +16,9 @@ struct EvictParams {
     int32_t *kv_len_out, *pos_shift_out;
     int W, sink, recent, heavy, budget;
     int dst_stride;
-    int d16;               // 16-byte pieces of a cache row
+    int d16, d16_log;      // 16-byte pieces of a cache row
+    int keys;              // keys a block of the selection has room for
+    FastDiv f_heads;       // division by Hkv
 };
 
 // Order of the weights as unsigned numbers: NaN lowest, -0 equal to +0.
@@ -26,133 +28,228 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-constexpr int kEvictThreads = 1024;
+// ---- thread-block clusters -----------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+// Every thread of every block of the cluster; writes to shared memory before it are seen after it.
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t load_from_block(const uint32_t* shared, uint32_t rank) {
+    uint32_t addr, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_u32(shared)), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
 
-// One block per (KV head, sequence).  The threshold (the heavy-th largest key between the sink and the recent rows) by
-// a radix selection of eight bits a pass, then the kept slots written out in ascending order.
+constexpr int kEvictThreads = 1024;
+constexpr int kEvictKeys = 40960;   // keys a block keeps in shared memory; more are read again from L2 in every pass
+constexpr int kEvictBins = 2048;
+constexpr int kEvictStatic = 3 * kEvictBins * 4;
+
+// One cluster of up to eight blocks per (KV head, sequence), each with a contiguous slice of the slots between the sink and
+// the recent rows.  The heavy-th largest key by a radix selection of 11, 11 and 10 bits, the blocks' histograms added up
+// through distributed shared memory; then the kept slots written in ascending order, each warp with a segment of its block's
+// slice, after one scan over the segments' counts.  Bound by the passes over the keys and the barriers between them, not by
+// the one read of the weights: a single block took 95 us for 128 heads of 26K slots, re-reading them and scanning 1024 at a
+// time.
 __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const EvictParams prm) {
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    extern __shared__ uint32_t evict_smem[];
+    uint32_t* hist = evict_smem;                    // [3][kEvictBins]
+    uint32_t* keys = evict_smem + 3 * kEvictBins;   // [prm.keys]
+    __shared__ uint32_t scan[32], seg_gt[32], seg_eq[32], found[2], totals[2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int CS = (int)cluster_size(), rank = (int)cluster_rank(), unit = blockIdx.x / CS;
+    const int h = unit % prm.c.Hkv, b = unit / prm.c.Hkv;
+    (void)h;
     const int n = seq_len(prm.c, b);
-    const long long unit = (long long)b * prm.c.Hkv + h;
-    const float* w = prm.weights + unit * prm.W;
-    int32_t* out = prm.idx + unit * prm.budget;
-    if (n <= prm.budget) {
-        for (int r = tid; r < prm.budget; r += kEvictThreads) out[r] = r < n ? r : -1;
-        return;
+    const float* w = prm.weights + (long long)unit * prm.W;
+    float* w_out = prm.weights_out + (long long)unit * prm.W;
+    int32_t* out = prm.idx + (long long)unit * prm.budget;
+    const int t0 = rank * kEvictThreads + tid, step = CS * kEvictThreads;
+    const bool all = n <= prm.budget;
+    // rows kept whatever they weigh, and the zeros behind the kept ones
+    for (int r = t0; r < prm.W; r += step) {
+        int src = -1;
+        if (all) src = r < n ? r : -1;
+        else if (r < prm.sink) src = r;
+        else if (r >= prm.sink + prm.heavy) src = r < prm.budget ? n - prm.budget + r : -1;
+        else continue;
+        if (r < prm.budget) out[r] = src;
+        w_out[r] = src >= 0 ? w[src] : 0.f;
     }
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t s_prefix, s_need;
-    const int m0 = prm.sink, m1 = n - prm.recent;  // the slots between: more than `heavy` of them, since n > budget
+    if (all || prm.heavy == 0) return;
+
+    const int m0 = prm.sink, len = n - prm.recent - m0;  // the slots between: more than `heavy` of them, since n > budget
+    const int slice = ((len + CS - 1) / CS + 31) & ~31, a = min(rank * slice, len), cnt = min(slice, len - a);
+    const float* mine = w + m0 + a;
+    const bool cached = cnt <= prm.keys;
+    auto key_at = [&](int i) { return cached ? keys[i] : weight_key(mine[i]); };
+    for (int i = tid; i < 3 * kEvictBins; i += kEvictThreads) hist[i] = 0;
+    __syncthreads();
     uint32_t prefix = 0, need = prm.heavy;
-    for (int shift = 24; need > 0 && shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += kEvictThreads) hist[i] = 0;
-        __syncthreads();
-        for (int j = m0 + tid; j < m1; j += kEvictThreads) {
-            const uint32_t k = weight_key(w[j]);
-            if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1u);
-        }
-        __syncthreads();
-        if (tid == 0) {
-            uint32_t left = need;
-            int bin = 255;
-            while (bin > 0 && hist[bin] < left) left -= hist[bin--];
-            s_prefix = (prefix << 8) | (uint32_t)bin;
-            s_need = left;
-        }
-        __syncthreads();
-        prefix = s_prefix;
-        need = s_need;
-    }
-    // keys above `prefix` are all kept, of those equal to it the first `need` (heavy == 0: none)
-    __shared__ uint32_t warp_sum[32];
-    uint32_t kept = 0, equal = 0;
-    for (int base = 0; base < n; base += kEvictThreads) {
-        const int j = base + tid;
-        bool keep = false, eq = false;
-        if (j < n) {
-            if (j < m0 || j >= m1) keep = true;
-            else if (prm.heavy > 0) {
-                const uint32_t k = weight_key(w[j]);
-                keep = k > prefix;
-                eq = k == prefix;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+        uint32_t* mh = hist + pass * kEvictBins;
+        for (int i0 = 0; i0 < cnt; i0 += kEvictThreads) {
+            const int i = i0 + tid;
+            bool in = i < cnt;
+            uint32_t k = 0;
+            if (in) {
+                if (pass == 0) {
+                    k = weight_key(mine[i]);
+                    if (cached) keys[i] = k;
+                } else {
+                    k = key_at(i);
+                }
+                in = pass == 0 || (k >> (shift + bits)) == prefix;
+            }
+            const uint32_t bin = in ? (k >> shift) & ((1u << bits) - 1) : 0xffffffffu;
+            // a warp whose keys all fall into one bin (zeros that nothing ever looked at) adds them at once
+            int same;
+            __match_all_sync(0xffffffffu, bin, &same);
+            if (same) {
+                if (lane == 0 && in) atomicAdd(mh + bin, 32u);
+            } else if (in) {
+                atomicAdd(mh + bin, 1u);
             }
         }
-        // rank of the equal ones first, then of all kept ones
-        const int lane = tid & 31, wid = tid >> 5;
-        const uint32_t beq = __ballot_sync(0xffffffffu, eq);
-        if (lane == 0) warp_sum[wid] = __popc(beq);
         __syncthreads();
-        uint32_t before = equal, total = 0;
-        for (int k = 0; k < 32; ++k) {
-            if (k < wid) before += warp_sum[k];
-            total += warp_sum[k];
+        if (CS > 1) cluster_sync();
+        // bins from the top down: thread t has bins 2047 - 2 t and 2046 - 2 t
+        uint32_t c[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t* at = mh + kEvictBins - 1 - 2 * tid - k;
+            c[k] = CS == 1 ? *at : 0u;
+            if (CS > 1)
+                for (int r = 0; r < CS; ++r) c[k] += load_from_block(at, r);
         }
-        equal += total;
-        if (eq) keep = before + __popc(beq & ((1u << lane) - 1)) < need;
+        uint32_t before = c[0] + c[1];
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, before, x);
+            if (lane >= x) before += y;
+        }
+        if (lane == 31) scan[warp] = before;
+        before -= c[0] + c[1];
         __syncthreads();
+        for (int k = 0; k < warp; ++k) before += scan[k];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (need > before && need <= before + c[k]) {
+                found[0] = kEvictBins - 1 - 2 * tid - k;
+                found[1] = need - before;
+            }
+            before += c[k];
+        }
+        __syncthreads();
+        prefix = (prefix << bits) | found[0];
+        need = found[1];
+    }
+    // keys above `prefix` are all kept, of those equal to it the first `need`
+    const int seg = ((cnt + 31) / 32 + 31) & ~31, s0 = min(warp * seg, cnt), s1 = min(s0 + seg, cnt);
+    uint32_t gt = 0, eq = 0;
+    for (int i = s0 + lane; i - lane < s1; i += 32) {
+        const uint32_t k = i < s1 ? key_at(i) : 0u;
+        gt += __popc(__ballot_sync(0xffffffffu, i < s1 && k > prefix));
+        eq += __popc(__ballot_sync(0xffffffffu, i < s1 && k == prefix));
+    }
+    if (lane == 0) {
+        seg_gt[warp] = gt;
+        seg_eq[warp] = eq;
+    }
+    __syncthreads();
+    uint32_t gt_before = 0, eq_before = 0, gt_all = 0, eq_all = 0;
+    for (int k = 0; k < 32; ++k) {
+        if (k < warp) {
+            gt_before += seg_gt[k];
+            eq_before += seg_eq[k];
+        }
+        gt_all += seg_gt[k];
+        eq_all += seg_eq[k];
+    }
+    if (CS > 1) {
+        if (tid == 0) {
+            totals[0] = gt_all;
+            totals[1] = eq_all;
+        }
+        cluster_sync();
+        for (int r = 0; r < rank; ++r) {
+            gt_before += load_from_block(totals, r);
+            eq_before += load_from_block(totals + 1, r);
+        }
+    }
+    uint32_t at = prm.sink + gt_before + min(eq_before, need);
+    for (int i = s0 + lane; i - lane < s1; i += 32) {
+        const uint32_t k = i < s1 ? key_at(i) : 0u;
+        const bool equal = i < s1 && k == prefix;
+        const uint32_t be = __ballot_sync(0xffffffffu, equal), below = (1u << lane) - 1;
+        const bool keep = (i < s1 && k > prefix) || (equal && eq_before + __popc(be & below) < need);
         const uint32_t bk = __ballot_sync(0xffffffffu, keep);
-        if (lane == 0) warp_sum[wid] = __popc(bk);
-        __syncthreads();
-        before = kept;
-        total = 0;
-        for (int k = 0; k < 32; ++k) {
-            if (k < wid) before += warp_sum[k];
-            total += warp_sum[k];
+        if (keep) {
+            const uint32_t r = at + __popc(bk & below);
+            out[r] = m0 + a + i;
+            w_out[r] = mine[i];
         }
-        kept += total;
-        if (keep) out[before + __popc(bk & ((1u << lane) - 1))] = j;
-        __syncthreads();
+        at += __popc(bk);
+        eq_before += __popc(be);
     }
+    if (CS > 1) cluster_sync();  // no block leaves while another may still read its shared memory
 }
 
-// Row r of the compacted cache from slot idx[b][h][r]: one thread per 16 bytes (K and V both).
+// Row r of the compacted cache from slot idx[b][h][r]: a thread moves 16 bytes of K and of V for four rows, whose reads are
+// all in flight together (205 -> 180 us for 16 x 8 heads of 8036 rows against one row a thread; 1.05 GB).  Runs after the selection's end; the new
+// lengths and shifts are written here and not there because kv_len_out may be kv_len, which the selection's blocks read.
+constexpr int kMoveRows = 4;
 __global__ void __launch_bounds__(256) evict_move_kernel(const EvictParams prm) {
-    const long long n = (long long)prm.c.B * prm.budget * prm.c.Hkv * prm.d16;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    const int e = (int)(i % prm.d16);
-    const int h = (int)((i / prm.d16) % prm.c.Hkv);
-    const int r = (int)((i / ((long long)prm.d16 * prm.c.Hkv)) % prm.budget);
-    const int b = (int)(i / ((long long)prm.d16 * prm.c.Hkv * prm.budget));
-    const int src = prm.idx[((long long)b * prm.c.Hkv + h) * prm.budget + r];
-    if (src < 0) return;
-    int row, to_row;
-    const int page = page_of(prm.c, b, src, &row);
-    const int entry = (int)fdiv((uint32_t)r, prm.c.f_page);
-    to_row = r - entry * (int)prm.c.f_page.d;
-    const int to = prm.dst_table[(long long)b * prm.dst_stride + entry];
-    if ((unsigned)to >= (unsigned)prm.c.n_pages) {
-        if (e == 0) refuse_input(36);
-        return;
-    }
-    uint4 k = make_uint4(0, 0, 0, 0), v = k;
-    if (page >= 0) {
-        k = *reinterpret_cast<const uint4*>(prm.c.K + page * prm.c.k_stride[0] + row * prm.c.k_stride[1] + h * prm.c.k_stride[2] + 16 * e);
-        v = *reinterpret_cast<const uint4*>(prm.c.V + page * prm.c.v_stride[0] + row * prm.c.v_stride[1] + h * prm.c.v_stride[2] + 16 * e);
-    }
-    *reinterpret_cast<uint4*>(prm.c.K + to * prm.c.k_stride[0] + to_row * prm.c.k_stride[1] + h * prm.c.k_stride[2] + 16 * e) = k;
-    *reinterpret_cast<uint4*>(prm.c.V + to * prm.c.v_stride[0] + to_row * prm.c.v_stride[1] + h * prm.c.v_stride[2] + 16 * e) = v;
-}
-
-// weights_out = the kept slots' weights, then zeros; and, by the first threads, the new lengths and shifts (here and
-// not in the selection: kv_len_out may be kv_len, which the selection's blocks read).
-__global__ void __launch_bounds__(256) evict_finish_kernel(const EvictParams prm) {
-    const long long units = (long long)prm.c.B * prm.c.Hkv;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i < prm.c.B) {
-        const int b = (int)i, n = seq_len(prm.c, b), m = min(n, prm.budget), s = shift_of(prm.c, b);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int b = blockIdx.y;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        const int n = seq_len(prm.c, b), m = min(n, prm.budget), s = shift_of(prm.c, b);
         prm.kv_len_out[b] = m;
         prm.pos_shift_out[b] = s + n - m;
     }
-    if (i >= units * prm.W) return;
-    const int j = (int)(i % prm.W);
-    const long long unit = i / prm.W;
-    float x = 0.f;
-    if (j < prm.budget) {
-        const int src = prm.idx[unit * prm.budget + j];
-        if (src >= 0) x = prm.weights[unit * prm.W + src];
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x, e = i & (prm.d16 - 1), u = i >> prm.d16_log;
+    const uint32_t r4 = fdiv(u, prm.f_heads);
+    const int h = (int)(u - r4 * prm.c.Hkv), r0 = (int)r4 * kMoveRows;
+    if (r0 >= prm.budget) return;
+    int src[kMoveRows];
+    const int32_t* idx = prm.idx + ((long long)b * prm.c.Hkv + h) * prm.budget;
+#pragma unroll
+    for (int k = 0; k < kMoveRows; ++k) src[k] = r0 + k < prm.budget ? idx[r0 + k] : -1;
+    uint4 kx[kMoveRows], vx[kMoveRows];
+#pragma unroll
+    for (int k = 0; k < kMoveRows; ++k) {
+        int row, page = -1;
+        if (src[k] >= 0) page = page_of(prm.c, b, src[k], &row);
+        kx[k] = vx[k] = make_uint4(0, 0, 0, 0);
+        if (page >= 0) {
+            kx[k] = *reinterpret_cast<const uint4*>(prm.c.K + page * prm.c.k_stride[0] + row * prm.c.k_stride[1] + h * prm.c.k_stride[2] + 16 * e);
+            vx[k] = *reinterpret_cast<const uint4*>(prm.c.V + page * prm.c.v_stride[0] + row * prm.c.v_stride[1] + h * prm.c.v_stride[2] + 16 * e);
+        }
     }
-    prm.weights_out[i] = x;
+#pragma unroll
+    for (int k = 0; k < kMoveRows; ++k) {
+        if (src[k] < 0) continue;
+        const int entry = (int)fdiv((uint32_t)(r0 + k), prm.c.f_page), row = r0 + k - entry * (int)prm.c.f_page.d;
+        const int to = prm.dst_table[(long long)b * prm.dst_stride + entry];
+        if ((unsigned)to >= (unsigned)prm.c.n_pages) {
+            if (e == 0) refuse_input(36);
+            continue;
+        }
+        *reinterpret_cast<uint4*>(prm.c.K + to * prm.c.k_stride[0] + row * prm.c.k_stride[1] + h * prm.c.k_stride[2] + 16 * e) = kx[k];
+        *reinterpret_cast<uint4*>(prm.c.V + to * prm.c.v_stride[0] + row * prm.c.v_stride[1] + h * prm.c.v_stride[2] + 16 * e) = vx[k];
+    }
 }
 
 }  // namespace segattn

@@ -294,7 +294,7 @@ def test_append_matches_the_definition(case, fp8):
                 k = ref.rotate(k, tab, layout)
             k, v = torch.from_numpy(k), torch.from_numpy(v)
             if fp8:
-                k, v = (k / c.k_scale[:, None]).clamp(-448, 448), (v / c.v_scale[:, None]).clamp(-448, 448)
+                k, v = (k * (1 / c.k_scale)[:, None]).clamp(-448, 448), (v * (1 / c.v_scale)[:, None]).clamp(-448, 448)
             at = c.table[b, slot // page].long(), slot % page
             want_k[at], want_v[at] = bits(k.to(kind)).cuda(), bits(v.to(kind)).cuda()
             if Hq:
@@ -309,6 +309,26 @@ def test_append_matches_the_definition(case, fp8):
         assert torch.equal(nan(bits(c.K)), nan(want_k)) and torch.equal(nan(bits(c.V)), nan(want_v))
     else:
         assert torch.equal(bits(c.K), want_k) and torch.equal(bits(c.V), want_v)
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.0371, 3.0, 1.0e-3, 2.0 ** -127, 1.0e-38, 2.0e38])
+def test_eight_bit_values_are_rounded_to_nearest_even(scale):
+    # values on and around the borders between two e4m3 values, times the scale's inverse in fp32
+    grid = torch.arange(0, 0x7f, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
+    border = (grid[1:] + grid[:-1]) / 2 * scale
+    near = torch.cat([border, grid * scale, border * (1 + 2.0 ** -9), border * (1 - 2.0 ** -9), torch.tensor([500.0 * scale, 1e30, 3e38, 0.0])])
+    x = near.to(torch.bfloat16)
+    x = torch.cat([x, -x])
+    x = torch.cat([x, x.new_zeros(-len(x) % 128)]).reshape(1, -1, 1, 128).cuda()
+    n = x.shape[1]
+    pages = torch.zeros(2, 16, 1, 128, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    assert n <= 16
+    s = torch.tensor([scale], device="cuda")
+    sa.kv_append(x, x, pages[:1], pages[1:], torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda"),
+                 k_scale=s, v_scale=s)
+    sa.poll_status()
+    want = (x[0].cpu().float() * (1 / torch.tensor(scale))).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+    assert torch.equal(pages[0, :n].view(torch.uint8).cpu(), want) and torch.equal(pages[1, :n].view(torch.uint8).cpu(), want)
 
 
 def test_append_in_place_and_bad_numbers():
