@@ -52,6 +52,7 @@ __device__ __forceinline__ uint32_t load_from_block(const uint32_t* shared, uint
 
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictKeys = 40960;   // keys a block keeps in shared memory; more are read again from L2 in every pass
+constexpr int kEvictAhead = 8;      // weights a thread has in flight
 constexpr int kEvictBins = 2048;
 constexpr int kEvictStatic = 3 * kEvictBins * 4;
 
@@ -77,16 +78,21 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
     const int t0 = rank * kEvictThreads + tid, step = CS * kEvictThreads;
     const bool all = n <= prm.budget;
     // rows kept whatever they weigh, and the zeros behind the kept ones
-    for (int r = t0; r < prm.W; r += step) {
-        int src = -1;
-        if (all) src = r < n ? r : -1;
-        else if (r < prm.sink) src = r;
-        else if (r >= prm.sink + prm.heavy) src = r < prm.budget ? n - prm.budget + r : -1;
-        else continue;
-        if (r < prm.budget) out[r] = src;
-        w_out[r] = src >= 0 ? w[src] : 0.f;
+    auto keep_the_rest = [&]() {
+        const int kept = all ? n : prm.budget, front = all ? n : prm.sink, gap = all ? 0 : prm.heavy;
+        for (int i = t0; i < kept - gap; i += step) {
+            const int r = i < front ? i : i + gap, src = i < front ? i : n - kept + r;
+            out[r] = src;
+            w_out[r] = w[src];
+        }
+        for (int r = kept + t0; r < prm.budget; r += step) out[r] = -1;
+#pragma unroll 4
+        for (int r = kept + t0; r < prm.W; r += step) w_out[r] = 0.f;
+    };
+    if (all || prm.heavy == 0) {
+        keep_the_rest();
+        return;
     }
-    if (all || prm.heavy == 0) return;
 
     const int m0 = prm.sink, len = n - prm.recent - m0;  // the slots between: more than `heavy` of them, since n > budget
     const int slice = ((len + CS - 1) / CS + 31) & ~31, a = min(rank * slice, len), cnt = min(slice, len - a);
@@ -100,27 +106,36 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
         uint32_t* mh = hist + pass * kEvictBins;
-        for (int i0 = 0; i0 < cnt; i0 += kEvictThreads) {
-            const int i = i0 + tid;
-            bool in = i < cnt;
-            uint32_t k = 0;
-            if (in) {
-                if (pass == 0) {
-                    k = weight_key(mine[i]);
-                    if (cached) keys[i] = k;
-                } else {
-                    k = key_at(i);
-                }
-                in = pass == 0 || (k >> (shift + bits)) == prefix;
-            }
+        auto count = [&](uint32_t k, bool in) {
             const uint32_t bin = in ? (k >> shift) & ((1u << bits) - 1) : 0xffffffffu;
             // a warp whose keys all fall into one bin (zeros that nothing ever looked at) adds them at once
-            int same;
-            __match_all_sync(0xffffffffu, bin, &same);
-            if (same) {
+            if (__all_sync(0xffffffffu, bin == __shfl_sync(0xffffffffu, bin, 0))) {
                 if (lane == 0 && in) atomicAdd(mh + bin, 32u);
             } else if (in) {
                 atomicAdd(mh + bin, 1u);
+            }
+        };
+        if (pass == 0 || !cached) {
+            for (int i0 = 0; i0 < cnt; i0 += kEvictAhead * kEvictThreads) {
+                float x[kEvictAhead];
+#pragma unroll
+                for (int y = 0; y < kEvictAhead; ++y) x[y] = i0 + y * kEvictThreads + tid < cnt ? mine[i0 + y * kEvictThreads + tid] : 0.f;
+#pragma unroll
+                for (int y = 0; y < kEvictAhead; ++y) {
+                    const int i = i0 + y * kEvictThreads + tid;
+                    if (i - tid >= cnt) break;
+                    const uint32_t k = weight_key(x[y]);
+                    if (cached && i < cnt) keys[i] = k;
+                    count(k, i < cnt && (pass == 0 || (k >> (shift + bits)) == prefix));
+                }
+            }
+        } else {
+            // few keys share the leading bits found so far: most warps only look
+#pragma unroll 4
+            for (int i = tid; i - tid < cnt; i += kEvictThreads) {
+                const uint32_t k = i < cnt ? keys[i] : 0u;
+                const bool in = i < cnt && (k >> (shift + bits)) == prefix;
+                if (__any_sync(0xffffffffu, in)) count(k, in);
             }
         }
         __syncthreads();
@@ -131,8 +146,13 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
         for (int k = 0; k < 2; ++k) {
             const uint32_t* at = mh + kEvictBins - 1 - 2 * tid - k;
             c[k] = CS == 1 ? *at : 0u;
-            if (CS > 1)
-                for (int r = 0; r < CS; ++r) c[k] += load_from_block(at, r);
+            if (CS > 1) {
+                uint32_t v[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] = r < CS ? load_from_block(at, r) : 0u;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) c[k] += v[r];
+            }
         }
         uint32_t before = c[0] + c[1];
 #pragma unroll
@@ -159,11 +179,14 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
     // keys above `prefix` are all kept, of those equal to it the first `need`
     const int seg = ((cnt + 31) / 32 + 31) & ~31, s0 = min(warp * seg, cnt), s1 = min(s0 + seg, cnt);
     uint32_t gt = 0, eq = 0;
-    for (int i = s0 + lane; i - lane < s1; i += 32) {
-        const uint32_t k = i < s1 ? key_at(i) : 0u;
-        gt += __popc(__ballot_sync(0xffffffffu, i < s1 && k > prefix));
-        eq += __popc(__ballot_sync(0xffffffffu, i < s1 && k == prefix));
+#pragma unroll 4
+    for (int i = s0 + lane; i < s1; i += 32) {
+        const uint32_t k = key_at(i);
+        gt += k > prefix;
+        eq += k == prefix;
     }
+    gt = __reduce_add_sync(0xffffffffu, gt);
+    eq = __reduce_add_sync(0xffffffffu, eq);
     if (lane == 0) {
         seg_gt[warp] = gt;
         seg_eq[warp] = eq;
@@ -190,11 +213,16 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
         }
     }
     uint32_t at = prm.sink + gt_before + min(eq_before, need);
+#pragma unroll 2
     for (int i = s0 + lane; i - lane < s1; i += 32) {
         const uint32_t k = i < s1 ? key_at(i) : 0u;
         const bool equal = i < s1 && k == prefix;
+        bool keep = i < s1 && k > prefix;
         const uint32_t be = __ballot_sync(0xffffffffu, equal), below = (1u << lane) - 1;
-        const bool keep = (i < s1 && k > prefix) || (equal && eq_before + __popc(be & below) < need);
+        if (be) {
+            keep = keep || (equal && eq_before + __popc(be & below) < need);
+            eq_before += __popc(be);
+        }
         const uint32_t bk = __ballot_sync(0xffffffffu, keep);
         if (keep) {
             const uint32_t r = at + __popc(bk & below);
@@ -202,8 +230,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
             w_out[r] = mine[i];
         }
         at += __popc(bk);
-        eq_before += __popc(be);
     }
+    keep_the_rest();
     if (CS > 1) cluster_sync();  // no block leaves while another may still read its shared memory
 }
 
