@@ -175,7 +175,7 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
         const int y = __shfl_up_sync(0xffffffffu, before, x);
         if (lane >= x) before += y;
     }
-    if (lane == 31) warp_sum[warp] = before;
+    if (lane == 31 && warp < kDecThreads / 32) warp_sum[warp] = before;  // the block's further warps have no sequence
     if (tid == 0) out->begin = out->end = 0;
     __syncthreads();
     int total = 0;

@@ -14,6 +14,7 @@
 
 #include "bwd_kernels.cuh"
 #include "decode_kernels.cuh"
+#include "decode_rows_kernels.cuh"
 #include "evict_kernels.cuh"
 #include "fwd_kernel.cuh"
 #include "mask.cuh"

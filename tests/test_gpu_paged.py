@@ -56,6 +56,9 @@ DECODE = [
     ([5000, 1200], 1, None, 16, 2, 128, 64, 1 << 30, 0, [1, 0]),               # plainly causal
     ([9000, 17], 2, None, 64, 8, 128, 256, 4096, 1024, [1] * 8),
     ([4097], 1, None, 8, 1, 64, 128, 2048, 512, [1]),
+    ([400, 90], 70, [70, 33], 4, 1, 128, 64, 128, 32, [0]),                    # 280 rows to the KV head
+    ([300, 41], 40, [40, 0], 8, 2, 64, 16, 100, 20, [1, 2]),
+    ([1500, 700, 130], 16, [16, 9, 16], 32, 8, 128, 64, 256, 64, [0, 1, 0, 1, 2, 1, 0, 1]),
 ]
 
 
@@ -85,37 +88,46 @@ def test_decode_gathers_attention_weights(case, fp8):
         assert torch.equal(acc[b, :, :m], w3[b, :, :m]) and torch.equal(acc[b, :, m:], kept[b, :, m:])
 
 
-def test_rows_nobody_sees_do_not_matter():
+@pytest.mark.parametrize("Lq,Hq,d,fp8", [(6, 4, 128, False), (6, 2, 64, False), (6, 12, 128, False), (40, 4, 128, False), (70, 4, 64, False),
+                                         (6, 4, 128, True), (6, 12, 64, True), (20, 4, 128, True)])
+def test_rows_nobody_sees_do_not_matter(Lq, Hq, d, fp8):
     # new row t must not feel the keys and values of the rows after it, whatever they hold; a local head not those before it
-    lens, Lq, Hq, Hkv, d, page, S, T = [70, 37], 6, 4, 2, 128, 16, 32, 8
+    lens, Hkv, page, S, T = [Lq + 64, Lq + 31], 2, 16, 32, 8
     mask = [0, 1]
-    c = ref.Cache(lens, Hkv, d, page, seed=5)
+    c = ref.Cache(lens, Hkv, d, page, fp8=fp8, seed=5)
     Q = rand_q(2, Lq, Hq, d)
     clean, lse, _ = run_decode(c, Q, S, T, mask)
-    last = 4    # rows from this one on are spoiled
-    for fill in (math.inf, -math.inf, math.nan, 3.0e38):
+    last = Lq - 2    # rows from this one on are spoiled
+    bits = lambda x: x.view(torch.uint8) if fp8 else x
+    for fill in ((0x7f, 0xff) if fp8 else (math.inf, -math.inf, math.nan, 3.0e38)):
         K, V = c.K.clone(), c.V.clone()
         for b, n in enumerate(lens):
             for j in range(n - Lq + last, n):
-                K[c.table[b, j // page].long(), j % page] = fill
-                V[c.table[b, j // page].long(), j % page] = fill
+                bits(K)[c.table[b, j // page].long(), j % page] = fill
+                bits(V)[c.table[b, j // page].long(), j % page] = fill
             low = min(ref.lowest_visible(n - Lq + t, S, T, 0, 0) for t in range(Lq))
             for j in range(0, low):
-                K[c.table[b, j // page].long(), j % page, 0] = fill
-                V[c.table[b, j // page].long(), j % page, 0] = fill
+                bits(K)[c.table[b, j // page].long(), j % page, 0] = fill
+                bits(V)[c.table[b, j // page].long(), j % page, 0] = fill
         w = torch.zeros(2, Hkv, c.max_pages * page, device="cuda")
-        O, l2 = sa.seg_attn_decode(Q, K, V, S=S, T=T, head_past_mask=mask, weights_out=w, **c.dev)
+        O, l2 = sa.seg_attn_decode(Q, K, V, S=S, T=T, head_past_mask=mask, weights_out=w, **c.dev, **c.scales)
         sa.poll_status()
         assert torch.equal(O[:, :last], clean[:, :last]) and torch.equal(l2[:, :, :last], lse[:, :, :last])
         assert not torch.isfinite(O[:, last:].float()).all()      # and those that see them do
+        # only V is spoiled: the weights are what they were, and the rows that see them have what the sum has
+        O, l2 = sa.seg_attn_decode(Q, c.K, V, S=S, T=T, head_past_mask=mask, **c.dev, **c.scales)
+        assert torch.equal(l2, lse) and torch.equal(O[:, :last], clean[:, :last])
+        if fp8 or not abs(fill) < math.inf:
+            assert not torch.isfinite(O[:, last:].float()).any()
 
 
-def test_rows_across_a_segment_border_do_not_feel_what_the_border_hides():
+@pytest.mark.parametrize("Hq,d", [(2, 64), (20, 128), (40, 64), (44, 128)])
+def test_rows_across_a_segment_border_do_not_feel_what_the_border_hides(Hq, d):
     # the first row of a segment sees the tail in front of it, the row before sees further back: infinities there reach one
     # of them only
     S, T, page = 32, 4, 16
-    c = ref.Cache([66], 1, 64, page, seed=8)      # rows 63 (old segment), 64 and 65 (new one)
-    Q = rand_q(1, 3, 2, 64)
+    c = ref.Cache([66], 1, d, page, seed=8)      # rows 63 (old segment), 64 and 65 (new one)
+    Q = rand_q(1, 3, Hq, d)
     clean, lse, _ = run_decode(c, Q, S, T, [0])
     K, V = c.K.clone(), c.V.clone()
     for j in (40, 59):                            # visible from 63, not from 64 on (which see 60..)
