@@ -57,10 +57,10 @@ __device__ __forceinline__ uint32_t load_16_slots(const PagedView& c, int b, int
     return loaded;
 }
 
-// Row r of a sequence's KV head (r = new row * g + query head of the group) into row r - r_base of an operand tile of 128
-// rows, rows of one warp; rows that are not there become zeros.
+// Row r of a sequence's KV head (r = new row * g + query head of the group) into row r - r_base of an operand tile, `count` rows
+// from `first` on by one warp; rows that are not there become zeros.
 template <int D>
-__device__ __forceinline__ void load_query_rows(const DecodeParams& p, int b, int h, int rows, int r_base, int first, int count, uint32_t tile) {
+__device__ __forceinline__ void load_query_rows(const DecodeParams& p, int b, int h, int rows, int r_base, int first, int count, uint32_t tile, int panel_bytes) {
     constexpr int C = D / 8, RPI = 32 / C;
     const int lane = threadIdx.x & 31, r0 = lane / C, ch = lane % C;
     for (int i = first; i < first + count; i += RPI) {
@@ -68,44 +68,58 @@ __device__ __forceinline__ void load_query_rows(const DecodeParams& p, int b, in
         const bool real = r < rows;
         const int t = (int)fdiv((uint32_t)(real ? r : 0), p.f_g), qh = h * p.g + (real ? r - t * p.g : 0);
         const __nv_bfloat16* q = p.Q + b * p.q_stride[0] + t * p.q_stride[1] + qh * p.q_stride[2] + ch * 8;
-        cp_async16_if(tile + panel_at(i + r0, ch, 16384), q, real);
+        cp_async16_if(tile + panel_at(i + r0, ch, panel_bytes), q, real);
     }
 }
 
+// One arrival on `bar` when all copies that this thread has issued so far have landed.
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+
 // ---- attention -----------------------------------------------------------------------------------------------------
-// One block to an SM walks its range of 64-slot tiles of the same list that decode_kernel uses (items of up to 128 rows).
-//   warps 0, 1   loaders: 32 slots of K and V each with cp.async into a ring of four stages, queries into one of two buffers
-//   warp 2       issuer: S(i) = Q K^T (128 x 64), then O += P(i-1) V (128 x D)
-//   warps 4-7    softmax of the even tiles, warps 8-11 of the odd ones: thread = row = TMEM lane; scores out of the group's S
-//                buffer, weights (bf16) into its P buffer, an O and a base of its own; the two are joined at an item's end
+// One block to an SM walks its range of 64-slot tiles of the same list that decode_kernel uses (items of up to QR rows).
+//   loaders      16 or 32 slots of K and V a warp with cp.async into a ring of stages, queries into one of two buffers
+//   issuer       S(i) = Q K^T (128 x 64), then O += P(i-1) V (128 x D)
+//   softmax      one group of warps for the even tiles, one for the odd ones: thread = row = TMEM lane; scores out of the
+//                group's S buffer, weights (bf16) into its P buffer, an O and a base of its own; joined at an item's end
 // TMEM (512 columns): S at 0 and 64, P at 128 and 160, O at 192 and 320.  A row's base moves as in decode_kernel, past a
-// slack only: most tiles leave O alone.  One group alone took 3 us a tile, twice what HBM needs; every wait is bounded.
-template <int D>
+// slack only: most tiles leave O alone.  The rows of an MMA do not mix, so that with items of QR = 64 rows the upper half of
+// the lanes computes on whatever is there and nobody reads it; its two warps of each softmax group are not needed (two of
+// them load), and the queries' smaller buffers leave room for six stages instead of four.  What bounds the kernel is the
+// way round of a stage (free, load, S, softmax, O: some 6000 cycles, of which the load's latency is 2400) over the number of
+// stages, not HBM: with four stages 1500 cycles a tile.  Every wait is bounded.
+template <int D, int QR>
 struct RowsShape {
-    static constexpr int kStages = 4, kLag = 2;
-    static constexpr int kKv = (D / 64) * 8192;    // a K or V tile: 64 rows, panels of 64 elements
-    static constexpr int kQ = (D / 64) * 16384;
+    static constexpr int kStages = D == 64 ? 8 : QR == 64 ? 6 : 4;
+    static constexpr int kKv = (D / 64) * 8192;       // a K or V tile: 64 rows, panels of 64 elements
+    static constexpr int kQPanel = QR * 128;
+    static constexpr int kQ = (D / 64) * kQPanel;
     static constexpr int kDynamic = kStages * 2 * kKv + 2 * kQ + 1024;
-    static constexpr int MB = 128, kTileLog = 6;
+    static constexpr int MB = QR, kTileLog = 6;
+    static_assert(QR == 128 || 128 * 128 + (D / 64 - 1) * kQPanel <= kQ + kStages * 2 * kKv, "an MMA's 128 rows of the second query buffer end in the ring");
+    static constexpr int kThreads = QR == 64 ? 320 : 384;
+    static constexpr int kLoaders = QR == 64 ? 4 : 2; // warps 0, 1 (, 6, 7); the issuer is warp 2, the groups start at warps 4 and 8
 };
-constexpr int kRowsThreads = 384;
 constexpr int kRowsBlocks = 160;  // blocks a launch has at most
 
-template <int D>
-__global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __grid_constant__ DecodeParams p) {
-    using Sh = RowsShape<D>;
-    constexpr int ST = Sh::kStages, LAG = Sh::kLag, MB = Sh::MB, C = D / 8;
-    enum { kFull = 0, kEmpty = ST, kSFull = 2 * ST, kPFull = 2 * ST + 2, kPvDone = 2 * ST + 4, kQFull = 2 * ST + 6, kQEmpty = 2 * ST + 8, kScan = 2 * ST + 10, kBars = 2 * ST + 12 };
+template <int D, int QR>
+__global__ void __launch_bounds__(RowsShape<D, QR>::kThreads, 1) decode_rows_kernel(const __grid_constant__ DecodeParams p) {
+    using Sh = RowsShape<D, QR>;
+    constexpr int ST = Sh::kStages, MB = Sh::MB, C = D / 8, NL = Sh::kLoaders, SW = 4 / NL * 16;  // slots of a loader warp
+    enum { kFull = 0, kEmpty = ST, kSFull = 2 * ST, kPFull = 2 * ST + 2, kPvDone = 2 * ST + 4, kQFull = 2 * ST + 6, kQEmpty = 2 * ST + 8, kScan = 2 * ST + 10, kSRead = 2 * ST + 12, kBars = 2 * ST + 14 };
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ BlockRange range;
     __shared__ int warp_sum[4];
     __shared__ uint32_t there[ST][4], tmem_slot;
-    __shared__ float2 end_ml[2][128];  // an item's end: base and sum of each row in the two groups
+    __shared__ float2 end_ml[2][QR];  // an item's end: base and sum of each row in the two groups
     const uint32_t base_s = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    auto sK = [&](int s) { return base_s + s * 2 * Sh::kKv; };
-    auto sV = [&](int s) { return base_s + s * 2 * Sh::kKv + Sh::kKv; };
-    auto sQ = [&](int s) { return base_s + ST * 2 * Sh::kKv + s * Sh::kQ; };
+    // The queries come first: an MMA reads 128 rows of them, with QR = 64 up to 16 KB past the second buffer's end, which has
+    // to stay within the block's shared memory (the ring's 96 KB and more).
+    auto sQ = [&](int s) { return base_s + s * Sh::kQ; };
+    auto sK = [&](int s) { return base_s + 2 * Sh::kQ + s * 2 * Sh::kKv; };
+    auto sV = [&](int s) { return sK(s) + Sh::kKv; };
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     next_kernel_may_start();
@@ -113,7 +127,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
     if (range.begin >= range.end) return;
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i)
-            mbar_init(bar(i), i < kEmpty || (i >= kQFull && i < kQEmpty) ? 64 : (i >= kPFull && i < kPvDone) || i >= kScan ? 4 : 1);
+            mbar_init(bar(i), i < kEmpty ? NL * 33 : i >= kQFull && i < kQEmpty ? NL * 32 : (i >= kPFull && i < kPvDone) || i >= kScan ? QR / 32 : 1);
         fence_mbar_init();
     }
     if (warp == 2) {
@@ -132,17 +146,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
     cur.read_sequence(p);
     cur.enter(p, range.tile);
 
-    if (warp < 2) {
+    const int loader = warp < 2 ? warp : NL == 4 && (warp == 6 || warp == 7) ? warp - 4 : -1;
+    if (loader >= 0) {
         // ---------------- loaders ----------------
+        // A stage's barrier counts every loader thread, when its copies have landed, and the warps' notes of what they loaded.
         bool ok = true;
-        uint32_t firsts = 0;  // bit k: the tile loaded k + 1 iterations ago was its piece's first
-        int signalled = 0, piece = 0, pieces_signalled = 0;
-        auto signal = [&](int i, bool first, int pc) {  // tile i (and the queries of piece pc) has landed
-            fence_proxy_async_smem();
-            mbar_arrive(bar(kFull + i % ST));
-            if (first) mbar_arrive(bar(kQFull + (pc & 1)));
-        };
-        for (int i = 0; i < n_tiles && ok; ++i) {
+        int piece = 0;
+        for (int i = 0; i < n_tiles; ++i) {
             const bool first = i == 0 || cur.tile == cur.end;
             if (i > 0 && first) {
                 cur.next_item(p);
@@ -150,93 +160,104 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
             }
             const int head = p.head_order[cur.first_head];
             if (first) {
-                const uint32_t par = ((uint32_t)(piece >> 1) & 1) ^ 1;
-                if (!__all_sync(0xffffffffu, mbar_try_wait(bar(kQEmpty + (piece & 1)), par))) {
-                    // the scores that free this buffer may wait for tiles that have been loaded but not yet signalled
-                    cp_async_wait<0>();
-                    for (; signalled < i; ++signalled) {
-                        const bool f = (firsts >> (i - 1 - signalled)) & 1;
-                        signal(signalled, f, pieces_signalled);
-                        pieces_signalled += f;
-                    }
-                    if (!(ok = warp_wait(bar(kQEmpty + (piece & 1)), par, 42))) break;
-                }
-                load_query_rows<D>(p, cur.b, head, cur.rows * p.g, cur.rb * MB, warp * 64, 64, sQ(piece & 1));
+                if (!(ok = warp_wait<true>(bar(kQEmpty + (piece & 1)), ((uint32_t)(piece >> 1) & 1) ^ 1, 42))) break;
+                load_query_rows<D>(p, cur.b, head, cur.rows * p.g, cur.rb * MB, loader * (QR / NL), QR / NL, sQ(piece & 1), Sh::kQPanel);
+                cp_async_arrive(bar(kQFull + (piece & 1)));
             }
             const int s = i % ST;
-            if (!(ok = warp_wait(bar(kEmpty + s), ((uint32_t)(i / ST) & 1) ^ 1, 43))) break;
+            if (!(ok = warp_wait<true>(bar(kEmpty + s), ((uint32_t)(i / ST) & 1) ^ 1, 43))) break;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t got = load_16_slots<D>(p.c, cur.b, head, cur.first_slot() + warp * 32 + k * 16, cur.lo, cur.hi, sK(s), sV(s), true,
-                                                      warp * 32 + k * 16, 8192, p.page_whole);
-                if (lane == 0) there[s][warp * 2 + k] = got;
+            for (int k = 0; k < SW; k += 16) {
+                const uint32_t got = load_16_slots<D>(p.c, cur.b, head, cur.first_slot() + loader * SW + k, cur.lo, cur.hi, sK(s), sV(s), true,
+                                                      loader * SW + k, 8192, p.page_whole);
+                if (lane == 0) there[s][(loader * SW + k) / 16] = got;
             }
-            cp_async_commit();
-            firsts = firsts << 1 | (first ? 1u : 0u);
+            cp_async_arrive(bar(kFull + s));
+            if (lane == 0) mbar_arrive(bar(kFull + s));
             ++cur.tile;
-            cp_async_wait<LAG>();
-            for (; signalled <= i - LAG; ++signalled) {
-                const bool f = (firsts >> (i - signalled)) & 1;
-                signal(signalled, f, pieces_signalled);
-                pieces_signalled += f;
-            }
-        }
-        cp_async_wait<0>();
-        for (; ok && signalled < n_tiles; ++signalled) {
-            const bool f = (firsts >> (n_tiles - 1 - signalled)) & 1;
-            signal(signalled, f, pieces_signalled);
-            pieces_signalled += f;
         }
     } else if (warp == 2) {
         // ---------------- issuer ----------------
-        bool ok = true, fresh = false, prev_fresh = false;
+        // S(i) as soon as its tile has landed and its buffer's scores have been read, O += P(j) V as soon as P(j) is there,
+        // whichever comes first.  What the loaders' copies wrote is in the generic proxy's order and the products read through
+        // the async one: the fence between the two stands here, after the barrier that the copies complete.
         constexpr uint32_t idesc_s = make_idesc_bf16(128, 64, 0, 0), idesc_o = make_idesc_bf16(128, D, 0, 1);
-        int piece = 0, piece_start = 0;
-        for (int i = 0; i <= n_tiles && ok; ++i) {
-            if (i < n_tiles) {
-                const bool first = i == 0 || cur.tile == cur.end;
-                if (i > 0 && first) {
-                    cur.next_item(p);
-                    ++piece;
-                    piece_start = i;
-                }
-                fresh = i - piece_start < 2;  // the first tile of its group in the piece
-                if (first && !(ok = warp_wait(bar(kQFull + (piece & 1)), (uint32_t)(piece >> 1) & 1, 44))) break;
-                if (!(ok = warp_wait(bar(kFull + i % ST), (uint32_t)(i / ST) & 1, 45))) break;
-                tc_fence_after();
-                const uint64_t qd = make_sdesc(sQ(piece & 1), 16, 1024), kd = make_sdesc(sK(i % ST), 16, 1024);
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    mma_ss(tS + (i & 1) * 64, qd + (((k / 4) * 16384 + (k % 4) * 32) >> 4), kd + (((k / 4) * 8192 + (k % 4) * 32) >> 4), idesc_s, k > 0);
-                mma_commit(bar(kSFull + (i & 1)));
-                ++cur.tile;
-                mma_commit_if(cur.tile == cur.end || i == n_tiles - 1, bar(kQEmpty + (piece & 1)));
+        int i = 0, j = 0, piece = 0, piece_start = 0;
+        uint32_t fresh = 0;  // bit k & 31: tile k is the first of its group in its piece
+        bool first = true, tile_there = false;
+        for (int idle = 0; j < n_tiles; ++idle) {
+            if (idle > (1 << 18)) {  // a long time without either: a bounded wait for what has to come next
+                if (!(j < i ? warp_wait<true>(bar(kPFull + (j & 1)), (uint32_t)(j >> 1) & 1, 46)
+                            : warp_wait<true>(bar(kFull + i % ST), (uint32_t)(i / ST) & 1, 45) &&
+                                  (!first || warp_wait<true>(bar(kQFull + (piece & 1)), (uint32_t)(piece >> 1) & 1, 44))))
+                    break;
+                idle = 0;
             }
-            if (i > 0) {
-                const int j = i - 1;
-                if (!(ok = warp_wait(bar(kPFull + (j & 1)), (uint32_t)(j >> 1) & 1, 46))) break;
+            if (j < i && __all_sync(0xffffffffu, mbar_test_wait(bar(kPFull + (j & 1)), (uint32_t)(j >> 1) & 1))) {
                 tc_fence_after();
                 const uint64_t vd = make_sdesc(sV(j % ST), 8192, 1024);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    mma_ts(tO + (j & 1) * 128, tP + (j & 1) * 32 + k * 8, vd + ((k * 2048) >> 4), idesc_o, !prev_fresh || k > 0);
+                    mma_ts(tO + (j & 1) * 128, tP + (j & 1) * 32 + k * 8, vd + ((k * 2048) >> 4), idesc_o, k > 0 || !((fresh >> (j & 31)) & 1));
                 mma_commit(bar(kPvDone + (j & 1)));
                 mma_commit(bar(kEmpty + j % ST));
+                ++j;
+                idle = 0;
             }
-            prev_fresh = fresh;
+            if (i == n_tiles) continue;
+            if (!tile_there) {
+                if (!__all_sync(0xffffffffu, mbar_test_wait(bar(kFull + i % ST), (uint32_t)(i / ST) & 1) &&
+                                                 (!first || mbar_test_wait(bar(kQFull + (piece & 1)), (uint32_t)(piece >> 1) & 1))))
+                    continue;
+                fence_proxy_async_smem();
+                tile_there = true;
+            }
+            if (i >= 2 && !__all_sync(0xffffffffu, mbar_test_wait(bar(kSRead + (i & 1)), (uint32_t)((i >> 1) - 1) & 1))) continue;
+            tc_fence_after();
+            const uint64_t qd = make_sdesc(sQ(piece & 1), 16, 1024), kd = make_sdesc(sK(i % ST), 16, 1024);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                mma_ss(tS + (i & 1) * 64, qd + (((k / 4) * Sh::kQPanel + (k % 4) * 32) >> 4), kd + (((k / 4) * 8192 + (k % 4) * 32) >> 4), idesc_s, k > 0);
+            mma_commit(bar(kSFull + (i & 1)));
+            fresh = (fresh & ~(1u << (i & 31))) | ((i - piece_start < 2 ? 1u : 0u) << (i & 31));
+            ++i;
+            ++cur.tile;
+            tile_there = first = false;
+            idle = 0;
+            if (cur.tile == cur.end || i == n_tiles) {
+                mma_commit(bar(kQEmpty + (piece & 1)));
+                if (i < n_tiles) {
+                    cur.next_item(p);
+                    ++piece;
+                    piece_start = i;
+                    first = true;
+                }
+            }
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && (warp & 3) < QR / 32) {
         // ---------------- softmax ----------------
         bool ok = true;
-        const int grp = (warp - 4) >> 2, row = (tid - 128) & 127, quarter = warp & 3;
+        const int grp = (warp - 4) >> 2, row = tid & 127, quarter = warp & 3;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, tSg = tS + lanes + grp * 64, tPg = tP + lanes + grp * 32;
         // All softmax warps meet at an item's end, whatever has become of them: a warp whose wait has failed gets there at once,
         // the others when theirs fail too, and none goes on when one has failed.
         auto both_agree = [](bool mine) {
             uint32_t all;
-            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 3, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                         : "=r"(all) : "r"((uint32_t)mine) : "memory");
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 3, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                         : "=r"(all) : "r"((uint32_t)mine), "n"(2 * QR) : "memory");
             return all != 0;
+        };
+        auto scores_read = [&] {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kSRead + grp));
+        };
+        // O += P V of the group's tile q (of the one before its tile, or its last): waited for tile by tile, so that a wait by
+        // parity cannot take one phase for another
+        auto products_done = [&](int q) {
+            const bool y = q < 0 || warp_wait<true>(bar(kPvDone + grp), (uint32_t)(q >> 1) & 1, 49);
+            tc_fence_after();
+            return y;
         };
         int scans = 0;
         int i0 = 0;  // the piece's first tile
@@ -254,10 +275,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
             int done = -1;  // the group's last tile of the piece
             const int slot_first = cur.first_slot();
             for (int i = i0 + ((i0 ^ grp) & 1); i < i0 + count; i += 2) {
-                // S(i) has come: the products of tile i - 2, this group's last, were issued before it and are done
-                if (!(ok = warp_wait(bar(kSFull + grp), (uint32_t)(i >> 1) & 1, 47))) break;
+                if (!(ok = warp_wait<true>(bar(kSFull + grp), (uint32_t)(i >> 1) & 1, 47))) break;
                 const int st = i % ST, slot0 = slot_first + (i - i0) * 64;
-                if (!(ok = warp_wait(bar(kFull + st), (uint32_t)(i / ST) & 1, 51))) break;  // done: for what the loaders wrote
+                if (!(ok = warp_wait<true>(bar(kFull + st), (uint32_t)(i / ST) & 1, 51))) break;  // done: for what the loaders wrote
                 tc_fence_after();
                 uint32_t pk[32];
                 unsigned long long bad = 0;
@@ -270,6 +290,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
                     tmem_ld_x32(tSg + 32, s1);
                     tmem_wait_ld_dep(s0);
                     reg_fence32(s1);
+                    scores_read();
                     const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2), base2 = f32x2(-base, -base);
                     auto over_base = [&](uint32_t (&s)[32]) {
 #pragma unroll
@@ -315,6 +336,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
                             }
                         }
                         if (done >= 0) {  // O holds the group's earlier tiles of the piece
+                            if (!(ok = products_done(i - 2))) break;
 #pragma unroll 1
                             for (int c = 0; c < D; c += 32) {
                                 uint32_t o[32];
@@ -339,6 +361,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
                     }
                     l += la + lb;
                 } else {
+                    scores_read();
 #pragma unroll
                     for (int e = 0; e < 32; ++e) pk[e] = 0u;
                 }
@@ -362,7 +385,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bar(kScan + grp));
                         if (quarter == 0) {
-                            if (!(ok = warp_wait(bar(kScan + grp), (uint32_t)scans & 1, 52))) break;
+                            if (!(ok = warp_wait<true>(bar(kScan + grp), (uint32_t)scans & 1, 52))) break;
 #pragma unroll 1
                             for (int j = 0; j < 64; ++j)
                                 if (((bad >> j) & 1) && lane < C) st_shared_v4(sV(st) + panel_at(j, lane, 8192), 0u, 0u, 0u, 0u);
@@ -371,6 +394,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
                         ++scans;
                     }
                 }
+                if (!(ok = products_done(i - 2))) break;  // they have read the P buffer
                 tmem_st_x32(tPg, pk);
                 tmem_wait_st();
                 tc_fence_before();
@@ -378,8 +402,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
                 if (lane == 0) mbar_arrive(bar(kPFull + grp));
                 done = i;
                 if (bad) {
-                    if (!(ok = warp_wait(bar(kPvDone + grp), (uint32_t)(i >> 1) & 1, 49))) break;
-                    tc_fence_after();
+                    if (!(ok = products_done(i))) break;
                     float w[64];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
@@ -408,8 +431,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) decode_rows_kernel(const __gr
                 }
             }
             // ---- the piece's rows: both groups' parts joined, each group writing one half of the dims ----
-            if (ok && done >= 0) ok = warp_wait(bar(kPvDone + grp), (uint32_t)(done >> 1) & 1, 50);
-            tc_fence_after();
+            if (ok && done >= 0) ok = products_done(done);
             end_ml[grp][row] = make_float2(done < 0 || slack == -INFINITY ? -INFINITY : base, l);
             tc_fence_before();
             ok = both_agree(ok);
@@ -523,7 +545,7 @@ __global__ void __launch_bounds__(128) decode_row_weights_kernel(const __grid_co
         bool ok = true;
         for (int r0 = 0, turn = 0; r0 < rows && ok; r0 += 128, ++turn) {
             const int m = min(128, rows - r0);
-            load_query_rows<D>(p, b, h, rows, r0, warp * 32, 32, q_tile);
+            load_query_rows<D>(p, b, h, rows, r0, warp * 32, 32, q_tile, 16384);
             if (tid < m) {
                 const int r = r0 + tid, t = (int)fdiv((uint32_t)r, p.f_g);
                 const float l = p.LSE[((long long)b * p.Hq + h * p.g + r - t * p.g) * p.c.Lq + t];
@@ -547,7 +569,7 @@ __global__ void __launch_bounds__(128) decode_row_weights_kernel(const __grid_co
                 }
                 mma_commit(bar);
             }
-            ok = warp_wait(bar, turn & 1, 41);
+            ok = warp_wait<true>(bar, turn & 1, 41);
             tc_fence_after();
             const bool have = ok && (loaded[tid >> 4] >> (tid & 15)) & 1;
             for (int c = 0; c < m && ok; c += 32) {
