@@ -502,57 +502,73 @@ __global__ void __launch_bounds__(RowsShape<D, QR>::kThreads, 1) decode_rows_ker
 // ---- attention weights ---------------------------------------------------------------------------------------------
 // Sum over the rows of each slot's weight, from the finished LSE: S^T = K Q^T again, 128 slots in M and up to 128 rows in N, a
 // thread with its slot's row of the accumulator.  Keeping the scores of the first pass instead would write and read 8 bytes a
-// (row, slot), more than the 256 bytes of K from 32 rows on.  A block per 128 slots of a (sequence, KV head), three to an SM.
-template <int D>
+// (row, slot), more than the 256 bytes of K from 32 rows on.  A block takes four tiles of 128 slots of one (sequence, KV head)
+// one after the other; three or four blocks to an SM cover each other's loads (two blocks with the next tile on its way while
+// one is computed took longer).  Where QR rows hold all of them the queries are loaded once.
+constexpr int kWeightTiles = 4;
+template <int D, int QR>
 struct RowWeightsShape {
-    static constexpr int kTile = (D / 64) * 16384;
-    static constexpr int kDynamic = 2 * kTile + 1024;
+    static constexpr int kTile = (D / 64) * 16384, kQPanel = QR * 128;
+    static constexpr int kDynamic = kTile + (D / 64) * kQPanel + 1024;
 };
-template <int D>
+template <int D, int QR>
 __global__ void __launch_bounds__(128) decode_row_weights_kernel(const __grid_constant__ DecodeParams p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(16) float lse2[128];
-    __shared__ int lo[128], hi[128];
+    __shared__ __align__(16) float lse2[QR];
+    __shared__ int lo[QR], hi[QR];
     __shared__ uint32_t tmem_slot, loaded[8];
     __shared__ __align__(8) uint64_t bar_mem;
     after_previous_kernel();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, h = blockIdx.y, b = blockIdx.z;
-    const int new_r = new_rows(p.c, b), n = seq_len(p.c, b), slot0 = blockIdx.x * 128, j = slot0 + tid;
-    if (slot0 >= n || new_r == 0) return;
+    const int new_r = new_rows(p.c, b), n = seq_len(p.c, b), first = blockIdx.x * (128 * kWeightTiles);
+    if (first >= n || new_r == 0) return;
     const int shift = shift_of(p.c, b), cls = p.head_class[h], rows = new_r * p.g;
-    const long long at = ((long long)b * p.c.Hkv + h) * p.W + j;
-    int all_lo, all_hi;
-    int inner_lo, inner_hi;  // every row sees the slots between these
+    const float* w_in = p.w_in ? p.w_in + ((long long)b * p.c.Hkv + h) * p.W : nullptr;
+    float* w_out = p.w_out + ((long long)b * p.c.Hkv + h) * p.W;
+    int all_lo, all_hi, inner_lo, inner_hi;  // slots that some row sees, and that every row sees
     visible_slots(p, n, new_r, shift, 0, cls, &all_lo, &inner_hi);
     visible_slots(p, n, new_r, shift, new_r - 1, cls, &inner_lo, &all_hi);
-    const bool inner = slot0 >= inner_lo && slot0 + 128 <= inner_hi;
-    float sum = 0.f;
-    if (slot0 < all_hi && slot0 + 128 > all_lo) {
-        const uint32_t tile = (smem_u32(smem_raw) + 1023u) & ~1023u, q_tile = tile + RowWeightsShape<D>::kTile, bar = smem_u32(&bar_mem);
-        if (tid == 0) {
-            mbar_init(bar, 1);
-            fence_mbar_init();
+    // this block's tiles with a visible slot: [t0, t1) of its kWeightTiles; the others take over what they had
+    const int end = min(n, first + 128 * kWeightTiles);
+    const int t0 = min(max((all_lo - first) / 128, 0), kWeightTiles), t1 = min(max((min(all_hi, end) - first + 127) / 128, t0), kWeightTiles);
+    for (int j = first + tid; j < end; j += 128)
+        if (j < first + t0 * 128 || j >= first + t1 * 128) w_out[j] = w_in ? w_in[j] : 0.f;
+    if (t0 == t1) return;
+    using Sh = RowWeightsShape<D, QR>;
+    const uint32_t k_tile = (smem_u32(smem_raw) + 1023u) & ~1023u, q_tile = k_tile + Sh::kTile, bar = smem_u32(&bar_mem);
+    if (tid == 0) {
+        mbar_init(bar, 1);
+        fence_mbar_init();
+    }
+    if (warp == 0) {
+        tmem_alloc(smem_u32(&tmem_slot), 128);
+        tmem_relinquish();
+    }
+    auto load_rows = [&](int r0) {
+        load_query_rows<D>(p, b, h, rows, r0, warp * (QR / 4), QR / 4, q_tile, Sh::kQPanel);
+        if (tid < QR && r0 + tid < rows) {
+            const int r = r0 + tid, t = (int)fdiv((uint32_t)r, p.f_g);
+            const float l = p.LSE[((long long)b * p.Hq + h * p.g + r - t * p.g) * p.c.Lq + t];
+            visible_slots(p, n, new_r, shift, t, cls, &lo[tid], &hi[tid]);
+            if (l == -INFINITY) hi[tid] = lo[tid];
+            lse2[tid] = l * 1.4426950408889634f;
         }
-        if (warp == 0) {
-            tmem_alloc(smem_u32(&tmem_slot), 128);
-            tmem_relinquish();
-        }
+    };
+    bool ok = true;
+    uint32_t turn = 0;
+    for (int t = t0; t < t1 && ok; ++t) {
+        const int slot0 = first + t * 128, j = slot0 + tid;
+        const bool inner = slot0 >= inner_lo && slot0 + 128 <= inner_hi;
+        float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const uint32_t got = load_16_slots<D>(p.c, b, h, slot0 + warp * 32 + k * 16, all_lo, all_hi, tile, 0, false, warp * 32 + k * 16, 16384, p.page_whole);
+            const uint32_t got = load_16_slots<D>(p.c, b, h, slot0 + warp * 32 + k * 16, all_lo, all_hi, k_tile, 0, false, warp * 32 + k * 16, 16384,
+                                                  p.page_whole);
             if (lane == 0) loaded[warp * 2 + k] = got;
         }
-        bool ok = true;
-        for (int r0 = 0, turn = 0; r0 < rows && ok; r0 += 128, ++turn) {
-            const int m = min(128, rows - r0);
-            load_query_rows<D>(p, b, h, rows, r0, warp * 32, 32, q_tile, 16384);
-            if (tid < m) {
-                const int r = r0 + tid, t = (int)fdiv((uint32_t)r, p.f_g);
-                const float l = p.LSE[((long long)b * p.Hq + h * p.g + r - t * p.g) * p.c.Lq + t];
-                visible_slots(p, n, new_r, shift, t, cls, &lo[tid], &hi[tid]);
-                if (l == -INFINITY) hi[tid] = lo[tid];
-                lse2[tid] = l * 1.4426950408889634f;
-            }
+        for (int r0 = 0; r0 < rows && ok; r0 += QR, ++turn) {
+            const int m = min(QR, rows - r0);
+            if (rows > QR || t == t0) load_rows(r0);
             cp_async_commit();
             cp_async_wait<0>();
             fence_proxy_async_smem();
@@ -560,12 +576,11 @@ __global__ void __launch_bounds__(128) decode_row_weights_kernel(const __grid_co
             __syncthreads();
             tc_fence_after();
             if (warp == 0) {
-                const uint64_t kd = make_sdesc(tile, 16, 1024), qd = make_sdesc(q_tile, 16, 1024);
+                const uint64_t kd = make_sdesc(k_tile, 16, 1024), qd = make_sdesc(q_tile, 16, 1024);
                 const uint32_t idesc = make_idesc_bf16(128, (m + 15) & ~15, 0, 0);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = ((k / 4) * 16384 + (k % 4) * 32) >> 4;
-                    mma_ss(tmem_slot, kd + off, qd + off, idesc, k > 0);
+                    mma_ss(tmem_slot, kd + (((k / 4) * 16384 + (k % 4) * 32) >> 4), qd + (((k / 4) * Sh::kQPanel + (k % 4) * 32) >> 4), idesc, k > 0);
                 }
                 mma_commit(bar);
             }
@@ -577,12 +592,16 @@ __global__ void __launch_bounds__(128) decode_row_weights_kernel(const __grid_co
                 tmem_ld_x32(tmem_slot + ((uint32_t)(warp * 32) << 16) + c, s);
                 tmem_wait_ld_dep(s);
                 if (have && inner && c + 32 <= m) {
+                    float x[4] = {};
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
                         const float4 l = *reinterpret_cast<const float4*>(lse2 + c + i);
-                        sum += ex2(fmaf(__uint_as_float(s[i]), p.scale_log2, -l.x)) + ex2(fmaf(__uint_as_float(s[i + 1]), p.scale_log2, -l.y));
-                        sum += ex2(fmaf(__uint_as_float(s[i + 2]), p.scale_log2, -l.z)) + ex2(fmaf(__uint_as_float(s[i + 3]), p.scale_log2, -l.w));
+                        x[0] += ex2(fmaf(__uint_as_float(s[i]), p.scale_log2, -l.x));
+                        x[1] += ex2(fmaf(__uint_as_float(s[i + 1]), p.scale_log2, -l.y));
+                        x[2] += ex2(fmaf(__uint_as_float(s[i + 2]), p.scale_log2, -l.z));
+                        x[3] += ex2(fmaf(__uint_as_float(s[i + 3]), p.scale_log2, -l.w));
                     }
+                    sum += (x[0] + x[1]) + (x[2] + x[3]);
                 } else if (have) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
@@ -592,13 +611,15 @@ __global__ void __launch_bounds__(128) decode_row_weights_kernel(const __grid_co
             tc_fence_before();
             ok = __syncthreads_and(ok);
         }
-        drain_if_failed();
-        if (warp == 0) {
-            __syncwarp();
-            tmem_dealloc(tmem_slot, 128);
-        }
+        if (j < n) w_out[j] = (w_in ? w_in[j] : 0.f) + sum;
     }
-    if (j < n) p.w_out[at] = (p.w_in ? p.w_in[at] : 0.f) + sum;
+    cp_async_wait<0>();
+    drain_if_failed();
+    __syncthreads();
+    if (warp == 0) {
+        __syncwarp();
+        tmem_dealloc(tmem_slot, 128);
+    }
 }
 
 }  // namespace segattn
