@@ -8,7 +8,9 @@
 
 namespace segattn {
 
-constexpr int kDecRowsMin = 33;  // rows to a KV head from which these kernels take over
+// Rows to a KV head from which these kernels take over: at 32 rows both take 46 us (4 x 14000 slots, half of the heads with
+// their whole past), at 24 and fewer decode_kernel is ahead, by far where weights are asked for; at 64 it takes 66 us to 49.
+constexpr int kDecRowsMin = 33;
 
 // 16-byte piece c of row r in an operand tile of 64-element panels with 128-byte swizzled rows.
 __device__ __forceinline__ uint32_t panel_at(int r, int c, int panel_bytes) {
