@@ -355,7 +355,8 @@ typedef struct {
     int32_t table_stride;        /* elements between rows of the block table, >= max_pages */
     void *K, *V;                 /* DEVICE, 16-byte aligned */
     int64_t k_stride[3], v_stride[3]; /* elements, for (page, row, head); multiples of 16 bytes; the last dimension is contiguous */
-    const float *k_scale, *v_scale;   /* E4M3: DEVICE [Hkv], > 0, finite, with finite inverses (not checked); BF16: NULL */
+    const float *k_scale, *v_scale;   /* E4M3: DEVICE [Hkv], > 0, finite, with finite inverses (not checked);
+                                       * an eviction, which moves rows as they are, needs none.  BF16: NULL */
     const int32_t* block_table;  /* DEVICE [B][max_pages]; entries past a sequence's last page are not read */
     const int32_t* kv_len;       /* DEVICE [B] */
     const int32_t* q_len;        /* DEVICE [B], new rows of each sequence, or NULL: Lq for all */

@@ -9,7 +9,7 @@ A cache is described by the same tensors in every call:
 ``kv_len``                int32 ``[B]``: rows of every sequence, the call's new ones included
 ``q_len``                 int32 ``[B]`` or None: how many of the ``Lq`` rows given are there (the first ones); None: all
 ``pos_shift``             int32 ``[B]`` or None: rows that evictions have taken out (global position = slot + shift)
-``k_scale``, ``v_scale``  fp32 ``[Hkv]``, for an 8-bit cache only
+``k_scale``, ``v_scale``  fp32 ``[Hkv]``, for an 8-bit cache only (where its values are read or written)
 
 Lengths stay on the device, so that a decoding step can be captured in a CUDA graph and replayed as they grow.
 """
@@ -91,7 +91,7 @@ def _mask_bytes(head_past_mask, Hkv: int) -> bytes:
     return _mask_arr(head_past_mask, Hkv).tobytes()
 
 
-def _cache(K, V, block_table, kv_len, q_len, pos_shift, k_scale, v_scale):
+def _cache(K, V, block_table, kv_len, q_len, pos_shift, k_scale, v_scale, reads_values: bool = True):
     """seg_kv_cache of these tensors as bytes, and (B, Hkv, d, page_size, max_pages, CUDA device)."""
     dev, kind = K.get_device(), K.dtype
     shape = K.shape
@@ -100,10 +100,11 @@ def _cache(K, V, block_table, kv_len, q_len, pos_shift, k_scale, v_scale):
     n_pages, page, Hkv, d = shape
     ks_ptr = vs_ptr = 0
     if kind is _E4M3:
-        if k_scale is None or v_scale is None:
-            raise ValueError("an 8-bit cache needs k_scale and v_scale")
-        ks_ptr = _flat(k_scale, _F32, (Hkv,), "k_scale", dev).data_ptr()
-        vs_ptr = _flat(v_scale, _F32, (Hkv,), "v_scale", dev).data_ptr()
+        if reads_values:
+            if k_scale is None or v_scale is None:
+                raise ValueError("an 8-bit cache needs k_scale and v_scale")
+            ks_ptr = _flat(k_scale, _F32, (Hkv,), "k_scale", dev).data_ptr()
+            vs_ptr = _flat(v_scale, _F32, (Hkv,), "v_scale", dev).data_ptr()
     elif kind is not _BF16:
         raise ValueError("the cache must be bf16 or float8_e4m3fn")
     elif k_scale is not None or v_scale is not None:
@@ -257,13 +258,14 @@ def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, he
 
 
 def kv_evict(weights, K_pages, V_pages, block_table, kv_len, dst_table, sink: int, recent: int, heavy: int, pos_shift=None,
-             k_scale=None, v_scale=None, weights_out=None, kv_len_out=None, pos_shift_out=None, workspace=None, stream=None):
+             weights_out=None, kv_len_out=None, pos_shift_out=None, workspace=None, stream=None):
     """Brings every sequence of more than sink + recent + heavy rows down to that many per KV head: the first `sink`, the last
     `recent` and the `heavy` rows of largest accumulated weight between them, copied in order to the pages of dst_table (int32
-    [B, pages], none of them a page the sequence has now) - the C entry point `seg_kv_evict`.  weights is fp32 [B, Hkv, W] as
+    [B, pages], none of them a page the sequence has now) - the C entry point `seg_kv_evict`.  Rows are moved as they are: an
+    8-bit cache's scales are not needed.  weights is fp32 [B, Hkv, W] as
     seg_attn_decode gathers it.  Returns (idx int32 [B, Hkv, budget] (the slots kept, then -1), kv_len, pos_shift, weights) of
     the evicted cache, whose block table is dst_table; kv_len_out may be kv_len and pos_shift_out pos_shift."""
-    c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, None, pos_shift, k_scale, v_scale)
+    c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, None, pos_shift, None, None, reads_values=False)
     _, dst_pages, dst_stride = _pages(dst_table, B, "dst_table", dev)
     W = weights.shape[-1] if weights.dim() == 3 else 0
     _flat(weights, _F32, (B, Hkv, W), "weights", dev)

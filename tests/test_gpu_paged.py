@@ -424,8 +424,7 @@ def test_evict_matches_the_definition(case, kind, fp8):
     shift = torch.arange(B, dtype=torch.int32, device="cuda") * 10
     bits = lambda t: t.view(torch.uint8) if fp8 else t.view(torch.int16)
     K0, V0 = bits(c.K).clone(), bits(c.V).clone()
-    idx, n2, s2, w2 = sa.kv_evict(w, c.K, c.V, dst_table=dst.cuda(), sink=sink, recent=recent, heavy=heavy, pos_shift=shift, **c.dev,
-                                  **c.scales)
+    idx, n2, s2, w2 = sa.kv_evict(w, c.K, c.V, dst_table=dst.cuda(), sink=sink, recent=recent, heavy=heavy, pos_shift=shift, **c.dev)
     sa.poll_status()
     want_k, want_v, want_w = K0.clone(), V0.clone(), torch.zeros(B, Hkv, W)
     wc = w.cpu()

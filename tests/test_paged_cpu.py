@@ -72,8 +72,11 @@ def evict(c, w=OK, W=128, sink=1, recent=20, heavy=10, dst=OK, pages=2, stride=2
 @pytest.mark.parametrize("bad", BAD_CACHES, ids=str)
 def test_bad_caches_are_refused(bad):
     c = cache(**bad)
-    assert decode(c) == 1 and append(c) == 1 and evict(c) == 1
-    assert sa.lib().seg_attn_decode_workspace_bytes(c, 1, 4, 0) == 0 and sa.lib().seg_kv_evict_workspace_bytes(c) == 0
+    assert decode(c) == 1 and append(c) == 1 and sa.lib().seg_attn_decode_workspace_bytes(c, 1, 4, 0) == 0
+    if bad == dict(dtype=1):      # without scales: an eviction reads no values
+        assert sa.lib().seg_kv_evict_workspace_bytes(c) > 0 and evict(c, ws=None) == 5
+    else:
+        assert evict(c) == 1 and sa.lib().seg_kv_evict_workspace_bytes(c) == 0
 
 
 @pytest.mark.parametrize("bad", [dict(Lq=-1), dict(Hq=3), dict(Hq=0), dict(S=0), dict(T=-1), dict(T=65), dict(scale=0.0), dict(scale=float("nan")),
