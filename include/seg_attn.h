@@ -338,7 +338,8 @@ segattn_status seg_rope_rotate(int32_t B, int32_t L, int32_t H, int32_t d, int32
 
 /* ---- Serving: a paged key/value cache, the attention of new tokens over it, and its eviction.  The paper stops at the
  * prefill; these continue it token by token under the same mask.  A sequence's rows lie in pages of page_size rows, slot j
- * in row j % page_size of page block_table[b][j / page_size]; a page belongs to one sequence.  kv_len[b] counts the rows
+ * in row j % page_size of page block_table[b][j / page_size]; a page that a call writes belongs to one sequence, one that
+ * is only read may be shared (a common prefix).  kv_len[b] counts the rows
  * including the call's new ones: new row t of sequence b (t < q_len[b]) has slot kv_len[b] - q_len[b] + t and the global
  * position slot + pos_shift[b], where pos_shift counts the rows that evictions have taken out.
  * Everything the kernels read per sequence is in device memory, so a captured graph follows the lengths as they grow.
@@ -348,7 +349,7 @@ segattn_status seg_rope_rotate(int32_t B, int32_t L, int32_t H, int32_t d, int32
 #define SEGATTN_KV_BF16 0
 #define SEGATTN_KV_E4M3 1 /* 8-bit values, 1 + 4 + 3 bits, times a scale per KV head */
 typedef struct {
-    int32_t B, Hkv, d;           /* sequences; KV heads, at most 64; head dimension, 64 or 128 */
+    int32_t B, Hkv, d;           /* sequences, at most 65535; KV heads, at most 64; head dimension, 64 or 128 */
     int32_t dtype;               /* SEGATTN_KV_* */
     int32_t page_size, n_pages;  /* rows in a page, >= 1; pages in K and in V */
     int32_t max_pages;           /* entries of a sequence's row of the block table; max_pages*page_size <= 2^30 */
@@ -384,6 +385,7 @@ segattn_status seg_kv_append(const seg_kv_cache* c, int32_t Lq, const void* K_ne
  *     weights_out[b][h][j] = (weights_in ? weights_in[b][h][j] : 0) + sum over the new rows and the query heads of h of the
  *     row's attention weight on j;
  *   other entries are left as they were.  weights_in may be weights_out.  W >= max_pages*page_size.
+ * SEGATTN_ERR_INVALID also where B * Hkv * (Hq/Hkv*Lq/8 rounded up) * (max_pages*page_size/64 + 3) passes 2^30.
  * `workspace`: DEVICE, 256-byte aligned, seg_attn_decode_workspace_bytes(...) bytes, scratch (0 = invalid parameters); calls
  * that may run at the same time, captured ones too, need one each.  Results do not change from run to run.
  * fp32 scores, statistics and accumulators; the weights are rounded to 16 bits before the product with V (bf16, or fp16
@@ -402,13 +404,11 @@ segattn_status seg_attn_decode(const seg_kv_cache* c, int32_t Lq, int32_t Hq, in
  *   idx          int32 contiguous [B][Hkv][budget]: the slots kept, ascending, then -1
  *   kv_len_out   int32 [B]: min(n, budget);  pos_shift_out int32 [B]: pos_shift + n - kv_len_out.  Either may be the cache's own.
  *   weights_out  fp32 contiguous [B][Hkv][W]: the kept slots' weights, then zeros; may not overlap weights
- * W >= max_pages*page_size, 1 <= budget <= dst_max_pages*page_size and budget <= W.  q_len is ignored.
- * `workspace`: DEVICE, 256-byte aligned, seg_kv_evict_workspace_bytes(c) bytes (0 = invalid parameters), scratch. */
-size_t seg_kv_evict_workspace_bytes(const seg_kv_cache* c);
+ * W >= max_pages*page_size, 1 <= budget <= dst_max_pages*page_size and budget <= W.  q_len is ignored.  Two kernels, no
+ * workspace. */
 segattn_status seg_kv_evict(const seg_kv_cache* c, const float* weights, int32_t W, int32_t sink, int32_t recent,
                             int32_t heavy, const int32_t* dst_table, int32_t dst_max_pages, int32_t dst_stride, int32_t* idx,
-                            int32_t* kv_len_out, int32_t* pos_shift_out, float* weights_out, void* workspace,
-                            size_t workspace_bytes, void* stream);
+                            int32_t* kv_len_out, int32_t* pos_shift_out, float* weights_out, void* stream);
 
 /* ---- Whole training-step call with HOST buffers (pinned or pageable): copies Q, K, V, dO to
  * the device arena, runs forward and backward, copies O, LSE, dQ, dK, dV back, and

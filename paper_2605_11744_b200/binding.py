@@ -90,9 +90,7 @@ def lib():
         L.seg_attn_decode_workspace_bytes.argtypes = [vp, i32, i32, i32]
         L.seg_attn_decode.argtypes = [vp, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp,
                                       ctypes.c_size_t, vp]
-        L.seg_kv_evict_workspace_bytes.restype = ctypes.c_size_t
-        L.seg_kv_evict_workspace_bytes.argtypes = [vp]
-        L.seg_kv_evict.argtypes = [vp, vp, i32, i32, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.seg_kv_evict.argtypes = [vp, vp, i32, i32, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp]
         L.seg_attn_status_string.restype = ctypes.c_char_p
         L.seg_attn_status_string.argtypes = [ctypes.c_int]
         L.seg_attn_last_cuda_error.restype = ctypes.c_int

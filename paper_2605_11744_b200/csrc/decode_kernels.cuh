@@ -48,7 +48,6 @@ struct DecodeParams {
     int row_blocks;                  // ceil(g Lq / (rows of an item))
     int page_whole;                  // page_size is a multiple of 16: a warp's slots lie in one page
     int pitch;                       // slots in a row of scores
-    int min_tiles;                   // a block's range has at least this many tiles
     float scale_log2;                // sm_scale * log2(e)
     // KV heads are taken in units of one class: 1, 2 or 4 of them, side by side in the block's warps
     int unit_log[3], units[3];       // by class: heads to a unit (log2), and units
@@ -184,7 +183,7 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
         if (k < warp) before += warp_sum[k];
         total += warp_sum[k];
     }
-    const int per = max(p.min_tiles, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+    const int per = max(1, (total + (int)gridDim.x - 1) / (int)gridDim.x);
     const int begin = min((int)blockIdx.x * per, total), end = min(begin + per, total);
     if (begin < end && begin >= before && begin < before + mine) {
         int off = begin - before, b = b0;
@@ -860,17 +859,17 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
     cp_async_wait<0>();
 }
 
-// Adds the parts of one row of an item that several blocks share; block.x = the row, block.y = the item, a thread one dim.
+// Adds the parts of one row of an item that several blocks share; block.x = the item, block.y = the row, a thread one dim.
 // A row has at most as many parts as the grid has blocks: their bases and sums are read by all threads at once, and the first
 // values of O beside them, so that two dependent reads are all the latency there is.
 template <int D>
 __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ DecodeParams p, int MB, int part_rows) {
     constexpr int AHEAD = 8;
-    const int rb = blockIdx.y % p.row_blocks, u = blockIdx.y / p.row_blocks, h = u % p.c.Hkv, b = u / p.c.Hkv;
-    const int rl = blockIdx.x, r = rb * MB + rl, tid = threadIdx.x;
+    const int rb = blockIdx.x % p.row_blocks, u = blockIdx.x / p.row_blocks, h = u % p.c.Hkv, b = u / p.c.Hkv;
+    const int rl = blockIdx.y, r = rb * MB + rl, tid = threadIdx.x;
     after_previous_kernel();
     if (r >= new_rows(p.c, b) * p.g) return;
-    const int2 blocks = p.item_blocks[blockIdx.y];
+    const int2 blocks = p.item_blocks[blockIdx.x];
     if (blocks.x == blocks.y) return;
     __shared__ float weight[kDecMaxBlocks];
     __shared__ float red[2][D / 32];

@@ -258,7 +258,7 @@ def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, he
 
 
 def kv_evict(weights, K_pages, V_pages, block_table, kv_len, dst_table, sink: int, recent: int, heavy: int, pos_shift=None,
-             weights_out=None, kv_len_out=None, pos_shift_out=None, workspace=None, stream=None):
+             weights_out=None, kv_len_out=None, pos_shift_out=None, stream=None):
     """Brings every sequence of more than sink + recent + heavy rows down to that many per KV head: the first `sink`, the last
     `recent` and the `heavy` rows of largest accumulated weight between them, copied in order to the pages of dst_table (int32
     [B, pages], none of them a page the sequence has now) - the C entry point `seg_kv_evict`.  Rows are moved as they are: an
@@ -276,12 +276,6 @@ def kv_evict(weights, K_pages, V_pages, block_table, kv_len, dst_table, sink: in
     weights_out = torch.empty_like(weights) if weights_out is None else _flat(weights_out, _F32, (B, Hkv, W), "weights_out", dev)
     kv_len_out = torch.empty_like(kv_len) if kv_len_out is None else _flat(kv_len_out, _I32, (B,), "kv_len_out", dev)
     pos_shift_out = torch.empty_like(kv_len) if pos_shift_out is None else _flat(pos_shift_out, _I32, (B,), "pos_shift_out", dev)
-    L = lib()
-    if workspace is None:
-        workspace = kv_len.new_empty((max(L.seg_kv_evict_workspace_bytes(c), 256),), dtype=torch.uint8)
-    elif workspace.get_device() != dev:
-        raise ValueError("workspace must be on the cache's device")
-    _call(dev, stream, L.seg_kv_evict, "seg_kv_evict", c, weights.data_ptr(), W, sink, recent, heavy, dst_table.data_ptr(), dst_pages,
-          dst_stride, idx.data_ptr(), kv_len_out.data_ptr(), pos_shift_out.data_ptr(), weights_out.data_ptr(), workspace.data_ptr(),
-          workspace.nbytes)
+    _call(dev, stream, lib().seg_kv_evict, "seg_kv_evict", c, weights.data_ptr(), W, sink, recent, heavy, dst_table.data_ptr(), dst_pages,
+          dst_stride, idx.data_ptr(), kv_len_out.data_ptr(), pos_shift_out.data_ptr(), weights_out.data_ptr())
     return idx, kv_len_out, pos_shift_out, weights_out

@@ -59,6 +59,8 @@ DECODE = [
     ([400, 90], 70, [70, 33], 4, 1, 128, 64, 128, 32, [0]),                    # 280 rows to the KV head
     ([300, 41], 40, [40, 0], 8, 2, 64, 16, 100, 20, [1, 2]),
     ([1500, 700, 130], 16, [16, 9, 16], 32, 8, 128, 64, 256, 64, [0, 1, 0, 1, 2, 1, 0, 1]),
+    ([(37 * b) % 211 for b in range(300)], 1, [1 if (37 * b) % 211 and b % 7 else 0 for b in range(300)], 4, 2, 64, 16, 50, 20, [0, 1]),
+    ([(37 * b) % 211 + 9 for b in range(200)], 9, [b % 10 for b in range(200)], 8, 2, 64, 16, 50, 20, [2, 1]),
 ]
 
 
@@ -203,6 +205,22 @@ def test_bad_numbers_are_reported_and_not_followed():
             sa.poll_status()
         second_is_right(O, lse)
     sa.poll_status()
+
+
+def test_a_cache_without_pages_and_a_shared_page():
+    for Lq, fp8 in ((1, False), (2, True), (40, False)):
+        kind = torch.float8_e4m3fn if fp8 else torch.bfloat16
+        K = torch.empty(0, 16, 2, 64, device="cuda").to(kind)
+        s = torch.ones(2, device="cuda") if fp8 else None
+        w = torch.full((3, 2, 4), 7.0, device="cuda")
+        O, lse = sa.seg_attn_decode(rand_q(3, Lq, 4, 64), K, K, torch.empty(3, 0, dtype=torch.int32, device="cuda"),
+                                    torch.zeros(3, dtype=torch.int32, device="cuda"), 64, 16, [0, 1], weights_out=w, k_scale=s, v_scale=s)
+        sa.poll_status()
+        assert not O.any() and (lse == -math.inf).all() and (w == 7.0).all()
+    c = ref.Cache([40, 50], 2, 64, 16, seed=2)      # both read the first sequence's first two pages
+    c.table[1, :2] = c.table[0, :2]
+    c.dev["block_table"] = c.table.cuda()
+    run_decode(c, rand_q(2, 1, 4, 64), 1 << 30, 0, [1, 1])
 
 
 def test_a_captured_step_follows_the_lengths():
