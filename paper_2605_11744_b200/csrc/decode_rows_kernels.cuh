@@ -89,8 +89,9 @@ __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
 // slack only: most tiles leave O alone.  The rows of an MMA do not mix, so that with items of QR = 64 rows the upper half of
 // the lanes computes on whatever is there and nobody reads it; its two warps of each softmax group are not needed (two of
 // them load), and the queries' smaller buffers leave room for six stages instead of four.  What bounds the kernel is the
-// way round of a stage (free, load, S, softmax, O: some 6000 cycles, of which the load's latency is 2400) over the number of
-// stages, not HBM: with four stages 1500 cycles a tile.  Every wait is bounded.
+// tensor pipe with half of its M empty, 1400 cycles a tile where HBM needs as many (4 x 14000 slots, half of the heads with
+// their whole past, 64 rows: 49 us; with the scores issued after the products 52, with four stages 57, one softmax group 97;
+// tiles of 128 slots, whose P has to share S's columns, 60).  Every wait is bounded.
 template <int D, int QR>
 struct RowsShape {
     static constexpr int kStages = D == 64 ? 8 : QR == 64 ? 6 : 4;
