@@ -59,9 +59,10 @@ constexpr int kEvictStatic = 3 * kEvictBins * 4;
 // One cluster of up to eight blocks per (KV head, sequence), each with a contiguous slice of the slots between the sink and
 // the recent rows.  The heavy-th largest key by a radix selection of 11, 11 and 10 bits, the blocks' histograms added up
 // through distributed shared memory; then the kept slots written in ascending order, each warp with a segment of its block's
-// slice, after one scan over the segments' counts.  Bound by the passes over the keys and the barriers between them, not by
-// the one read of the weights: a single block took 95 us for 128 heads of 26K slots, re-reading them and scanning 1024 at a
-// time.
+// slice, after one scan over the segments' counts.  Bound by the instructions of the passes over the keys and the barriers
+// between them, not by the one read of the weights: 33 us for 128 heads of 26K slots.  Keys are taken four at a time once they
+// are in shared memory, and a histogram's warp looks for one common bin over all of its keys at once (19.1M -> 13.8M
+// instructions, 38 -> 33 us); re-reading the weights in every pass and scanning 1024 slots at a time it was 95.
 __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const EvictParams prm) {
     extern __shared__ uint32_t evict_smem[];
     uint32_t* hist = evict_smem;                    // [3][kEvictBins]
@@ -98,7 +99,21 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
     const int slice = ((len + CS - 1) / CS + 31) & ~31, a = min(rank * slice, len), cnt = min(slice, len - a);
     const float* mine = w + m0 + a;
     const bool cached = cnt <= prm.keys;
-    auto key_at = [&](int i) { return cached ? keys[i] : weight_key(mine[i]); };
+    // four keys from index i on (a multiple of four); what lies behind the slice's end counts as no key
+    const int n4 = (cnt + 3) / 4;
+    auto keys_at = [&](int i4, uint32_t (&k)[4]) {
+        if (cached) {
+            const uint4 v = reinterpret_cast<const uint4*>(keys)[i4];
+            k[0] = v.x;
+            k[1] = v.y;
+            k[2] = v.z;
+            k[3] = v.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[e] = 4 * i4 + e < cnt ? weight_key(mine[4 * i4 + e]) : 0u;
+        }
+    };
+    auto there = [&](int i4, int e) { return 4 * i4 + e < cnt; };
     for (int i = tid; i < 3 * kEvictBins; i += kEvictThreads) hist[i] = 0;
     __syncthreads();
     uint32_t prefix = 0, need = prm.heavy;
@@ -106,35 +121,50 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
         uint32_t* mh = hist + pass * kEvictBins;
-        auto count = [&](uint32_t k, bool in) {
-            const uint32_t bin = in ? (k >> shift) & ((1u << bits) - 1) : 0xffffffffu;
-            // a warp whose keys all fall into one bin (zeros that nothing ever looked at) adds them at once
-            if (__all_sync(0xffffffffu, bin == __shfl_sync(0xffffffffu, bin, 0))) {
-                if (lane == 0 && in) atomicAdd(mh + bin, 32u);
-            } else if (in) {
-                atomicAdd(mh + bin, 1u);
+        // N keys of each lane into the histogram.  A warp whose keys all fall into one bin (zeros that nothing ever looked at)
+        // adds them at once.
+        auto count = [&](auto& k, const uint32_t in) {
+            constexpr int N = sizeof(k) / sizeof(k[0]);
+            const uint32_t mask = (1u << bits) - 1, b0 = (k[0] >> shift) & mask;
+            bool same = in == (1u << N) - 1;
+#pragma unroll
+            for (int e = 1; e < N; ++e) same = same && ((k[e] >> shift) & mask) == b0;
+            const uint32_t lead = __shfl_sync(0xffffffffu, b0, 0);  // by every lane, before anything that only some evaluate
+            if (__all_sync(0xffffffffu, same && b0 == lead)) {
+                if (lane == 0) atomicAdd(mh + b0, 32u * N);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if ((in >> e) & 1) atomicAdd(mh + ((k[e] >> shift) & mask), 1u);
             }
         };
-        if (pass == 0 || !cached) {
+        if (pass == 0) {
             for (int i0 = 0; i0 < cnt; i0 += kEvictAhead * kEvictThreads) {
                 float x[kEvictAhead];
 #pragma unroll
                 for (int y = 0; y < kEvictAhead; ++y) x[y] = i0 + y * kEvictThreads + tid < cnt ? mine[i0 + y * kEvictThreads + tid] : 0.f;
+                uint32_t k[kEvictAhead], in = 0;
 #pragma unroll
                 for (int y = 0; y < kEvictAhead; ++y) {
                     const int i = i0 + y * kEvictThreads + tid;
-                    if (i - tid >= cnt) break;
-                    const uint32_t k = weight_key(x[y]);
-                    if (cached && i < cnt) keys[i] = k;
-                    count(k, i < cnt && (pass == 0 || (k >> (shift + bits)) == prefix));
+                    k[y] = weight_key(x[y]);
+                    if (i < cnt) {
+                        in |= 1u << y;
+                        if (cached) keys[i] = k[y];
+                    }
                 }
+                count(k, in);
             }
         } else {
             // few keys share the leading bits found so far: most warps only look
-#pragma unroll 4
-            for (int i = tid; i - tid < cnt; i += kEvictThreads) {
-                const uint32_t k = i < cnt ? keys[i] : 0u;
-                const bool in = i < cnt && (k >> (shift + bits)) == prefix;
+            for (int i = tid; i - tid < n4; i += kEvictThreads) {
+                uint32_t k[4];
+                uint32_t in = 0;
+                if (i < n4) {
+                    keys_at(i, k);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) in |= ((k[e] >> (shift + bits)) == prefix && there(i, e) ? 1u : 0u) << e;
+                }
                 if (__any_sync(0xffffffffu, in)) count(k, in);
             }
         }
@@ -163,7 +193,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
         if (lane == 31) scan[warp] = before;
         before -= c[0] + c[1];
         __syncthreads();
-        for (int k = 0; k < warp; ++k) before += scan[k];
+        before += __reduce_add_sync(0xffffffffu, lane < warp ? scan[lane] : 0u);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             if (need > before && need <= before + c[k]) {
@@ -177,13 +207,16 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
         need = found[1];
     }
     // keys above `prefix` are all kept, of those equal to it the first `need`
-    const int seg = ((cnt + 31) / 32 + 31) & ~31, s0 = min(warp * seg, cnt), s1 = min(s0 + seg, cnt);
+    const int seg = ((n4 + 31) / 32 + 31) & ~31, s0 = min(warp * seg, n4), s1 = min(s0 + seg, n4);  // in fours
     uint32_t gt = 0, eq = 0;
-#pragma unroll 4
     for (int i = s0 + lane; i < s1; i += 32) {
-        const uint32_t k = key_at(i);
-        gt += k > prefix;
-        eq += k == prefix;
+        uint32_t k[4];
+        keys_at(i, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            gt += there(i, e) && k[e] > prefix;
+            eq += there(i, e) && k[e] == prefix;
+        }
     }
     gt = __reduce_add_sync(0xffffffffu, gt);
     eq = __reduce_add_sync(0xffffffffu, eq);
@@ -192,15 +225,9 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
         seg_eq[warp] = eq;
     }
     __syncthreads();
-    uint32_t gt_before = 0, eq_before = 0, gt_all = 0, eq_all = 0;
-    for (int k = 0; k < 32; ++k) {
-        if (k < warp) {
-            gt_before += seg_gt[k];
-            eq_before += seg_eq[k];
-        }
-        gt_all += seg_gt[k];
-        eq_all += seg_eq[k];
-    }
+    uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? seg_gt[lane] : 0u);
+    uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? seg_eq[lane] : 0u);
+    const uint32_t gt_all = __reduce_add_sync(0xffffffffu, seg_gt[lane]), eq_all = __reduce_add_sync(0xffffffffu, seg_eq[lane]);
     if (CS > 1) {
         if (tid == 0) {
             totals[0] = gt_all;
@@ -213,30 +240,52 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
         }
     }
     uint32_t at = prm.sink + gt_before + min(eq_before, need);
-#pragma unroll 2
     for (int i = s0 + lane; i - lane < s1; i += 32) {
-        const uint32_t k = i < s1 ? key_at(i) : 0u;
-        const bool equal = i < s1 && k == prefix;
-        bool keep = i < s1 && k > prefix;
-        const uint32_t be = __ballot_sync(0xffffffffu, equal), below = (1u << lane) - 1;
-        if (be) {
-            keep = keep || (equal && eq_before + __popc(be & below) < need);
-            eq_before += __popc(be);
+        uint32_t k[4], keep = 0, equal = 0;
+        const uint32_t below = (1u << lane) - 1;
+        if (i < s1) {
+            keys_at(i, k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                keep |= (there(i, e) && k[e] > prefix ? 1u : 0u) << e;
+                equal |= (there(i, e) && k[e] == prefix ? 1u : 0u) << e;
+            }
         }
-        const uint32_t bk = __ballot_sync(0xffffffffu, keep);
-        if (keep) {
-            const uint32_t r = at + __popc(bk & below);
-            out[r] = m0 + a + i;
-            w_out[r] = mine[i];
+        if (__any_sync(0xffffffffu, equal)) {
+            // ranks among the equal ones: lane after lane, four slots each
+            uint32_t before = eq_before, total = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t b = __ballot_sync(0xffffffffu, (equal >> e) & 1);
+                before += __popc(b & below);
+                total += __popc(b);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if ((equal >> e) & 1) keep |= (before++ < need ? 1u : 0u) << e;
+            eq_before += total;
         }
-        at += __popc(bk);
+        uint32_t r = at, total = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t b = __ballot_sync(0xffffffffu, (keep >> e) & 1);
+            r += __popc(b & below);
+            total += __popc(b);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if ((keep >> e) & 1) {
+                out[r] = m0 + a + 4 * i + e;
+                w_out[r++] = mine[4 * i + e];
+            }
+        at += total;
     }
     keep_the_rest();
     if (CS > 1) cluster_sync();  // no block leaves while another may still read its shared memory
 }
 
 // Row r of the compacted cache from slot idx[b][h][r]: a thread moves 16 bytes of K and of V for four rows, whose reads are
-// all in flight together (205 -> 180 us for 16 x 8 heads of 8036 rows against one row a thread; 1.05 GB).  Runs after the selection's end; the new
+// all in flight together (205 -> 160 us for 16 x 8 heads of 8036 rows against one row a thread; 1.05 GB).  Runs after the selection's end; the new
 // lengths and shifts are written here and not there because kv_len_out may be kv_len, which the selection's blocks read.
 constexpr int kMoveRows = 4;
 __global__ void __launch_bounds__(256) evict_move_kernel(const EvictParams prm) {
