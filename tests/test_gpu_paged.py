@@ -587,3 +587,77 @@ def test_decode_evict_decode():
     sa.poll_status()
     new = w2[:, :, budget:budget + more].sum((0, 2))
     assert (new > 0).all() and not w2[:, :, budget + more:].any()
+
+
+def test_a_captured_decoding_loop_with_an_eviction():
+    # one graph: a token appended, attended over, weights gathered, the length moved on; another: an eviction into the spare
+    # pages.  Replayed against the same calls made one by one
+    B, Hq, Hkv, d, page, S, T = 2, 8, 2, 128, 16, 32, 8
+    mask, sink, recent, heavy = [0, 1], 1, S + T, 6
+    table = sa.rope_table_scaled(400, 64, kind="linear", factor=2.0)
+    g = torch.Generator().manual_seed(31)
+    steps = [[torch.randn(B, 1, H, d, generator=g).bfloat16().cuda() for H in (Hkv, Hkv, Hq)] for _ in range(14)]
+
+    def make():
+        c = ref.Cache([60, 75], Hkv, d, page, seed=13, spare=12, max_pages=6)
+        c.table[0, 4], c.table[1, 5] = c.spare[10], c.spare[11]      # room for the new rows
+        x = dict(c=c, K=c.K, V=c.V, bt=c.table.clone().cuda(), n=c.dev["kv_len"].clone(), shift=torch.zeros(B, dtype=torch.int32, device="cuda"),
+                 w=torch.zeros(B, Hkv, 110, device="cuda"), w2=torch.zeros(B, Hkv, 110, device="cuda"), k=steps[0][0].clone(), v=steps[0][1].clone(),
+                 q=steps[0][2].clone(), dst=torch.tensor(c.spare[:10], dtype=torch.int32).reshape(B, 5).cuda())
+        x["bt2"] = torch.full((B, 6), -1, dtype=torch.int32, device="cuda")
+        x["bt2"][:, :5] = x["dst"]
+        return x
+
+    def token(x, bt, w, stream=None):
+        x["n"] += 1
+        q = sa.kv_append(x["k"], x["v"], x["K"], x["V"], bt, x["n"], table=table, Q=x["q"], pos_shift=x["shift"], stream=stream)
+        return sa.seg_attn_decode(q, x["K"], x["V"], bt, x["n"], S, T, mask, pos_shift=x["shift"], weights=w, weights_out=w, stream=stream)
+
+    def evict(x, stream=None):
+        return sa.kv_evict(x["w"], x["K"], x["V"], x["bt"], x["n"], x["dst"], sink, recent, heavy, pos_shift=x["shift"], weights_out=x["w2"],
+                           kv_len_out=x["n"], pos_shift_out=x["shift"], stream=stream)
+
+    def feed(x, k):
+        for name, t in zip(("k", "v", "q"), steps[k]):
+            x[name].copy_(t)
+
+    one, rep = make(), make()
+    outs = []
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):                  # the direct calls on a stream of their own, given by name
+        for k in range(14):
+            feed(one, k)
+            if k == 3:
+                idx = evict(one, stream=side)[0]
+            O, lse = token(one, one["bt"] if k < 3 else one["bt2"], one["w"] if k < 3 else one["w2"], stream=side)
+            outs.append((O.clone(), lse.clone()))
+    side.synchronize()
+    start = {n: rep[n].clone() for n in ("n", "shift", "w", "w2")}
+    K0, V0 = rep["K"].clone(), rep["V"].clone()
+    graphs = []
+    for f in (lambda: token(rep, rep["bt"], rep["w"]), lambda: evict(rep), lambda: token(rep, rep["bt2"], rep["w2"])):
+        f()                                        # once outside, then the state put back
+        gr = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(gr):
+            res = f()
+        graphs.append((gr, res))
+    for n, t in start.items():
+        rep[n].copy_(t)
+    rep["K"].copy_(K0)
+    rep["V"].copy_(V0)
+    for k in range(14):
+        feed(rep, k)
+        if k == 3:
+            graphs[1][0].replay()
+            assert torch.equal(graphs[1][1][0], idx)
+        gr, (O, lse) = graphs[0 if k < 3 else 2]
+        gr.replay()
+        assert torch.equal(O, outs[k][0]) and torch.equal(lse, outs[k][1]), k
+    sa.poll_status()
+    for n in ("n", "shift", "w2"):
+        assert torch.equal(one[n], rep[n]), n
+    assert one["n"].tolist() == [sink + recent + heavy + 11] * 2 and not one["w2"][:, :, 96:].any()
+    for b in range(B):
+        assert torch.equal(torch.isnan(one["K"].float()), torch.isnan(rep["K"].float()))
