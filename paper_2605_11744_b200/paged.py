@@ -15,6 +15,7 @@ Lengths stay on the device, so that a decoding step can be captured in a CUDA gr
 """
 from __future__ import annotations
 
+import functools
 import struct
 from typing import Optional
 
@@ -29,9 +30,10 @@ _LAYOUTS = {"half": 0, "interleaved": 1}
 _KINDS = {"plain": 0, "linear": 1, "by_parts": 2}
 _BF16, _E4M3, _I32, _F32 = torch.bfloat16, torch.float8_e4m3fn, torch.int32, torch.float32
 # A decoding step's calls last a few microseconds on the device, so their way there counts: devices are compared by number,
-# structures packed in one go, and the current stream is asked for as torch's own generated code asks for it (a Stream object
-# costs as much as a launch).
+# structures packed in one go, and the current stream and device are asked for as torch's own generated code asks for them (a
+# Stream object costs as much as a launch).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _check(status: int, where: str):
@@ -74,11 +76,23 @@ def _call(dev: int, stream, fn, where: str, *args):
         raise ValueError("the stream belongs to another device than the tensors")
     else:
         stream = stream.cuda_stream
-    if torch.cuda.current_device() == dev:
+    if _current_device() == dev:
         _check(fn(*args, stream), where)
     else:
         with torch.cuda.device(dev):
             _check(fn(*args, stream), where)
+
+
+def _on_stream(f):
+    """`stream=`: the call runs with that stream current, so that what it allocates (results, workspaces) comes from the
+    stream's own memory and is not handed to others while the kernels run."""
+    @functools.wraps(f)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return f(*args, **kw)
+        with torch.cuda.stream(stream):
+            return f(*args, stream=stream, **kw)
+    return call
 
 
 def _mask_bytes(head_past_mask, Hkv: int) -> bytes:
@@ -135,6 +149,7 @@ def _pages(t, B, what: str, dev: int):
     return rows, n, s[0] if rows > 1 else n
 
 
+@_on_stream
 def rope_table_scaled(n_pos: int, rot_dim: int, base: float = 10000.0, kind: str = "plain", factor: float = 1.0,
                       trained_len: float = 0.0, turns_lo: float = 0.0, turns_hi: float = 0.0, amplitude: float = 1.0,
                       device="cuda", stream=None) -> torch.Tensor:
@@ -159,6 +174,7 @@ def _table(table, dev: int):
     return table.shape[0], 2 * table.shape[1]
 
 
+@_on_stream
 def rope_rotate(X, table, positions: Optional[torch.Tensor] = None, pos0: int = 0, layout: str = "half", inverse: bool = False,
                 out: Optional[torch.Tensor] = None, stream=None):
     """Rows of X [B, L, H, d] rotated at `positions` (int32 [B, L]; None: pos0, pos0 + 1, ...) by a table of rope_table or
@@ -171,7 +187,9 @@ def rope_rotate(X, table, positions: Optional[torch.Tensor] = None, pos0: int = 
     xs = _rows4(X, shape, "X", dev)
     if out is None:
         out = torch.empty_like(X)
-    ys = _rows4(out, shape, "out", dev)
+        ys = _STRIDE3.pack(*out.stride()[:3])
+    else:
+        ys = _rows4(out, shape, "out", dev)
     x, y = X.data_ptr(), out.data_ptr()
     if x == y and x and xs != ys:
         raise ValueError("a rotation in place needs the strides of X")
@@ -184,6 +202,7 @@ def rope_rotate(X, table, positions: Optional[torch.Tensor] = None, pos0: int = 
     return out
 
 
+@_on_stream
 def kv_append(K_new, V_new, K_pages, V_pages, block_table, kv_len, table: Optional[torch.Tensor] = None, layout: str = "half",
               Q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, q_len=None, pos_shift=None, k_scale=None,
               v_scale=None, stream=None):
@@ -216,6 +235,7 @@ def kv_append(K_new, V_new, K_pages, V_pages, block_table, kv_len, table: Option
     return q_out
 
 
+@_on_stream
 def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, head_past_mask=None, sm_scale: Optional[float] = None,
                     q_len=None, pos_shift=None, k_scale=None, v_scale=None, weights=None, weights_out=None, out=None, lse=None,
                     workspace: Optional[torch.Tensor] = None, stream=None):
@@ -248,7 +268,7 @@ def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, he
     L = lib()
     if workspace is None:
         need = L.seg_attn_decode_workspace_bytes(c, Lq, Hq, 0 if weights_out is None else 1)
-        workspace = Q.new_empty((max(need, 256),), dtype=torch.uint8)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=Q.device)
     elif workspace.get_device() != dev:
         raise ValueError("workspace must be on the cache's device")
     _call(dev, stream, L.seg_attn_decode, "seg_attn_decode", c, Lq, Hq, S, T, d ** -0.5 if sm_scale is None else sm_scale,
@@ -257,6 +277,7 @@ def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, he
     return out, lse
 
 
+@_on_stream
 def kv_evict(weights, K_pages, V_pages, block_table, kv_len, dst_table, sink: int, recent: int, heavy: int, pos_shift=None,
              weights_out=None, kv_len_out=None, pos_shift_out=None, stream=None):
     """Brings every sequence of more than sink + recent + heavy rows down to that many per KV head: the first `sink`, the last

@@ -257,6 +257,28 @@ def test_a_captured_step_follows_the_lengths():
     sa.poll_status()
 
 
+def test_a_call_on_a_given_stream_allocates_there():
+    # results and workspaces of a call on another stream than the current one must not be handed out on the current one while
+    # its kernels run: many calls on a side stream, their memory freed at once, while the current stream keeps allocating
+    c = ref.Cache([3000, 2000], 2, 128, 64, seed=12)
+    Q = rand_q(2, 1, 16, 128)
+    w = torch.rand(2, 2, c.max_pages * 64, device="cuda")
+    want = sa.seg_attn_decode(Q, c.K, c.V, S=64, T=16, head_past_mask=[1, 1], **c.dev)
+    table = sa.rope_table_scaled(8, 128)
+    turned = sa.rope_rotate(Q, table)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(30):
+        got.append(sa.seg_attn_decode(Q, c.K, c.V, S=64, T=16, head_past_mask=[1, 1], stream=side, **c.dev) + (sa.rope_rotate(Q, table, stream=side),))
+        torch.full((1 << 22,), math.nan, device="cuda")
+    side.synchronize()
+    torch.cuda.synchronize()
+    for O, lse, y in got:
+        assert torch.equal(O, want[0]) and torch.equal(lse, want[1]) and torch.equal(y, turned)
+    sa.poll_status()
+
+
 def test_offsets_past_32_bits():
     # pages 2^31 + elements apart
     page, Hkv, d = 16, 2, 128
