@@ -492,6 +492,7 @@ __global__ void __launch_bounds__(RowsShape<D, QR>::kThreads, 1) decode_rows_ker
         }
     }
     // ---------------- teardown ----------------
+    cp_async_commit();  // the loaders' copies report to barriers: after a failed wait nobody else may have waited for them
     cp_async_wait<0>();
     drain_if_failed();
     tc_fence_before();
