@@ -223,6 +223,22 @@ def test_a_cache_without_pages_and_a_shared_page():
     run_decode(c, rand_q(2, 1, 4, 64), 1 << 30, 0, [1, 1])
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("Lq,Hq,max_pages", [(1, 4, 0), (9, 4, 0), (40, 4, 0), (1, 4, 1), (9, 4, 2), (40, 4, 3)])
+def test_nothing_is_written_behind_the_workspace(Lq, Hq, max_pages, fp8):
+    # the workspace is exactly as long as asked for; a cache without slots has no scores to keep
+    B, Hkv, d, page = 3, 2, 64, 16
+    c = ref.Cache([0] * B if max_pages == 0 else [max_pages * page] * B, Hkv, d, page, fp8=fp8, seed=1)
+    table = c.dev["block_table"][:, :max_pages].contiguous()
+    view = sa.paged._cache(c.K, c.V, table, c.dev["kv_len"], None, None, c.scales.get("k_scale"), c.scales.get("v_scale"))[0]
+    need = sa.lib().seg_attn_decode_workspace_bytes(view, Lq, Hq, 1)
+    buf = torch.full((need + (1 << 16),), 0x5a, dtype=torch.uint8, device="cuda")
+    w = torch.full((B, Hkv, max_pages * page + 4), 7.0, device="cuda")
+    sa.seg_attn_decode(rand_q(B, Lq, Hq, d), c.K, c.V, table, c.dev["kv_len"], 64, 16, [0, 1], weights_out=w, workspace=buf[:need], **c.scales)
+    sa.poll_status()
+    assert (buf[need:] == 0x5a).all() and (w[:, :, max_pages * page:] == 7.0).all()
+
+
 def test_a_captured_step_follows_the_lengths():
     # one decoding step captured, replayed while the lengths, the table and the inputs change; two graphs side by side
     c = ref.Cache([200, 120], 2, 128, 16, seed=9)
