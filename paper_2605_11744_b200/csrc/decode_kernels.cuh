@@ -50,6 +50,7 @@ struct DecodeParams {
     FastDiv f_S, f_g;
     int S, T, W, Hq, g;
     int row_blocks;                  // ceil(g Lq / (rows of an item))
+    int blocks;                      // blocks the workspace has parts for
     int page_whole;                  // page_size is a multiple of 16: a warp's slots lie in one page
     int pitch;                       // slots in a row of scores
     float scale_log2;                // sm_scale * log2(e)
@@ -863,6 +864,11 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
     cp_async_wait<0>();
 }
 
+// Whether an item's first and last block, as found in the workspace, name parts to be added up: not where one block holds all
+// of the item, and not where nobody wrote them (the block that should have may have left after an expired wait; the workspace
+// is scratch memory and can hold anything there).
+__host__ __device__ inline bool parts_to_join(int first, int last, int blocks) { return first >= 0 && first < last && last < blocks; }
+
 // Adds the parts of one row of an item that several blocks share; block.x = the item, block.y = the row, a thread one dim.
 // A row has at most as many parts as the grid has blocks: their bases and sums are read by all threads at once, and the first
 // values of O beside them, so that two dependent reads are all the latency there is.
@@ -874,7 +880,7 @@ __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ 
     after_previous_kernel();
     if (r >= new_rows(p.c, b) * p.g) return;
     const int2 blocks = p.item_blocks[blockIdx.x];
-    if (blocks.x == blocks.y) return;
+    if (!parts_to_join(blocks.x, blocks.y, p.blocks)) return;
     __shared__ float weight[kDecMaxBlocks];
     __shared__ float red[2][D / 32];
     const int n = blocks.y - blocks.x + 1;

@@ -124,6 +124,24 @@ def test_bad_rotations_are_refused():
     assert L.seg_rope_table_scaled(0, 64, sc(), None, None) == 0
 
 
+def test_block_ranges_that_nobody_wrote_are_not_followed(tmp_path):
+    # the join takes an item's first and last block from scratch memory, which after an expired wait holds anything
+    src, exe = tmp_path / "parts.cu", tmp_path / "parts"
+    src.write_text('#include <cstdio>\n#include <climits>\n#include "decode_kernels.cuh"\nint main() {\n'
+                   'const int blocks = 148, v[] = {INT_MIN, -5, -1, 0, 1, 3, 147, 148, 160, 0x5a5a5a5a, INT_MAX};\n'
+                   'for (int a : v) for (int b : v) {\n'
+                   '  const bool parts = 0 <= a && a < blocks && 0 <= b && b < blocks && a < b;\n'
+                   '  if (segattn::parts_to_join(a, b, blocks) != parts) { printf("%d %d\\n", a, b); return 1; }\n'
+                   '}\nstatic_assert(segattn::kDecMaxBlocks >= 160, "room for the weights of every part");\nreturn 0; }\n')
+    csrc = os.path.join(ROOT, "paper_2605_11744_b200", "csrc")
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    subprocess.check_call([nvcc, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", csrc, "-I", os.path.join(ROOT, "include"),
+                           "-o", str(exe), str(src)])
+    assert subprocess.run([str(exe)]).returncode == 0
+    text = open(os.path.join(csrc, "decode_kernels.cuh")).read()
+    assert re.search(r"item_blocks\[blockIdx\.x\];\s*if \(!parts_to_join\(blocks\.x, blocks\.y, p\.blocks\)\) return;", text)
+
+
 def test_nothing_to_do_is_fine_without_a_device():
     assert decode(cache(B=0)) == 0 and append(cache(B=0)) == 0 and evict(cache(B=0)) == 0
     assert decode(cache(), Lq=0) == 0 and append(cache(), Lq=0) == 0
