@@ -345,7 +345,8 @@ segattn_status seg_rope_rotate(int32_t B, int32_t L, int32_t H, int32_t d, int32
  * Everything the kernels read per sequence is in device memory, so a captured graph follows the lengths as they grow.
  * Numbers are checked where they are read: a page number outside [0, n_pages), a length outside [0, max_pages*page_size]
  * or a q_len outside [0, Lq] makes the next seg_attn_poll_status return SEGATTN_ERR_INVALID; such a page's rows are neither
- * read (they count as not visible) nor written, such a length is cut to its range. */
+ * read (they count as not visible) nor written.  Attention and eviction go on with such a length cut to its range (and a
+ * negative pos_shift taken as 0); an append cuts nothing, it leaves out the rows that the numbers give no place. */
 #define SEGATTN_KV_BF16 0
 #define SEGATTN_KV_E4M3 1 /* 8-bit values, 1 + 4 + 3 bits, times a scale per KV head */
 typedef struct {
@@ -367,8 +368,9 @@ typedef struct {
 /* Writes the new rows K_new, V_new (bf16 [B][Lq][Hkv][d]) into the cache.  With `table` (see seg_rope_rotate; rot_dim, layout
  * and n_pos as there) the keys are rotated by their positions first, and so are the queries Q (bf16 [B][Lq][Hq][d], may
  * be NULL; Q_out may be Q) into Q_out; without a table keys are copied and Q must be NULL.  An e4m3 cache stores x times
- * the scale's inverse (both rounded to fp32), rounded to nearest even and saturated at +-448.  Rows t >= q_len[b] are neither read nor written.  A new row
- * whose slot or position is out of range is not written (status as above).  One kernel; B * Lq * (Hq + 2 Hkv) * d at most
+ * the scale's inverse (both rounded to fp32), rounded to nearest even and saturated at +-448.  Rows t >= q_len[b] are neither read nor written.  Not written
+ * either (status as above) are a new row whose slot kv_len[b] - q_len[b] + t lies outside [0, max_pages*page_size) or whose
+ * position is not in the table, and the rows of a sequence whose q_len is out of range or, with a table, whose pos_shift is negative.  One kernel; B * Lq * (Hq + 2 Hkv) * d at most
  * 2^36. */
 segattn_status seg_kv_append(const seg_kv_cache* c, int32_t Lq, const void* K_new, const int64_t kn_stride[3],
                              const void* V_new, const int64_t vn_stride[3], int32_t Hq, const void* Q,

@@ -209,12 +209,16 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams prm) 
             inv[k] = h >= 0 && h < 2 * Hkv ? __frcp_rn(h < Hkv ? prm.k_scale[h] : prm.v_scale[h - Hkv]) : 1.f;
         }
     }
-    const int slot = seq_len(prm.c, b) - rows + t;
-    const long long pos = (long long)slot + shift_of(prm.c, b);
-    if (slot < 0 || (prm.table && pos >= prm.n_pos)) {
+    // From the numbers as they are given: a length or a count of rows cut to its range would move the rows to slots, and
+    // turn them by positions, that are not theirs.
+    const long long at = (long long)prm.c.kv_len[b] - rows + t;
+    const int shift = prm.c.pos_shift ? prm.c.pos_shift[b] : 0;
+    const long long pos = at + shift;
+    if (at < 0 || at >= prm.c.cap || (prm.c.q_len && prm.c.q_len[b] != rows) || (prm.table && (shift < 0 || pos >= prm.n_pos))) {
         if (u == 0 && g == 0) refuse_input(35);
         return;
     }
+    const int slot = (int)at;
     UnitAngles ang;
     const bool turns = prm.table && u * 16 < prm.rot;
     if (turns && h0 < prm.Hq + Hkv) ang.load(prm.table + pos * (prm.rot / 2) + u * 8, 1.f);

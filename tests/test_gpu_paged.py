@@ -432,6 +432,59 @@ def test_append_in_place_and_bad_numbers():
     sa.poll_status()
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("rotated", [False, True])
+def test_append_writes_no_row_in_another_s_place(rotated, fp8):
+    # lengths past the table's capacity, below zero, more new rows than were given, a negative shift: rows without a place are
+    # left out, the others go to their own slots, and every row that was there keeps its bits
+    Hkv, d, page, Lq, pages = 2, 64, 8, 4, 5
+    cap = page * pages
+    g = torch.Generator().manual_seed(8)
+    new = [torch.randn(2, Lq, Hkv, d, generator=g).bfloat16().cuda() for _ in range(2)]
+    table = sa.rope_table_scaled(3 * cap, 32) if rotated else None
+    low, high = -(1 << 31), (1 << 31) - 1
+    for n, q_len, shift in ((cap + 1, None, None), (cap + 3, None, None), (cap + 4, None, None), (cap + 5, 2, None), (high, None, 5), (low, None, None),
+                            (-1, None, None), (3, None, None), (cap, 5, None), (cap - 7, high, None), (20, -1, None), (20, low, None), (cap + 1, 0, None),
+                            (20, None, -3), (20, None, low), (20, 4, 2)):
+        c = ref.Cache([cap, cap], Hkv, d, page, fp8=fp8, seed=3)
+        bits = lambda t: t.view(torch.uint8) if fp8 else t.view(torch.int16)
+        K0, V0 = bits(c.K).clone(), bits(c.V).clone()
+        i32 = lambda x, other: None if x is None else torch.tensor([x, other], dtype=torch.int32, device="cuda")
+        sa.kv_append(new[0], new[1], c.K, c.V, c.dev["block_table"], i32(n, cap), table=table, q_len=i32(q_len, Lq), pos_shift=i32(shift, 0), **c.scales)
+        rows = Lq if q_len is None else q_len
+        valid = 0 <= rows <= Lq and not (rotated and shift is not None and shift < 0)
+        here = [t for t in range(Lq) if valid and t < rows and 0 <= n - rows + t < cap]
+        bad = not valid or (shift is not None and shift < 0) or len(here) < rows
+        if bad and not (shift is not None and shift < 0 and not rotated):
+            with pytest.raises(sa.SegAttnError) as e:
+                sa.poll_status()
+            assert e.value.status == 1
+        elif not bad:
+            sa.poll_status()
+        else:      # a shift that nothing uses may be reported or not
+            try:
+                sa.poll_status()
+            except sa.SegAttnError:
+                pass
+        # what the rows that have a place should be: the same rows appended alone, all numbers in range
+        want = ref.Cache([cap, cap], Hkv, d, page, fp8=fp8, seed=3)
+        for b, ts in ((0, here), (1, list(range(Lq)))):
+            for t in ts:
+                slot = (n - rows + t) if b == 0 else cap - Lq + t
+                one = dict(block_table=want.dev["block_table"][b:b + 1], kv_len=torch.tensor([slot + 1], dtype=torch.int32, device="cuda"))
+                sh = torch.tensor([shift if b == 0 and shift is not None and shift >= 0 else 0], dtype=torch.int32, device="cuda")
+                sa.kv_append(new[0][b:b + 1, t:t + 1], new[1][b:b + 1, t:t + 1], want.K, want.V, table=table, pos_shift=sh, **one, **want.scales)
+        sa.poll_status()
+        assert torch.equal(bits(c.K), bits(want.K)) and torch.equal(bits(c.V), bits(want.V)), (n, q_len, shift)
+        touched = torch.zeros(c.K.shape[0], page, dtype=torch.bool, device="cuda")
+        for b, ts in ((0, here), (1, list(range(Lq)))):
+            for t in ts:
+                slot = (n - rows + t) if b == 0 else cap - Lq + t
+                touched[c.table[b, slot // page].long(), slot % page] = True
+        assert torch.equal(bits(c.K)[~touched], K0[~touched]) and torch.equal(bits(c.V)[~touched], V0[~touched])
+    sa.poll_status()
+
+
 # ---- eviction ---------------------------------------------------------------------------------------------------------
 
 EVICT = [
