@@ -211,19 +211,18 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams prm) 
     }
     // From the numbers as they are given: a length or a count of rows cut to its range would move the rows to slots, and
     // turn them by positions, that are not theirs.
-    const long long at = (long long)prm.c.kv_len[b] - rows + t;
-    const int shift = prm.c.pos_shift ? prm.c.pos_shift[b] : 0;
-    const long long pos = at + shift;
-    if (at < 0 || at >= prm.c.cap || (prm.c.q_len && prm.c.q_len[b] != rows) || (prm.table && (shift < 0 || pos >= prm.n_pos))) {
+    const int n = prm.c.kv_len[b], shift = prm.c.pos_shift ? prm.c.pos_shift[b] : 0;
+    const uint32_t slot = (uint32_t)n - (uint32_t)(rows - t), pos = slot + (uint32_t)shift;
+    if (n < 0 || slot >= (uint32_t)prm.c.cap || (prm.c.q_len && prm.c.q_len[b] != rows) ||
+        (prm.table && (shift < 0 || pos >= (uint32_t)prm.n_pos))) {
         if (u == 0 && g == 0) refuse_input(35);
         return;
     }
-    const int slot = (int)at;
     UnitAngles ang;
     const bool turns = prm.table && u * 16 < prm.rot;
-    if (turns && h0 < prm.Hq + Hkv) ang.load(prm.table + pos * (prm.rot / 2) + u * 8, 1.f);
+    if (turns && h0 < prm.Hq + Hkv) ang.load(prm.table + (long long)pos * (prm.rot / 2) + u * 8, 1.f);
     int prow = 0, page = -1;
-    if (h0 + HPT > prm.Hq) page = page_of(prm.c, b, slot, &prow);
+    if (h0 + HPT > prm.Hq) page = page_of(prm.c, b, (int)slot, &prow);
 #pragma unroll
     for (int k = 0; k < HPT; ++k) {
         const int h = h0 + k;
