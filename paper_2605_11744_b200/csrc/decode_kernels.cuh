@@ -318,8 +318,13 @@ struct DecodeShape {
 };
 
 // A weight of exp2(score - base) may exceed 1 by this power of two before the base is moved up to the row's maximum: most
-// tiles then need no maximum across lanes and no rescaling, and a weight in fp16 or bf16 keeps its relative precision.
+// tiles then need no maximum across lanes and no rescaling.  A weight in bf16 keeps its relative precision wherever it lies.
 constexpr float kDecSlack = 8.f;
+// One in fp16, beside an 8-bit cache, keeps it down to 2^-14 only, and from 2^-25 on it is zero: a base at the maximum would
+// lose the small weights of a long cache that one key dominates (32K slots that share a hundredth of the weight came out wrong
+// by an eighth).  So the base is put 2^13 under the maximum, and moved when a weight would pass 2^15, fp16's largest power:
+// weights are exact to fp16's half step down to 2^-27 of the largest.
+constexpr float kHalfRoom = 13.f, kHalfTop = 15.f;
 
 template <int D, bool FP8, int NT, int WM>
 __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
@@ -642,15 +647,17 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                             // row by row: what one row sees must not move another row's base (and with it its rounding)
                             f[e] = 1.f;
                             if (mx > slack[nt][e]) {
-                                const float moved = base[nt][e] + mx;
+                                const float moved = base[nt][e] + (FP8 ? mx - kHalfRoom : mx);
                                 mx = moved - base[nt][e];  // by what the rounded base has moved: scores and sums follow it
                                 f[e] = slack[nt][e] == -INFINITY ? 0.f : ex2(-mx);
                                 base[nt][e] = moved;
-                                slack[nt][e] = kDecSlack;
+                                slack[nt][e] = FP8 ? kHalfTop : kDecSlack;
+                                // a base past 2^26 is rounded by whole powers of two: what that leaves over fp16's top is cut
+                                auto over_new_base = [&](float x) { return FP8 && x - mx > kHalfTop ? kHalfTop : x - mx; };
 #pragma unroll
                                 for (int k = 0; k < KP; ++k) {
-                                    s[k][nt][e] -= mx;
-                                    s[k][nt][e + 2] -= mx;
+                                    s[k][nt][e] = over_new_base(s[k][nt][e]);
+                                    s[k][nt][e + 2] = over_new_base(s[k][nt][e + 2]);
                                 }
                             }
                             l[nt][e] *= f[e];

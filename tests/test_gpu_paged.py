@@ -150,6 +150,60 @@ def test_large_and_equal_scores():
     run_decode(c, Q, 1 << 30, 0, [1, 1], want_weights=True)
 
 
+@pytest.mark.parametrize("d,Lq,tail", [(64, 1, 0.01), (64, 4, 0.001), (64, 8, 0.01), (64, 16, 0.001), (128, 1, 0.001), (128, 8, 0.001), (128, 16, 0.01),
+                                       (128, 24, 0.001)])
+def test_small_weights_beside_a_dominant_key_keep_their_precision(d, Lq, tail):
+    # 32K slots of an 8-bit cache whose first key takes all but `tail` of the weight and has no value of its own: what comes out
+    # is the small weights' work.  Many sequences over the same pages, so that one block goes through (nearly) a whole sequence.
+    n, B, Hkv, g, page = 32768, 448, 4, 4, 256
+    gen = torch.Generator().manual_seed(d + Lq)
+    k, v = 4 * torch.randn(n // page, page, Hkv, d, generator=gen), 4 * torch.randn(n // page, page, Hkv, d, generator=gen) + 4
+    ks, vs = torch.full((Hkv,), 0.25), torch.full((Hkv,), 0.25)
+    Q = torch.randn(B, Lq, Hkv * g, d, generator=gen)
+    # element 0 is the first key's own: its score is what the others' sum needs to come to `tail`
+    k[..., 0], k[0, 0], v[0, 0] = 0, 0, 0
+    Q[..., 0], k[0, 0, :, 0] = 4.0, (math.log(n / tail) + 0.5) * d ** 0.5
+    K, V = k.to(torch.float8_e4m3fn).cuda(), v.to(torch.float8_e4m3fn).cuda()
+    Q = Q.bfloat16()
+    table = torch.arange(n // page, dtype=torch.int32).expand(B, -1).contiguous()
+    O, lse = sa.seg_attn_decode(Q.cuda(), K, V, table.cuda(), torch.full((B,), n, dtype=torch.int32, device="cuda"), 1 << 30, 0, [1] * Hkv,
+                                k_scale=ks.cuda(), v_scale=vs.cuda())
+    sa.poll_status()
+    some = [0, 1, 223, 447] if Lq == 1 else [5, 300]
+    Or, lr, spread, terms, w = ref.decode(f64(Q[some]), K, V, table[some].numpy(), [n] * len(some), [Lq] * len(some), 1 << 30, 0, [1] * Hkv, d ** -0.5, page,
+                                          k_scale=ks.double().numpy(), v_scale=vs.double().numpy())
+    assert (w[:, :, 0] / (Lq * g) > 1 - 4 * tail).all() and (w[:, :, 0] / (Lq * g) < 1 - tail / 4).all()
+    # as in check_decode, and half a step of an fp16 number below its normal range, 2^-25, where the largest weight is 2^13 at least
+    es = (d + 8) * ref.FP32 * terms + 2.0 ** -18
+    size = (np.abs(ref.rows_of(V, table[0].numpy(), n, page)) * 0.25).sum(0).repeat(g, 0)      # [Hq, d]
+    bound = (ref.FP16 + 2 * es.transpose(0, 2, 1)[..., None]) * spread + 1.02 * ref.BF16 * np.abs(Or) + 2.0 ** -38 * size
+    err = np.abs(f64(O[some]) - Or)
+    assert (err <= bound).all(), float((err / bound).max())
+    assert (np.abs(lse[some].cpu().double().numpy() - lr) <= es + 4 * ref.FP32 * np.abs(lr)).all()
+
+
+@pytest.mark.parametrize("Hq", [4, 16, 64])
+def test_scores_too_large_for_a_fraction(Hq):
+    # scores of 2e9, whose fp32 steps are 128: a base is rounded by more than the slack, and nothing may overflow for it
+    n, d, page = 300, 64, 16
+    c = ref.Cache([n], 1, d, page, fp8=True, seed=2)
+    K = c.K.clone()
+    K.view(torch.uint8)[:] = torch.full((1,), 1.0).to(torch.float8_e4m3fn).view(torch.uint8).item()
+    for j, x in ((7, 448.0), (130, 448.0), (131, 416.0)):
+        K[c.table[0, j // page].long(), j % page] = torch.full((1, d), x, device="cuda").to(torch.float8_e4m3fn)
+    Q = torch.full((1, 1, Hq, d), 65536.0, dtype=torch.bfloat16, device="cuda")
+    s = torch.full((1,), 8.0, device="cuda")
+    O, lse = sa.seg_attn_decode(Q, K, c.V, c.dev["block_table"], c.dev["kv_len"], 1 << 30, 0, [1], k_scale=s, v_scale=s)
+    sa.poll_status()
+    # which of the two equal keys wins is within the scores' rounding; the row is their mean with some weights
+    vals = ref.rows_of(c.V, c.table[0].numpy(), n, page)[[7, 130], 0] * 8.0
+    slack = (2 * ref.FP16 + 1.02 * ref.BF16) * np.abs(vals).max(0)
+    got = f64(O)[0, 0]
+    assert (got >= vals.min(0) - slack).all() and (got <= vals.max(0) + slack).all()
+    top = d * 65536.0 * 448 * 8 * d ** -0.5
+    assert (np.abs(lse.cpu().double().numpy() - top) <= 8 * ref.FP32 * top).all()
+
+
 def test_layouts_and_strides():
     lens = [130, 47]
     c = ref.Cache(lens, 4, 128, 16, seed=4, head_major=True)
