@@ -554,8 +554,8 @@ __global__ void __launch_bounds__(128) decode_row_weights_kernel(const __grid_co
             const int r = r0 + tid, t = (int)fdiv((uint32_t)r, p.f_g);
             const float l = p.LSE[((long long)b * p.Hq + h * p.g + r - t * p.g) * p.c.Lq + t];
             visible_slots(p, n, new_r, shift, t, cls, &lo[tid], &hi[tid]);
-            if (l == -INFINITY) hi[tid] = lo[tid];
-            lse2[tid] = l * 1.4426950408889634f;
+            // a row without a finite score weighs nothing anywhere: exp2(score - inf) is 0 on the path that looks at no mask too
+            lse2[tid] = l == -INFINITY ? INFINITY : l * 1.4426950408889634f;
         }
     };
     bool ok = true;

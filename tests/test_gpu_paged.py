@@ -141,6 +141,35 @@ def test_rows_across_a_segment_border_do_not_feel_what_the_border_hides(Hq, d):
     assert not torch.isfinite(O[:, 0].float()).any()
 
 
+@pytest.mark.parametrize("fp8,Lq", [(False, 2), (False, 8), (False, 16), (False, 32), (False, 48), (True, 2), (True, 16)])
+def test_a_row_whose_scores_are_all_minus_infinity_weighs_nothing(Lq, fp8):
+    # one query head's scores pass fp32's range downwards at every slot: O = 0, LSE = -inf, and the weights are the other rows'
+    n, Hq, d, page, dead = 420, 4, 128, 16, 1
+    c = ref.Cache([n], 1, d, page, fp8=fp8, seed=4)
+    K = c.K.float()
+    K[..., 0] = 100.0 if fp8 else 1.0e4
+    K = K.to(c.K.dtype)
+    Q = rand_q(1, Lq, Hq, d)
+    Q[..., 0] = 0
+    Q[0, Lq // 2, dead, 0] = -2.0e38
+    if fp8:
+        c.scales["k_scale"].fill_(16.0)      # times 100 times 2e38, over the root of 128
+    w = torch.zeros(1, 1, c.max_pages * page, device="cuda")
+    O, lse = sa.seg_attn_decode(Q, K, c.V, S=1 << 30, T=0, head_past_mask=[1], weights_out=w, **c.dev, **c.scales)
+    sa.poll_status()
+    assert not O[0, Lq // 2, dead].any() and lse[0, dead, Lq // 2] == -math.inf
+    assert torch.isfinite(w).all()
+    kw = {} if not fp8 else dict(k_scale=np.array([16.0]), v_scale=c.v_scale.double().numpy())
+    Q[0, Lq // 2, dead] = 0                  # a row of equal weights instead, taken off the reference's sum
+    want = ref.decode(f64(Q), K, c.V, c.table.numpy(), [n], [Lq], 1 << 30, 0, [1], d ** -0.5, page, **kw)
+    e = n - Lq + Lq // 2
+    want_w = want[4][0, 0]
+    want_w[:e + 1] -= 1.0 / (e + 1)
+    es = (d + 8) * ref.FP32 * want[3].max() + 2.0 ** -18
+    assert abs(w.double().sum().item() - (Lq * Hq - 1)) <= 2 * es * Lq * Hq
+    assert (np.abs(w[0, 0].cpu().double().numpy() - want_w) <= 2 * es * want_w + 4 * ref.FP32 * Lq * Hq).all()
+
+
 def test_large_and_equal_scores():
     # scores of +-1e4 (one key wins outright) and keys that are all alike (every weight 1/n)
     c = ref.Cache([300], 2, 128, 16, seed=2)
