@@ -384,6 +384,8 @@ segattn_status seg_kv_append(const seg_kv_cache* c, int32_t Lq, const void* K_ne
  * own-segment heads see what they would have seen without it.)  S = 2^30 makes every head plainly causal.
  *   O bf16 [B][Lq][Hq][d], LSE fp32 contiguous [B][Hq][Lq] as in seg_attn_fwd; rows t >= q_len[b] are left as they were; a
  *   row that sees no key gets O = 0, LSE = -inf.  A row's result does not depend on rows it does not see, whatever they hold.
+ *   O may be Q, with its strides (a view that shares some of its elements is SEGATTN_ERR_INVALID); not with weights_out and
+ *   more than 32 rows to a KV head (Hq/Hkv * Lq) of a bf16 cache, whose weights read Q once more (SEGATTN_ERR_INVALID).
  *   weights_out (NULL: none): fp32 contiguous [B][Hkv][W]; for every slot j < kv_len[b] of sequences with new rows
  *     weights_out[b][h][j] = (weights_in ? weights_in[b][h][j] : 0) + sum over the new rows and the query heads of h of the
  *     row's attention weight on j;

@@ -2,6 +2,7 @@
 // the host side of the mask scheduler, and kernel launches.  Built as one translation unit.
 #include "seg_attn.h"
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdio>

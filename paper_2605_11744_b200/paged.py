@@ -243,7 +243,8 @@ def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, he
     point `seg_attn_decode`: row t of sequence b stands at slot kv_len - q_len + t and sees what seg_attn_fwd would show it
     (segments of S, tail T, one head class per KV head).  weights_out [B, Hkv, W] fp32, W >= max_pages * page_size, takes
     every slot's attention weight summed over the rows and query heads of its KV head, added to `weights` if given (which may
-    be the same tensor).  Rows from q_len on, in O and in LSE, are left as they were."""
+    be the same tensor).  Rows from q_len on, in O and in LSE, are left as they were.
+    `out` may be Q, except with weights_out and more than 32 rows to a KV head (Hq/Hkv * Lq) of a bf16 cache."""
     c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, q_len, pos_shift, k_scale, v_scale)
     if Q.dim() != 4:
         raise ValueError("Q must be [B, Lq, Hq, d]")

@@ -233,6 +233,37 @@ def test_scores_too_large_for_a_fraction(Hq):
     assert (np.abs(lse.cpu().double().numpy() - top) <= 8 * ref.FP32 * top).all()
 
 
+@pytest.mark.parametrize("Lq,Hq,d,fp8", [(1, 8, 128, False), (4, 8, 64, False), (8, 8, 128, False), (16, 8, 128, False), (40, 8, 64, False),
+                                         (1, 8, 64, True), (16, 8, 128, True), (40, 8, 64, True)])
+def test_outputs_in_the_queries_place(Lq, Hq, d, fp8):
+    # out may be Q; not where the gathered weights of many rows read Q again; never where a view shares some of its elements
+    c = ref.Cache([900, 300], 2, d, 16, fp8=fp8, seed=9)
+    Q = rand_q(2, Lq, Hq, d, pad_heads=1)
+    many = Lq * Hq // 2 > 32 and not fp8
+    call = lambda q, **kw: sa.seg_attn_decode(q, c.K, c.V, S=64, T=16, head_past_mask=[0, 1], **c.dev, **c.scales, **kw)
+    for with_w in (False, True):
+        w = [torch.zeros(2, 2, c.max_pages * 16, device="cuda") if with_w else None for _ in range(2)]
+        O, lse = call(Q, weights_out=w[0])
+        q = torch.cat([Q, Q.new_full((2, Lq, 1, d), 7.0)], 2)
+        kept = q.clone()
+        if many and with_w:
+            with pytest.raises(sa.SegAttnError) as e:
+                call(q[:, :, :Hq], out=q[:, :, :Hq], weights_out=w[1])
+            assert e.value.status == 1 and torch.equal(q, kept) and not w[1].any()
+            continue
+        O2, l2 = call(q[:, :, :Hq], out=q[:, :, :Hq], weights_out=w[1])
+        assert torch.equal(O, O2) and torch.equal(lse, l2) and (q[:, :, Hq] == 7.0).all()
+        assert w[0] is None or torch.equal(w[0], w[1])
+    q = torch.cat([Q, Q], 2)
+    for out in (q[:, :, 1:Hq + 1], q[:, :, Hq - 1:2 * Hq - 1]):
+        with pytest.raises(sa.SegAttnError):
+            call(q[:, :, :Hq], out=out)
+    O, lse = call(Q)
+    O2, l2 = call(q[:, :, :Hq], out=q[:, :, Hq:])       # the other half of the same buffer
+    assert O2.data_ptr() == q[:, :, Hq:].data_ptr() and torch.equal(O, O2) and torch.equal(lse, l2) and torch.equal(q[:, :, :Hq], Q)
+    sa.poll_status()
+
+
 def test_layouts_and_strides():
     lens = [130, 47]
     c = ref.Cache(lens, 4, 128, 16, seed=4, head_major=True)

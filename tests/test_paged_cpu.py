@@ -84,6 +84,53 @@ def test_bad_decode_calls_are_refused(bad):
     assert decode(cache(), **bad) == 1
 
 
+def units(at, strides, shape, d):
+    # the 16-byte pieces that a tensor of 16-bit elements covers
+    rows = [at // 16 + (i * strides[0] + j * strides[1] + k * strides[2]) // 8 for i in range(shape[0]) for j in range(shape[1]) for k in range(shape[2])]
+    return {r + x for r in rows for x in range(d // 8)}
+
+
+def test_outputs_that_share_elements_with_the_queries_are_refused():
+    # Without a workspace a call that passes comes to 5 before it touches a device.  Against the sets of elements themselves:
+    # nested strides, permuted ones, expanded ones, interleaved views, unequal strides
+    rng = np.random.default_rng(5)
+    seen = [0, 0]
+    for trial in range(1500):
+        B, Lq, Hq, d = int(rng.integers(1, 4)), int(rng.integers(1, 5)), 2 * int(rng.integers(1, 4)), 64
+        kind = trial % 5
+        order = rng.permutation(3)
+        def nest(gap):
+            s, size = [0, 0, 0], d
+            for i in order:
+                s[i] = size + 8 * int(rng.integers(0, gap + 1))
+                size = s[i] * (B, Lq, Hq)[i]
+            return s
+        qs = nest(12)
+        os_ = list(qs) if kind < 3 else nest(12)
+        if kind == 2:
+            qs[int(rng.integers(0, 3))] = 0
+        if kind == 4:
+            qs, os_ = [8 * int(x) for x in rng.integers(0, 60, 3)], [8 * int(x) for x in rng.integers(0, 60, 3)]
+        span = sum(s * (n - 1) for s, n in zip(qs, (B, Lq, Hq))) + d
+        at = OK + 2 * 8 * int(rng.integers(-span // 8 - 2, span // 8 + 3))
+        pack = lambda s: paged._STRIDE3.pack(*s)
+        got = decode(cache(B=B, d=d), Lq=Lq, Hq=Hq, Q=OK, qs=pack(qs), O=at, os_=pack(os_), ws=None)
+        same = at == OK and all(n == 1 or a == b for a, b, n in zip(qs, os_, (B, Lq, Hq)))
+        shared = bool(units(OK, qs, (B, Lq, Hq), d) & units(at, os_, (B, Lq, Hq), d))
+        assert got == (1 if shared and not same else 5), (trial, qs, os_, at - OK, (B, Lq, Hq))
+        seen[shared] += 1
+    assert min(seen) > 100      # both answers were asked for
+    # queries and outputs side by side in one buffer, large; a row more would meet
+    big = dict(Lq=4096, Hq=64, qs=paged._STRIDE3.pack(4096 * 128 * 128, 128 * 128, 128), os_=paged._STRIDE3.pack(4096 * 128 * 128, 128 * 128, 128), ws=None)
+    assert decode(cache(), O=OK + 2 * 64 * 128, **big) == 5 and decode(cache(), O=OK + 2 * 63 * 128, **big) == 1
+    # the same view, unless the weights of many rows read the queries again (a bf16 cache, from 33 rows to a KV head on)
+    for Lq, kw, want in ((1, {}, 5), (8, dict(wout=OK << 8, W=128), 5), (16, {}, 5), (16, dict(wout=OK << 8, W=128), 5), (17, {}, 5),
+                         (17, dict(wout=OK << 8, W=128), 1)):
+        assert decode(cache(), Lq=Lq, Hq=4, ws=None, **kw) == want, (Lq, kw)
+    eight = cache(dtype=1, k_scale=OK, v_scale=OK)
+    assert decode(eight, Lq=17, Hq=4, ws=None, wout=OK << 8, W=128) == 5
+
+
 def test_missing_workspaces_are_refused():
     for kw in (dict(ws=None), dict(ws=OK + 16), dict(ws_bytes=16)):
         assert decode(cache(), **kw) == 5
