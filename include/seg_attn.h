@@ -41,9 +41,10 @@
  *     and the streamed prefill several launches and copies): what was enqueued before it still
  *     runs, so treat the outputs, and for the streamed prefill the handle's state, as undefined.
  *   - The kernels share one device status word per process (see seg_attn_poll_status).  Once a
- *     kernel has set it - a bounded wait that ran out, an index a kernel refused - later kernels
- *     give up their waits early too, so outputs enqueued after that are undefined until
- *     seg_attn_poll_status has been called, which reads and clears the word.
+ *     bounded wait has run out, later kernels give up their waits early too, so outputs enqueued
+ *     after that are undefined until seg_attn_poll_status has been called, which reads and clears
+ *     the word.  An input that a kernel refused (an index or a length out of range) is recorded
+ *     there as well, unless a wait has run out, and touches no other kernel.
  *   - Base pointers must be 16-byte aligned and every stride a multiple of 8 elements
  *     (tiles are moved by TMA).  d is 64 or 128.  0 <= T <= S.  Any Lq, kv_len >= 0.
  *   - Arithmetic: bf16 inputs, fp32 accumulation on the tensor cores, fp32 softmax
@@ -434,8 +435,9 @@ segattn_status seg_attn_step_host(const seg_attn_params* p, const void* Q_host, 
 
 /* ---- Status and accounting */
 /* Synchronises `stream`, then reads and clears the device status word that kernels set when a
- * bounded wait expires or a kernel refuses its input.  Returns SEGATTN_OK, SEGATTN_ERR_TIMEOUT,
- * SEGATTN_ERR_INVALID (an index out of range in seg_attn_gather_context) or SEGATTN_ERR_CUDA. */
+ * bounded wait expires or a kernel refuses its input.  Returns SEGATTN_OK, SEGATTN_ERR_TIMEOUT (also
+ * where an input was refused besides), SEGATTN_ERR_INVALID (an index, position, page or length out of range
+ * where a kernel read it) or SEGATTN_ERR_CUDA. */
 segattn_status seg_attn_poll_status(void* stream);
 const char* seg_attn_status_string(segattn_status s);
 /* Last CUDA error code (cudaError_t or CUresult as int) recorded by this thread's failing call. */

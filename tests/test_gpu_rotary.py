@@ -99,6 +99,38 @@ def test_a_position_out_of_the_table_is_reported():
     sa.poll_status()
 
 
+def test_a_refused_input_does_not_end_the_waits_of_other_kernels():
+    # until it is polled, a refused position stays in the status word that all kernels share: a wait goes on to its own limit all
+    # the same (1 ms here), and what that reports is the graver of the two; after the poll the word is clear
+    X = torch.ones(1, 4, 2, 64, dtype=torch.bfloat16, device="cuda")
+    table = sa.rope_table_scaled(10, 32)
+    bad = torch.tensor([[0, 10, -1, 9]], dtype=torch.int32, device="cuda")
+    sa.rope_rotate(X, table, positions=bad)
+    sa.selftest_wait_timeout()
+    with pytest.raises(sa.SegAttnError) as e:
+        sa.poll_status()
+    assert e.value.status == 4
+    sa.poll_status()
+    sa.selftest_wait_timeout()          # the other way round
+    sa.rope_rotate(X, table, positions=bad)
+    with pytest.raises(sa.SegAttnError) as e:
+        sa.poll_status()
+    assert e.value.status == 4
+    # a training step with a refused input outstanding is the step it would have been
+    from util import rand_inputs
+    Q, K, V, dO = rand_inputs(1, 1500, 4, 2, 128, seed=4)
+    O, lse = sa.seg_attn_fwd(Q, K, V, 256, 64, [0, 1])
+    want = (O, lse) + tuple(sa.seg_attn_bwd(Q, K, V, O, lse, dO, 256, 64, [0, 1]))
+    sa.poll_status()
+    sa.rope_rotate(X, table, positions=bad)
+    O, lse = sa.seg_attn_fwd(Q, K, V, 256, 64, [0, 1])
+    got = (O, lse) + tuple(sa.seg_attn_bwd(Q, K, V, O, lse, dO, 256, 64, [0, 1]))
+    with pytest.raises(sa.SegAttnError) as e:
+        sa.poll_status()
+    assert e.value.status == 1
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_agrees_with_the_half_rotation_of_the_framework():
     X = torch.randn(2, 100, 4, 128, generator=torch.Generator().manual_seed(0)).bfloat16().cuda()
     table = sa.rope_table(200, 128)
