@@ -319,7 +319,8 @@ segattn_status seg_attn_gather_context_rope(int32_t B, int32_t Hkv, int32_t d, i
  *                          again): the backward pass, which takes dY to dX.  fp32 arithmetic with separately rounded
  *                          products, one rounding to bf16.  A position outside [0, n_pos) is not looked up: its row comes
  *                          out zero and the next seg_attn_poll_status returns SEGATTN_ERR_INVALID.
- * d and rot_dim are multiples of 16, 16 <= rot_dim <= d <= 256, n_pos <= 2^24, and B * L * H * d at most 2^36. */
+ * d and rot_dim are multiples of 16, 16 <= rot_dim <= d <= 256, n_pos <= 2^24, B * L below 2^31, and
+ * B * L * H * d at most 2^35. */
 #define SEGATTN_ROPE_PLAIN 0
 #define SEGATTN_ROPE_LINEAR 1
 #define SEGATTN_ROPE_BY_PARTS 2
@@ -371,8 +372,8 @@ typedef struct {
  * be NULL; Q_out may be Q) into Q_out; without a table keys are copied and Q must be NULL.  An e4m3 cache stores x times
  * the scale's inverse (both rounded to fp32), rounded to nearest even and saturated at +-448.  Rows t >= q_len[b] are neither read nor written.  Not written
  * either (status as above) are a new row whose slot kv_len[b] - q_len[b] + t lies outside [0, max_pages*page_size) or whose
- * position is not in the table, and the rows of a sequence whose q_len is out of range or, with a table, whose pos_shift is negative.  One kernel; B * Lq * (Hq + 2 Hkv) * d at most
- * 2^36. */
+ * position is not in the table, and the rows of a sequence whose q_len is out of range or, with a table, whose pos_shift is negative.  One kernel;
+ * B * Lq below 2^31, and B * Lq * (Hq + 2 Hkv) * d at most 2^35. */
 segattn_status seg_kv_append(const seg_kv_cache* c, int32_t Lq, const void* K_new, const int64_t kn_stride[3],
                              const void* V_new, const int64_t vn_stride[3], int32_t Hq, const void* Q,
                              const int64_t q_stride[3], void* Q_out, const int64_t qo_stride[3], const float* table,

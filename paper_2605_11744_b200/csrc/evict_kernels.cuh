@@ -70,8 +70,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const Evict
     __shared__ uint32_t scan[32], seg_gt[32], seg_eq[32], found[2], totals[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int CS = (int)cluster_size(), rank = (int)cluster_rank(), unit = blockIdx.x / CS;
-    const int h = unit % prm.c.Hkv, b = unit / prm.c.Hkv;
-    (void)h;
+    const int b = unit / prm.c.Hkv;
     const int n = seq_len(prm.c, b);
     const float* w = prm.weights + (long long)unit * prm.W;
     float* w_out = prm.weights_out + (long long)unit * prm.W;

@@ -189,6 +189,15 @@ def test_block_ranges_that_nobody_wrote_are_not_followed(tmp_path):
     assert re.search(r"item_blocks\[blockIdx\.x\];\s*if \(!parts_to_join\(blocks\.x, blocks\.y, p\.blocks\)\) return;", text)
 
 
+def test_rotations_and_appends_past_the_limits_are_refused():
+    big = 0x7fffffff
+    for B, n, H in ((1 << 16, 1 << 15, 1), (big, big, 1), (big, big, big), (1, 1, big), (1, 1 << 20, 1 << 14), (2, 1 << 24, 511)):
+        assert sa.lib().seg_rope_rotate(B, n, H, 128, 128, 0, OK, ST, OK, ST, OK, 0, 0, OK, 10, None) == 1, (B, n, H)
+    for B, Lq, Hq in ((1 << 15, 1 << 16, 0), (65535, big, 0), (1, 1 << 20, 1 << 14), (1, big, big)):
+        kw = dict(Hq=Hq, Q=OK, qs=ST, qo=OK, qos=ST, table=OK, n_pos=10, rot=64) if Hq else {}
+        assert append(cache(B=B), Lq=Lq, **kw) == 1, (B, Lq, Hq)
+
+
 def test_nothing_to_do_is_fine_without_a_device():
     assert decode(cache(B=0)) == 0 and append(cache(B=0)) == 0 and evict(cache(B=0)) == 0
     assert decode(cache(), Lq=0) == 0 and append(cache(), Lq=0) == 0
