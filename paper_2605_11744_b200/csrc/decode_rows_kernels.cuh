@@ -88,10 +88,12 @@ __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
 // TMEM (512 columns): S at 0 and 64, P at 128 and 160, O at 192 and 320.  A row's base moves as in decode_kernel, past a
 // slack only: most tiles leave O alone.  The rows of an MMA do not mix, so that with items of QR = 64 rows the upper half of
 // the lanes computes on whatever is there and nobody reads it; its two warps of each softmax group are not needed (two of
-// them load), and the queries' smaller buffers leave room for six stages instead of four.  What bounds the kernel is the
-// tensor pipe with half of its M empty, 1400 cycles a tile where HBM needs as many (4 x 14000 slots, half of the heads with
-// their whole past, 64 rows: 49 us; with the scores issued after the products 52, with four stages 57, one softmax group 97;
-// tiles of 128 slots, whose P has to share S's columns, 60).  Every wait is bounded.
+// them load), and the queries' smaller buffers leave room for six stages instead of four.  4 x 14000 slots, half of the heads with
+// their whole past, 64 rows: 49 us, 2900 cycles for each of a block's 31 tiles, of which the twelve products take some 770.  No
+// part of the SM is full (DRAM 33%, tensor pipe 22%, issue slots 23%): a tile goes from scores through softmax and weights to its
+// product in one dependent chain, and two tiles, one to a group, are on their way at a time.  With the scores issued after the
+// products it took 52 us, with four stages 57, with one softmax group 97, with tiles of 128 slots, whose P has to share S's columns,
+// 60.  Every wait is bounded.
 template <int D, int QR>
 struct RowsShape {
     static constexpr int kStages = D == 64 ? 8 : QR == 64 ? 6 : 4;
