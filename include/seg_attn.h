@@ -396,7 +396,7 @@ segattn_status seg_kv_append(const seg_kv_cache* c, int32_t Lq, const void* K_ne
  * `workspace`: DEVICE, 256-byte aligned, seg_attn_decode_workspace_bytes(...) bytes, scratch (0 = invalid parameters); calls
  * that may run at the same time, captured ones too, need one each.  Results do not change from run to run.
  * fp32 scores, statistics and accumulators; the weights are rounded to 16 bits before the product with V (bf16, or fp16
- * beside an e4m3 cache). */
+ * beside an e4m3 cache: half a step, 2^-11, down to 2^-27 of the row's largest weight, and 2^-38 of that one below). */
 size_t seg_attn_decode_workspace_bytes(const seg_kv_cache* c, int32_t Lq, int32_t Hq, int32_t with_weights);
 segattn_status seg_attn_decode(const seg_kv_cache* c, int32_t Lq, int32_t Hq, int32_t S, int32_t T, float sm_scale,
                                const uint8_t* head_past_mask, const void* Q, const int64_t q_stride[3], void* O,
