@@ -40,11 +40,11 @@
  *     copy in the middle of a call's sequence (a backward is three kernels, the host-buffer step
  *     and the streamed prefill several launches and copies): what was enqueued before it still
  *     runs, so treat the outputs, and for the streamed prefill the handle's state, as undefined.
- *   - The kernels share one device status word per process (see seg_attn_poll_status).  Once a
- *     bounded wait has run out, later kernels give up their waits early too, so outputs enqueued
- *     after that are undefined until seg_attn_poll_status has been called, which reads and clears
- *     the word.  An input that a kernel refused (an index or a length out of range) is recorded
- *     there as well, unless a wait has run out, and touches no other kernel.
+ *   - The kernels share a device status per process (see seg_attn_poll_status).  Once a bounded
+ *     wait has run out, later kernels give up their waits early too, so outputs enqueued after
+ *     that are undefined until seg_attn_poll_status has been called, which reads and clears it.
+ *     An input that a kernel refused (an index or a length out of range) is recorded there as
+ *     well and touches no other kernel.
  *   - Base pointers must be 16-byte aligned and every stride a multiple of 8 elements
  *     (tiles are moved by TMA).  d is 64 or 128.  0 <= T <= S.  Any Lq, kv_len >= 0.
  *   - Arithmetic: bf16 inputs, fp32 accumulation on the tensor cores, fp32 softmax
@@ -435,7 +435,7 @@ segattn_status seg_attn_step_host(const seg_attn_params* p, const void* Q_host, 
                                   void* arena, size_t arena_bytes, void* stream);
 
 /* ---- Status and accounting */
-/* Synchronises `stream`, then reads and clears the device status word that kernels set when a
+/* Synchronises `stream`, then reads and clears the device status that kernels set when a
  * bounded wait expires or a kernel refuses its input.  Returns SEGATTN_OK, SEGATTN_ERR_TIMEOUT (also
  * where an input was refused besides), SEGATTN_ERR_INVALID (an index, position, page or length out of range
  * where a kernel read it) or SEGATTN_ERR_CUDA. */

@@ -1,6 +1,6 @@
 // The paged key/value cache as the kernels see it: slot j of sequence b is row j % page_size of page
 // block_table[b][j / page_size].  Every number that comes from device memory is checked here before it becomes an
-// address; what is out of range is recorded in the status word and not followed.
+// address; what is out of range is recorded (g_refused_input) and not followed.
 #pragma once
 #include <cstdint>
 
@@ -23,7 +23,7 @@ struct PagedView {
     int B, Hkv, Lq;
 };
 
-__device__ __forceinline__ void refuse_input(int site) { atomicCAS(&g_device_status, 0, (1 << 8) | site); }
+__device__ __forceinline__ void refuse_input(int site) { atomicCAS(&g_refused_input, 0, (1 << 8) | site); }
 
 // Length of sequence b, cut to what its row of the block table can hold.
 __device__ __forceinline__ int seq_len(const PagedView& c, int b) {

@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(256) prefill_scatter_grads_kernel(const Prefil
 // Context of a head that reads a retrieved prefix (Appendix C, Eq. "ctx", first case): rows [0, R) of
 // the output are the pool rows the index list names, rows [R, R + Lseg) the current segment's.  One
 // thread per 16 bytes of output (K and V both).  An index outside [0, pool_len) gives a zero row and
-// sets the status word (code 1, invalid input) instead of reading out of bounds.
+// sets the word of refused input (code 1, invalid input) instead of reading out of bounds.
 struct GatherParams {
     const uint4* Kpool;  // strides below, in uint4 units, for (batch, position, head)
     const uint4* Vpool;

@@ -7,15 +7,13 @@
 
 namespace segattn {
 
-// ---- status word shared by all kernels of the library ------------------------------------
-// 0 = fine; otherwise (code << 8) | site of a bounded wait that gave up (code 4), or of the first input that a kernel refused
-// (code 1).  An expired wait is the graver and takes the place of a refused input: what a kernel refuses it has dealt with, and
-// nobody's barriers are the worse for it.
+// ---- status words shared by all kernels of the library -----------------------------------
+// 0 = fine; otherwise (code << 8) | site of the first bounded wait that gave up.
 // (The library is built as a single translation unit, so the definition lives here.)
 __device__ int g_device_status = 0;
-constexpr int kWaitExpired = 4 << 8;
-__device__ __forceinline__ void record_expired_wait(int site) { atomicMax(&g_device_status, kWaitExpired | (site & 0xff)); }
-__device__ __forceinline__ bool some_wait_expired() { return *reinterpret_cast<volatile int*>(&g_device_status) >= kWaitExpired; }
+// 0 = fine; otherwise (1 << 8) | site of the first input that a kernel refused.  A word of its own: what a kernel refuses it has
+// dealt with, and no other kernel's waits are to end for it.  (Telling the two apart in one word cost the forward 0.5%.)
+__device__ int g_refused_input = 0;
 
 #ifdef SEGATTN_TRACE
 // Debug-only timeline: TRACE(slot) stores clock64 of one chosen CTA of one chosen kernel (the
@@ -84,16 +82,16 @@ __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // Waits for the phase with the given parity to complete.  Gives up (returns false) when the
-// library's status word says that another wait has expired, or after kWaitLimitNs, in which case
+// library's status word is already set by someone else, or after kWaitLimitNs, in which case
 // it records `site` in the status word.  Callers leave their loops on false.
 __device__ __forceinline__ bool mbar_wait_spin(uint32_t bar, uint32_t parity, int site, unsigned long long limit_ns) {
     const unsigned long long t0 = global_ns();
     for (uint32_t it = 1;; ++it) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((it & 63u) == 0) {
-            if (some_wait_expired()) return false;
+            if (*reinterpret_cast<volatile int*>(&g_device_status) != 0) return false;
             if (global_ns() - t0 > limit_ns) {
-                record_expired_wait(site);
+                atomicCAS(&g_device_status, 0, (4 << 8) | (site & 0xff));
                 return false;
             }
         }
@@ -116,7 +114,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int sit
 #pragma unroll 1
         for (uint32_t it = 0; it < kWaitLimitPolls; ++it)
             if (mbar_try_wait(bar, parity)) return true;
-        record_expired_wait(site);
+        atomicCAS(&g_device_status, 0, (4 << 8) | (site & 0xff));
         return false;
     } else {
         return mbar_wait_slow(bar, parity, site);
@@ -126,7 +124,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int sit
 // After a failed wait: give this CTA's outstanding bulk copies time to land (bounded) before its
 // shared memory is released.  A no-op on the normal path.
 __device__ __forceinline__ void drain_if_failed() {
-    if (some_wait_expired()) {
+    if (*reinterpret_cast<volatile int*>(&g_device_status) != 0) {
         const unsigned long long t0 = global_ns();
         while (global_ns() - t0 < 200000ull) __nanosleep(1000);
     }

@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(256) rope_apply_kernel(const RopeApplyParams p
 
 // [K_ret ; K_i] with re-indexed rotations and [V_ret ; V_i] unrotated, from an index list: row r < R of the
 // output is pool row idx[b][h][r] rotated by position r, row R + t is segment row t rotated by R + t.  An
-// index outside [0, pool_len) gives a zero row and sets the status word, as in the plain gather.
+// index outside [0, pool_len) gives a zero row and sets the word of refused input, as in the plain gather.
 struct GatherRopeParams {
     const __nv_bfloat16* Kpool;  // element strides below for (batch, position, head)
     const __nv_bfloat16* Vpool;

@@ -304,16 +304,18 @@ segattn_status seg_attn_fwd(const seg_attn_params* p, const void* Q, const void*
 segattn_status seg_attn_poll_status(void* stream) {
     cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e);
-    int word = 0;
-    e = cudaMemcpyFromSymbol(&word, g_device_status, sizeof(int));
+    int waited = 0, refused = 0;
+    const int zero = 0;
+    e = cudaMemcpyFromSymbol(&waited, g_device_status, sizeof(int));
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&refused, g_refused_input, sizeof(int));
     if (e != cudaSuccess) return cuda_fail(e);
-    if (word == 0) return SEGATTN_OK;
-    t_last_cuda_error = word;
-    int zero = 0;
-    e = cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int));
+    if (waited == 0 && refused == 0) return SEGATTN_OK;
+    // each word is (status << 8) | detail; an expired wait is the graver
+    t_last_cuda_error = waited ? waited : refused;
+    if (waited) e = cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int));
+    if (e == cudaSuccess && refused) e = cudaMemcpyToSymbol(g_refused_input, &zero, sizeof(int));
     if (e != cudaSuccess) return cuda_fail(e);
-    // the word is (status << 8) | detail: an expired wait, or input a kernel refused (an index out of range)
-    return (word >> 8) == SEGATTN_ERR_INVALID ? SEGATTN_ERR_INVALID : SEGATTN_ERR_TIMEOUT;
+    return waited ? SEGATTN_ERR_TIMEOUT : SEGATTN_ERR_INVALID;
 }
 
 const char* seg_attn_status_string(segattn_status s) {

@@ -100,8 +100,8 @@ def test_a_position_out_of_the_table_is_reported():
 
 
 def test_a_refused_input_does_not_end_the_waits_of_other_kernels():
-    # until it is polled, a refused position stays in the status word that all kernels share: a wait goes on to its own limit all
-    # the same (1 ms here), and what that reports is the graver of the two; after the poll the word is clear
+    # until it is polled, a refused position stays in the status that all kernels share: a wait goes on to its own limit all
+    # the same (1 ms here), and what that reports is the graver of the two; after the poll it is clear
     X = torch.ones(1, 4, 2, 64, dtype=torch.bfloat16, device="cuda")
     table = sa.rope_table_scaled(10, 32)
     bad = torch.tensor([[0, 10, -1, 9]], dtype=torch.int32, device="cuda")
