@@ -417,6 +417,94 @@ segattn_status seg_kv_evict(const seg_kv_cache* c, const float* weights, int32_t
                             int32_t heavy, const int32_t* dst_table, int32_t dst_max_pages, int32_t dst_stride, int32_t* idx,
                             int32_t* kv_len_out, int32_t* pos_shift_out, float* weights_out, void* stream);
 
+/* ---- Pages from the lengths that requests ask for, on the device: so that a decoding loop admits, grows, rolls back and ends its
+ * sequences without the host.  want (DEVICE int32 [B]) is the length every sequence is to have; with n = kv_len[b] and pages of
+ * page_size rows, a sequence that shrinks (0: it is done) gives the pages behind its new length back to the list free_pages (DEVICE
+ * int32 [n_pages], the first *free_count of them free), and one that grows takes pages from the list's end, after all that is given
+ * back, in the order of b: the first that does not find enough of them, and every later one that needs any, stays as it is (what it
+ * already has included), to be asked for again.  A page on the list and in a table belongs to one sequence: pages that sequences
+ * share are not given back by a call of this kind.
+ *   block_table     [B][max_pages], row stride table_stride: new entries are written, others are left as they were
+ *   kv_len_out      int32 [B]: want[b] or, where the sequence stayed as it is, kv_len[b]; may be kv_len or want
+ *   free_count_out  int32 [1]; may be free_count
+ *   q_len           int32 [B]: max(0, kv_len_out - kv_len), the new rows as the calls below take them
+ *   slots           int64 [B][Lq]: page * page_size + row of new row t, -1 from q_len[b] on (8-byte aligned)
+ *   positions       int32 [B][Lq]: kv_len + t + pos_shift (NULL: 0) of new row t, 0 from q_len[b] on: what seg_rope_rotate takes
+ * A sequence grows by at most Lq rows.  One out of range (want < 0 or past max_pages * page_size, a larger growth, a kv_len out of
+ * range) stays as it is, a free_count outside [0, n_pages] is cut, a page number outside [0, n_pages) comes out as -1 in the table
+ * and the slots: each makes the next seg_attn_poll_status return SEGATTN_ERR_INVALID.  B <= 65535, max_pages * page_size <= 2^30.
+ * `workspace`: DEVICE, 256-byte aligned, seg_pages_workspace_bytes(B) bytes (0: invalid B), scratch.  One or two kernels. */
+size_t seg_pages_workspace_bytes(int32_t B);
+segattn_status seg_pages_resize(int32_t B, int32_t Lq, int32_t page_size, int32_t n_pages, const int32_t* want, int32_t* block_table,
+                                int32_t max_pages, int32_t table_stride, const int32_t* kv_len, const int32_t* pos_shift,
+                                int32_t* free_pages, const int32_t* free_count, int32_t* kv_len_out, int32_t* free_count_out,
+                                int32_t* q_len, int64_t* slots, int32_t* positions, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- An 8-bit cache with a scale for each block of rows and head, instead of one for a head that has to be right before the first
+ * token.  A block is `rows` (16, 32, 64 or 128; a divisor of page_size) rows of a page from a multiple of it on; the value of a
+ * stored element x is x times its block's scale.  The seg_kv_cache beside it has dtype E4M3 and k_scale = v_scale = NULL. */
+typedef struct {
+    float *k, *v;                     /* DEVICE, addressed by (page, block of the page, head) */
+    int64_t k_stride[3], v_stride[3]; /* elements, >= 0 */
+    int32_t rows;
+} seg_block_scales;
+
+/* seg_kv_append (same arguments, same rows left out) into such a cache.  With m the largest finite magnitude that the call adds
+ * to a block (of keys after their rotation), the block's scale becomes the smallest power of two 2^e >= m / 448, -40 <= e <= 119, or stays
+ * where the block has rows of its sequence already and their scale is larger; where it grows those rows are brought to it (times
+ * old / new, rounded to nearest even: exact, but for values below 2^-6 times the new scale).  Stored is x times the scale's inverse,
+ * rounded to nearest even and saturated at +-448; infinities saturate, a NaN stays one.  Scales of blocks that are written into for the
+ * first time may hold anything before.  One kernel. */
+segattn_status seg_blocks_append(const seg_kv_cache* c, const seg_block_scales* scales, int32_t Lq, const void* K_new,
+                                 const int64_t kn_stride[3], const void* V_new, const int64_t vn_stride[3], int32_t Hq, const void* Q,
+                                 const int64_t q_stride[3], void* Q_out, const int64_t qo_stride[3], const float* table,
+                                 int32_t n_pos, int32_t rot_dim, int32_t layout, void* stream);
+
+/* ---- Sparse attention over the far past: a head of class PAST reads, of everything before its segment's tail, the n blocks whose mean
+ * keys score highest against the query, found when the token is decoded.  (seg_retrieval_select is the paper's own operator, for a
+ * segment at a time over keys that lie in one piece; this one is for rows of the paged cache, each with a choice of its own.)
+ * Blocks are `block` slots (16, 32, 64 or 128; a divisor of page_size), block j the slots [j block, (j + 1) block) of a sequence.
+ *   means   of a full block's keys: with m = their mean in double, rounded to fp32, and scale = max |m| / 127 (fp32), q = m / scale
+ *           (fp32) rounded to the nearest integer.  A block with an infinite or NaN mean gets q = 0 and a NaN scale.
+ *           q is int8 contiguous [n_pages][page_size / block][Hkv][d], 16-byte aligned, scale fp32 [n_pages][page_size / block][Hkv]. */
+typedef struct {
+    int8_t* q;      /* DEVICE */
+    float* scale;   /* DEVICE */
+    int32_t block;
+} seg_block_means;
+/* Means of every block that holds one of the sequence's newest q_len (NULL: Lq) rows and is full; other blocks' are left as they were.
+ * The cache's V is not read; `scales` is NULL or its blocks' (of which only those of K are read).  One kernel. */
+segattn_status seg_blocks_summarise(const seg_kv_cache* c, const seg_block_scales* scales, int32_t Lq, const seg_block_means* means, void* stream);
+/* The choice of each new row t and KV head.  For a head of class PAST, with lo the lowest slot that a head of class LOCAL would show
+ * the row (seg_attn_decode), blocks j < R = lo / block (rounded down) are to choose from.  The query: the head's query heads summed in
+ * double, rounded to fp32 (s), step = max |s| / 127, p = s / step rounded to the nearest integer (0 where s is not finite); block j scores
+ * (float)(sum over p_i q_ji) * scale_j, exact but for that product.  The blocks below `sink` are chosen in any case, and of the others those of the
+ * largest scores (equal: lower block; NaN lowest): n together, or all R where there are no more.
+ *   idx   int32 contiguous [B][Lq][Hkv][n]: ascending, then -1; all -1 for heads of other classes.  Rows t >= q_len[b] are left as they were.
+ * K, V and their strides in c are not used.  1 <= n <= 128, 0 <= sink <= n; max_pages * page_size / block at most 393000.  One kernel. */
+segattn_status seg_blocks_select(const seg_kv_cache* c, int32_t Lq, int32_t Hq, int32_t S, int32_t T, const uint8_t* head_past_mask,
+                                 const void* Q, const int64_t q_stride[3], const seg_block_means* means, int32_t n, int32_t sink,
+                                 int32_t* idx, void* stream);
+/* Blocks to attend to, as seg_blocks_select writes them or of any other origin: 1 <= n <= 128 for each [B][Lq][Hkv].  The entries that
+ * count are those in front of the first that does not ascend within [0, R); if that one is not -1 the next seg_attn_poll_status
+ * returns SEGATTN_ERR_INVALID.  Lists of heads of other classes are not read. */
+typedef struct {
+    const int32_t* idx; /* DEVICE, contiguous [B][Lq][Hkv][n] */
+    int32_t n, block;
+} seg_block_choice;
+
+/* seg_attn_decode over a cache with a scale for each block (scales, or NULL: as c says) and, or, with chosen blocks (choice, or NULL).
+ * With a choice a head of class PAST sees the slots of its row's blocks and every slot from R block (see above) to the row's own; the other classes see
+ * what they do without one, and weights_out must be NULL.  Each new row's choice is its own: a call of many rows reads the
+ * slots they all see once for each.  Scales of V should lie within a factor of 2^100 of each other; those of unread blocks may hold anything.
+ * Everything else is seg_attn_decode's, its workspace excepted: seg_attn_decode_blocks_workspace_bytes(...) of the same arguments. */
+size_t seg_attn_decode_blocks_workspace_bytes(const seg_kv_cache* c, const seg_block_scales* scales, const seg_block_choice* choice,
+                                              int32_t Lq, int32_t Hq, int32_t with_weights);
+segattn_status seg_attn_decode_blocks(const seg_kv_cache* c, const seg_block_scales* scales, const seg_block_choice* choice, int32_t Lq,
+                                      int32_t Hq, int32_t S, int32_t T, float sm_scale, const uint8_t* head_past_mask, const void* Q,
+                                      const int64_t q_stride[3], void* O, const int64_t o_stride[3], float* LSE, const float* weights_in,
+                                      float* weights_out, int32_t W, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- Whole training-step call with HOST buffers (pinned or pageable): copies Q, K, V, dO to
  * the device arena, runs forward and backward, copies O, LSE, dQ, dK, dV back, and
  * synchronises `stream` before returning.  Host tensors are contiguous in the layouts

@@ -1,0 +1,463 @@
+// Blocks of rows of the paged cache: 8-bit values with a scale for each block and head, means of blocks, and the choice of blocks
+// by their means.  A block is 2^k rows of a page, 16 to 128, and starts at a multiple of its size in its page and its sequence.
+#pragma once
+#include <cfloat>
+#include <cstdint>
+
+#include "decode_kernels.cuh"
+#include "evict_kernels.cuh"
+#include "paged_cache.cuh"
+#include "rotary_kernels.cuh"
+
+namespace segattn {
+
+// ---- new rows into a cache with a scale for each block ---------------------------------------------------------------
+struct AppendBlocksParams {
+    AppendParams a;                        // a.n: threads that rotate queries
+    float *ks, *vs;
+    long long ks_stride[3], vs_stride[3];  // elements, for (page, block of the page, head)
+    uint32_t units, unit_blocks;           // (sequence, block, K and V heads); thread blocks that work on them
+    FastDiv f_heads2, f_blocks;            // 2 Hkv; blocks that the new rows of a sequence can touch
+    int log;                               // log2 of a block's rows
+};
+
+// The exponent of the scale of a block whose largest value is `top`: 2^e >= top / 448, the smallest such, cut to [-40, 119] (2^119
+// times 448 is bf16's range; 2^-40 lies below every value that matters and keeps the scales of a cache within reach of each other).
+__device__ __forceinline__ int scale_exponent(float top) {
+    const uint32_t bits = __float_as_uint(top);
+    const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);  // 448 = 1.75 * 2^8
+    return min(max(e, -40), 119);
+}
+// 16 values in 8 bits times r, in 8 bits again
+__device__ __forceinline__ uint4 rescale16(const uint4& v, float r) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float x[16];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint32_t lo, hi;
+        e4m3x4_to_half(w[k], lo, hi);
+        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+        x[4 * k] = __fmul_rn(a.x, r);
+        x[4 * k + 1] = __fmul_rn(a.y, r);
+        x[4 * k + 2] = __fmul_rn(b.x, r);
+        x[4 * k + 3] = __fmul_rn(b.y, r);
+    }
+    const uint2 y0 = e4m3x8(x), y1 = e4m3x8(x + 8);
+    return make_uint4(y0.x, y0.y, y1.x, y1.y);
+}
+
+// The queries' part of the call: as kv_append_kernel does it.
+template <bool INTERLEAVED, int HPT>
+__device__ __forceinline__ void rotate_queries(const AppendParams& prm, uint32_t i) {
+    const uint32_t hu = fdiv(i, prm.f_units), row = fdiv(hu, prm.f_groups);
+    const int u = (int)(i - hu * prm.f_units.d), h0 = (int)(hu - row * prm.f_groups.d) * HPT;
+    const int b = (int)fdiv(row, prm.f_Lq), t = (int)(row - (uint32_t)b * prm.f_Lq.d);
+    const int rows = new_rows(prm.c, b);
+    if (t >= rows) return;
+    int r0, r1;
+    unit_offsets<INTERLEAVED>(u, prm.rot, &r0, &r1);
+    const __nv_bfloat16* x = prm.Q + b * prm.q_stride[0] + t * prm.q_stride[1] + h0 * prm.q_stride[2];
+    __nv_bfloat16* y = prm.Qo + b * prm.qo_stride[0] + t * prm.qo_stride[1] + h0 * prm.qo_stride[2];
+    uint4 lo[HPT], hi[HPT];
+#pragma unroll
+    for (int k = 0; k < HPT; ++k)
+        if (h0 + k < prm.Hq) {
+            lo[k] = *reinterpret_cast<const uint4*>(x + k * prm.q_stride[2] + r0);
+            hi[k] = *reinterpret_cast<const uint4*>(x + k * prm.q_stride[2] + r1);
+        }
+    const int n = prm.c.kv_len[b], shift = prm.c.pos_shift ? prm.c.pos_shift[b] : 0;
+    const uint32_t slot = (uint32_t)n - (uint32_t)(rows - t), pos = slot + (uint32_t)shift;
+    if (n < 0 || slot >= (uint32_t)prm.c.cap || (prm.c.q_len && prm.c.q_len[b] != rows) || shift < 0 || pos >= (uint32_t)prm.n_pos) {
+        if (u == 0 && h0 == 0) refuse_input(35);
+        return;
+    }
+    UnitAngles ang;
+    const bool turns = u * 16 < prm.rot;
+    if (turns) ang.load(prm.table + (long long)pos * (prm.rot / 2) + u * 8, 1.f);
+#pragma unroll
+    for (int k = 0; k < HPT; ++k)
+        if (h0 + k < prm.Hq) {
+            float v[16];
+            unpack8(lo[k], v);
+            unpack8(hi[k], v + 8);
+            if (turns) rotate16<INTERLEAVED>(v, ang);
+            *reinterpret_cast<uint4*>(y + k * prm.qo_stride[2] + r0) = pack8(v);
+            *reinterpret_cast<uint4*>(y + k * prm.qo_stride[2] + r1) = pack8(v + 8);
+        }
+}
+
+// G threads (a warp, or the thread block) take one block of one K or V head: its new rows into registers, rotated, their largest value,
+// the block's scale, and the rows in 8 bits.  Where the block has rows already its scale can only grow, and with it those rows are
+// brought to the new one: by a power of two, which costs a value nothing but at the lowest octave of its range.
+template <int D, bool INTERLEAVED, int G, int STEPS>
+__global__ void __launch_bounds__(256) append_blocks_kernel(const __grid_constant__ AppendBlocksParams p) {
+    const AppendParams& a = p.a;
+    if (blockIdx.x >= p.unit_blocks) {
+        const uint32_t i = (blockIdx.x - p.unit_blocks) * 256u + threadIdx.x;
+        if (i < a.n) rotate_queries<INTERLEAVED, 2>(a, i);
+        return;
+    }
+    constexpr int U = D / 16, RP = G / U;  // threads to a row, rows at a time
+    __shared__ uint32_t red[8];
+    const uint32_t unit = blockIdx.x * (256 / G) + threadIdx.x / G;
+    if (unit >= p.units) return;
+    const int tid = threadIdx.x % G, u = tid % U, rr = tid / U;
+    const uint32_t bk = fdiv(unit, p.f_heads2), b = fdiv(bk, p.f_blocks);
+    const int hh = (int)(unit - bk * p.f_heads2.d), k = (int)(bk - b * p.f_blocks.d), Hkv = a.c.Hkv;
+    const bool val = hh >= Hkv;
+    const int h = val ? hh - Hkv : hh;
+    const int rows = new_rows(a.c, b), n = a.c.kv_len[b], shift = a.c.pos_shift ? a.c.pos_shift[b] : 0;
+    if (rows == 0) return;
+    // From the numbers as they are given; rows that they give no place are left out.
+    const int first = n - rows;
+    int lo = max(first, 0), hi = min(n, a.c.cap);
+    if (a.table) hi = (int)min((long long)hi, (long long)a.n_pos - shift);
+    if (n < 0 || (a.c.q_len && a.c.q_len[b] != rows) || (a.table && shift < 0)) hi = lo;
+    if (hi - lo < rows && k == 0 && hh == 0 && tid == 0) refuse_input(35);
+    const int start = ((lo >> p.log) + k) << p.log, from = max(lo, start), to = (int)min((long long)hi, (long long)start + (1 << p.log));
+    if (from >= to) return;
+    int prow;
+    const int page = page_of(a.c, b, start, &prow);
+    if (page < 0) return;
+
+    int e0, e1;  // this thread's two halves of a row
+    unit_offsets<INTERLEAVED>(u, val ? 0 : a.rot, &e0, &e1);
+    const __nv_bfloat16* src = val ? a.Vn + b * a.vn_stride[0] + h * a.vn_stride[2] : a.Kn + b * a.kn_stride[0] + h * a.kn_stride[2];
+    const long long src_row = val ? a.vn_stride[1] : a.kn_stride[1], dst_row = val ? a.c.v_stride[1] : a.c.k_stride[1];
+    const bool turns = !val && a.table && u * 16 < a.rot;
+    float* scale_at = val ? p.vs + page * p.vs_stride[0] + (prow >> p.log) * p.vs_stride[1] + h * p.vs_stride[2]
+                          : p.ks + page * p.ks_stride[0] + (prow >> p.log) * p.ks_stride[1] + h * p.ks_stride[2];
+    const float old = start < lo ? *scale_at : 0.f;
+    uint4 raw[STEPS][2];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const int slot = from + s * RP + rr;
+        if (slot < to) {
+            const __nv_bfloat16* x = src + (slot - first) * src_row;
+            raw[s][0] = *reinterpret_cast<const uint4*>(x + e0);
+            raw[s][1] = *reinterpret_cast<const uint4*>(x + e1);
+        }
+    }
+    float x[STEPS][16], top = 0.f;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const int slot = from + s * RP + rr;
+        if (slot < to) {
+            unpack8(raw[s][0], x[s]);
+            unpack8(raw[s][1], x[s] + 8);
+            if (turns) {
+                UnitAngles ang;
+                ang.load(a.table + (long long)(slot + shift) * (a.rot / 2) + u * 8, 1.f);
+                rotate16<INTERLEAVED>(x[s], ang);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float m = fabsf(x[s][e]);
+                if (m <= FLT_MAX) top = fmaxf(top, m);  // neither an infinity, which saturates, nor a NaN has a say
+            }
+        }
+    }
+    uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+    if (G > 32) {
+        if ((tid & 31) == 0) red[tid >> 5] = most;
+        __syncthreads();
+        most = __reduce_max_sync(0xffffffffu, red[tid & 7]);
+    }
+    const float scale = fmaxf(old, __uint_as_float((uint32_t)(127 + scale_exponent(__uint_as_float(most))) << 23));
+    char* dst = val ? a.c.V + page * a.c.v_stride[0] + prow * dst_row + h * a.c.v_stride[2]
+                    : a.c.K + page * a.c.k_stride[0] + prow * dst_row + h * a.c.k_stride[2];
+    if (start < lo && scale > old) {
+        const float r = __fdiv_rn(old, scale);
+        for (int row = rr; row < lo - start; row += RP) {
+            uint4* at = reinterpret_cast<uint4*>(dst + row * dst_row + u * 16);
+            *at = rescale16(*at, r);
+        }
+    }
+    if (tid == 0 && scale != old) *scale_at = scale;
+    const float inv = __frcp_rn(scale);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const int slot = from + s * RP + rr;
+        if (slot < to) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[s][e] = __fmul_rn(x[s][e], inv);
+            const uint2 y0 = e4m3x8(x[s]), y1 = e4m3x8(x[s] + 8);
+            char* row = dst + (slot - start) * dst_row;
+            if (INTERLEAVED || val || !turns) {
+                *reinterpret_cast<uint4*>(row + e0) = make_uint4(y0.x, y0.y, y1.x, y1.y);
+            } else {
+                *reinterpret_cast<uint2*>(row + e0) = y0;
+                *reinterpret_cast<uint2*>(row + e1) = y1;
+            }
+        }
+    }
+}
+
+// ---- means of blocks --------------------------------------------------------------------------------------------------
+struct SummariseParams {
+    PagedView c;
+    const float* ks;            // e4m3: scales by strides (0, 0, 1) for one to a head
+    long long ks_stride[3];
+    int ks_log;
+    int8_t* sums;               // [n_pages][blocks of a page][Hkv][D]
+    float* sum_scale;           // [n_pages][blocks of a page][Hkv]
+    FastDiv f_heads, f_blocks;  // Hkv; blocks that the new rows of a sequence can touch
+    int log, per_page;          // log2 of a block's rows; blocks of a page
+};
+
+// One thread block takes one head's block of rows, if the new rows have filled it: the mean of its keys, in 64 bits from whole
+// products, so that the order of the sum does not show; then c = max |mean| / 127 and the mean in steps of c.
+template <int D, bool FP8>
+__global__ void __launch_bounds__(128) summarise_kernel(const SummariseParams p) {
+    constexpr int PER = FP8 ? 16 : 8, T = D / PER, RP = 128 / T;  // values of a thread, threads to a row, rows at a time
+    __shared__ double part[RP][D];
+    __shared__ float red[4];
+    const int tid = threadIdx.x;
+    const uint32_t bk = fdiv(blockIdx.x, p.f_heads), b = fdiv(bk, p.f_blocks);
+    const int h = (int)(blockIdx.x - bk * p.f_heads.d), k = (int)(bk - b * p.f_blocks.d);
+    const int rows = new_rows(p.c, b), n = seq_len(p.c, b);
+    if (rows == 0) return;
+    const int start = ((max(n - rows, 0) >> p.log) + k) << p.log;
+    if ((long long)start + (1 << p.log) > n) return;
+    int prow;
+    const int page = page_of(p.c, b, start, &prow);
+    if (page < 0) return;
+    const int c = tid % T, r = tid / T;
+    const char* src = p.c.K + page * p.c.k_stride[0] + prow * p.c.k_stride[1] + h * p.c.k_stride[2] + c * 16;
+    double sum[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) sum[e] = 0.0;
+#pragma unroll 4
+    for (int row = r; row < 1 << p.log; row += RP) {
+        const uint4 v = *reinterpret_cast<const uint4*>(src + row * p.c.k_stride[1]);
+        if (FP8) {
+            const double s = p.ks[page * p.ks_stride[0] + ((prow + row) >> p.ks_log) * p.ks_stride[1] + h * p.ks_stride[2]];
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint32_t lo, hi;
+                e4m3x4_to_half(w[q], lo, hi);
+                const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo)), y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                sum[(4 * q) % PER] += s * x.x;
+                sum[(4 * q + 1) % PER] += s * x.y;
+                sum[(4 * q + 2) % PER] += s * y.x;
+                sum[(4 * q + 3) % PER] += s * y.y;
+            }
+        } else {
+            float x[8];
+            unpack8(v, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += x[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) part[r][c * PER + e] = sum[e];
+    __syncthreads();
+    float mean = 0.f;
+    if (tid < D) {
+        double all = 0.0;
+#pragma unroll
+        for (int k2 = 0; k2 < RP; ++k2) all += part[k2][tid];
+        mean = (float)(all / (double)(1 << p.log));
+    }
+    // |mean| as bits, so that an infinity or a NaN among them is the largest
+    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(mean)));
+    if ((tid & 31) == 0) red[tid >> 5] = __uint_as_float(most);
+    __syncthreads();
+    uint32_t top = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = max(top, __float_as_uint(red[w]));
+    const bool fine = top < 0x7f800000u;
+    const float step = fine ? __fdiv_rn(__uint_as_float(top), 127.f) : __uint_as_float(0x7fffffffu);
+    const long long at = ((long long)page * p.per_page + (prow >> p.log)) * p.c.Hkv + h;
+    if (tid < D) p.sums[at * D + tid] = fine && step > 0.f ? (int8_t)__float2int_rn(__fdiv_rn(mean, step)) : (int8_t)0;
+    if (tid == 0) p.sum_scale[at] = step;
+}
+
+// ---- the choice of blocks ---------------------------------------------------------------------------------------------
+struct SelectParams {
+    PagedView c;                // K, V and their strides unused
+    const __nv_bfloat16* Q;
+    long long q_stride[3];
+    const int8_t* sums;
+    const float* sum_scale;
+    int32_t* idx;               // [B][Lq][Hkv][n]
+    FastDiv f_S;
+    int S, T, g, n, sink, log, per_page, keys;
+    uint8_t head_class[64];
+};
+
+constexpr int kSelThreads = 512;
+constexpr int kSelBins = 2048;
+constexpr int kSelKeys = 49152;  // blocks that a thread block has room for
+constexpr int kSelSlice = 4096;  // blocks that a thread block of a cluster has at least
+
+// The lowest slot that a row at `slot` sees whole through a head with a past: its tail's start, rounded down to a block.
+__device__ __forceinline__ int whole_from(const SelectParams& p, int slot, int shift) {
+    const uint32_t pos = (uint32_t)slot + (uint32_t)shift;
+    const long long start = (long long)fdiv(pos, p.f_S) * p.S;
+    return (int)max(0ll, max(0ll, start - p.T) - shift) >> p.log << p.log;
+}
+
+// A cluster takes one (new row, KV head).  The query, summed over the head's query heads and brought to 8 bits, against the means
+// of the blocks before the row's tail: integer products, so that a score is the same in whatever order it is added up; then the n
+// largest by a radix selection (evict_select_kernel's, with the sums over the cluster's blocks through distributed shared memory)
+// and their numbers in ascending order.
+template <int D>
+__global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_constant__ SelectParams p) {
+    constexpr int T = D / 16, PW = 32 / T;  // lanes to a mean, means of a warp's load
+    extern __shared__ uint32_t sel_smem[];
+    uint32_t* hist = sel_smem;                 // [3][kSelBins]
+    uint32_t* keys = sel_smem + 3 * kSelBins;  // [p.keys]
+    __shared__ __align__(16) int8_t query[D];
+    __shared__ uint32_t red[kSelThreads / 32], seg_gt[kSelThreads / 32], seg_eq[kSelThreads / 32], found[2], totals[2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int CS = (int)cluster_size(), rank = (int)cluster_rank(), unit = blockIdx.x / CS;
+    const int h = unit % p.c.Hkv, bt = unit / p.c.Hkv, b = bt / p.c.Lq, t = bt - b * p.c.Lq;
+    const int rows = new_rows(p.c, b);
+    if (t >= rows) return;
+    int32_t* out = p.idx + (long long)unit * p.n;
+    const int slot = seq_len(p.c, b) - rows + t;
+    const int m = p.head_class[h] == kHeadPast && slot >= 0 ? whole_from(p, slot, shift_of(p.c, b)) >> p.log : 0;  // blocks to choose from
+    if (m <= p.n) {
+        for (int i = rank * kSelThreads + tid; i < p.n; i += CS * kSelThreads) out[i] = i < m ? i : -1;
+        return;
+    }
+
+    // the query
+    float q = 0.f;
+    if (tid < D) {
+        double sum = 0.0;
+        const __nv_bfloat16* at = p.Q + b * p.q_stride[0] + t * p.q_stride[1] + (long long)h * p.g * p.q_stride[2] + tid;
+        for (int x = 0; x < p.g; ++x) sum += (double)__bfloat162float(at[x * p.q_stride[2]]);
+        q = (float)sum;
+    }
+    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(q)));
+    if (lane == 0) red[warp] = most;
+    for (int i = tid; i < 3 * kSelBins; i += kSelThreads) hist[i] = 0;
+    __syncthreads();
+    const uint32_t top = __reduce_max_sync(0xffffffffu, lane < D / 32 ? red[lane] : 0u);
+    const float step = __fdiv_rn(__uint_as_float(top), 127.f);
+    if (tid < D) query[tid] = top > 0 && top < 0x7f800000u && step > 0.f ? (int8_t)__float2int_rn(__fdiv_rn(q, step)) : (int8_t)0;
+    __syncthreads();
+    const uint4 q16 = *reinterpret_cast<const uint4*>(query + lane % T * 16);
+
+    // the scores of this block's slice, as unsigned numbers of the same order
+    const int slice = (((m + CS - 1) / CS + 31) & ~31), j0 = min(rank * slice, m), cnt = min(slice, m - j0);
+    constexpr int AHEAD = 4;
+    for (int i0 = warp * PW * AHEAD; i0 < cnt; i0 += kSelThreads / 32 * PW * AHEAD) {
+        uint4 k16[AHEAD];
+        float sc[AHEAD];
+#pragma unroll
+        for (int y = 0; y < AHEAD; ++y) {
+            const int i = i0 + y * PW + lane / T;
+            k16[y] = make_uint4(0, 0, 0, 0);
+            sc[y] = 0.f;
+            if (i < cnt) {
+                int prow;
+                const int page = page_of(p.c, b, (j0 + i) << p.log, &prow);
+                sc[y] = __uint_as_float(0x7fffffffu);  // of a page that is not there: lowest
+                if (page >= 0) {
+                    const long long at = ((long long)page * p.per_page + (prow >> p.log)) * p.c.Hkv + h;
+                    k16[y] = *reinterpret_cast<const uint4*>(p.sums + at * D + lane % T * 16);
+                    sc[y] = p.sum_scale[at];
+                }
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < AHEAD; ++y) {
+            int s = __dp4a((int)k16[y].x, (int)q16.x, __dp4a((int)k16[y].y, (int)q16.y, __dp4a((int)k16[y].z, (int)q16.z, __dp4a((int)k16[y].w, (int)q16.w, 0))));
+#pragma unroll
+            for (int x = 1; x < T; x <<= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
+            const int i = i0 + y * PW + lane / T;
+            if (lane % T == 0 && i < cnt) keys[i] = j0 + i < p.sink ? 0xffffffffu : weight_key(__fmul_rn((float)s, sc[y]));
+        }
+    }
+    __syncthreads();
+
+    // the n-th largest key
+    uint32_t prefix = 0, need = p.n;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+        uint32_t* mh = hist + pass * kSelBins;
+        for (int i = tid; i < cnt; i += kSelThreads)
+            if (pass == 0 || keys[i] >> (shift + bits) == prefix) atomicAdd(mh + ((keys[i] >> shift) & ((1u << bits) - 1)), 1u);
+        __syncthreads();
+        if (CS > 1) cluster_sync();
+        // bins from the top down, four to a thread
+        uint32_t c[4], before = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t* at = mh + kSelBins - 1 - 4 * tid - k;
+            c[k] = 0;
+            if (CS == 1) c[k] = *at;
+            else
+                for (int r = 0; r < CS; ++r) c[k] += load_from_block(at, r);
+            before += c[k];
+        }
+        const uint32_t mine = before;
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, before, x);
+            if (lane >= x) before += y;
+        }
+        if (lane == 31) red[warp] = before;
+        before -= mine;
+        __syncthreads();
+        before += __reduce_add_sync(0xffffffffu, lane < warp ? red[lane] : 0u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (need > before && need <= before + c[k]) {
+                found[0] = kSelBins - 1 - 4 * tid - k;
+                found[1] = need - before;
+            }
+            before += c[k];
+        }
+        __syncthreads();
+        prefix = (prefix << bits) | found[0];
+        need = found[1];
+    }
+    // keys above `prefix` are all chosen, of those equal to it the first `need`; each warp has a segment of the slice
+    const int seg = (((cnt + kSelThreads / 32 - 1) / (kSelThreads / 32)) + 31) & ~31, s0 = min(warp * seg, cnt), s1 = min(s0 + seg, cnt);
+    uint32_t gt = 0, eq = 0;
+    for (int i = s0 + lane; i < s1; i += 32) {
+        gt += keys[i] > prefix;
+        eq += keys[i] == prefix;
+    }
+    gt = __reduce_add_sync(0xffffffffu, gt);
+    eq = __reduce_add_sync(0xffffffffu, eq);
+    if (lane == 0) {
+        seg_gt[warp] = gt;
+        seg_eq[warp] = eq;
+    }
+    __syncthreads();
+    constexpr int W = kSelThreads / 32;
+    uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? seg_gt[lane] : 0u);
+    uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? seg_eq[lane] : 0u);
+    if (CS > 1) {
+        const uint32_t gt_all = __reduce_add_sync(0xffffffffu, lane < W ? seg_gt[lane] : 0u), eq_all = __reduce_add_sync(0xffffffffu, lane < W ? seg_eq[lane] : 0u);
+        if (tid == 0) {
+            totals[0] = gt_all;
+            totals[1] = eq_all;
+        }
+        cluster_sync();
+        for (int r = 0; r < rank; ++r) {
+            gt_before += load_from_block(totals, r);
+            eq_before += load_from_block(totals + 1, r);
+        }
+    }
+    for (int i0 = s0; i0 < s1; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t key = i < s1 ? keys[i] : 0u;
+        const uint32_t above = __ballot_sync(0xffffffffu, i < s1 && key > prefix), same = __ballot_sync(0xffffffffu, i < s1 && key == prefix);
+        const uint32_t below = (1u << lane) - 1;
+        const uint32_t g_at = gt_before + __popc(above & below), e_at = eq_before + __popc(same & below);
+        if (((above >> lane) & 1) || (((same >> lane) & 1) && e_at < need)) out[g_at + min(e_at, need)] = j0 + i;
+        gt_before += __popc(above);
+        eq_before += __popc(same);
+    }
+    if (CS > 1) cluster_sync();  // the others may still read this block's totals
+}
+
+}  // namespace segattn

@@ -59,6 +59,14 @@ struct DecodeParams {
     uint8_t head_class[64];
     uint8_t head_order[64];          // the heads by class, unit after unit
     uint8_t head_in_unit[64];        // by head
+    // an 8-bit cache with a scale for each block of 2^scale_log rows of a page and head
+    const float *ks, *vs;
+    long long ks_stride[3], vs_stride[3];  // elements, for (page, block of the page, head)
+    int scale_log;
+    // blocks of 2^choice_log slots that heads with a past read of what lies behind their tail
+    int choice_log, n_chosen;
+    const int32_t* chosen;           // [B][Lq][Hkv][n_chosen]; null: no choice, the whole past
+    int head_blocks;                 // ceil(g / (rows of an item)), an item being of one new row
 };
 
 // Programmatic launch: the next kernel of the stream may be set up from here on, and this kernel waits for the end (and the
@@ -79,11 +87,32 @@ __device__ __forceinline__ void visible_slots(const DecodeParams& p, int n, int 
     }
 }
 
+// With chosen blocks an item is up to MB query heads of one new row, and its slots are numbered through: a head with a past has
+// the chosen blocks one after the other in [0, far), then what it sees whole, from its tail's start (rounded down to a block) on:
+// number v stands for slot v + off there.  Every number in [*lo, *hi) is visible to every row of the item.
+__device__ __forceinline__ void numbered_slots(const DecodeParams& p, int n, int rows, int shift, int t, int cls, int* lo, int* hi, int* far, int* off) {
+    visible_slots(p, n, rows, shift, t, cls == kHeadPast ? kHeadLocal : cls, lo, hi);
+    *far = *off = 0;
+    if (cls == kHeadPast) {
+        const int blocks = *lo >> p.choice_log, whole = blocks << p.choice_log;
+        *far = min(blocks, p.n_chosen) << p.choice_log;
+        *off = whole - *far;
+        *hi = max(*hi - *off, *far);
+        *lo = 0;
+    }
+    *hi = max(*hi, *lo);
+}
+
 // ---- the list of tiles -------------------------------------------------------------------------------------------
 // Slots the rows of one row block see between them (their lower and upper ends both grow with the row), and its tiles:
 // whole tiles of 2^tile_log slots, at least one, so that rows that see nothing are written too.
-template <int MB>
+template <int MB, bool SEL = false>
 __device__ __forceinline__ int item_tiles(const DecodeParams& p, int n, int rows, int shift, int cls, int tile_log, int rb, int* lo, int* hi) {
+    if (SEL) {
+        int far, off;
+        numbered_slots(p, n, rows, shift, rb / p.head_blocks, cls, lo, hi, &far, &off);
+        return max(1, ((*hi + (1 << tile_log) - 1) >> tile_log) - (*lo >> tile_log));
+    }
     const int last = min((rb + 1) * MB, rows * p.g) - 1;
     int l0, h0, l1, h1;
     visible_slots(p, n, rows, shift, (int)fdiv((uint32_t)(rb * MB), p.f_g), cls, &l0, &h0);
@@ -93,11 +122,31 @@ __device__ __forceinline__ int item_tiles(const DecodeParams& p, int n, int rows
     return max(1, ((*hi + (1 << tile_log) - 1) >> tile_log) - (l0 >> tile_log));
 }
 
+// whether row block rb of a sequence has a row
+template <int MB, bool SEL>
+__device__ __forceinline__ bool has_rows(const DecodeParams& p, int rows, int rb) {
+    return SEL ? rb < rows * p.head_blocks : rb * MB < rows * p.g;
+}
+// New row t and query head hq (of its KV head) that row i of a row block stands for; whether it is there (else t of a row that is).
+template <int MB, bool SEL>
+__device__ __forceinline__ bool row_of(const DecodeParams& p, int rows, int rb, int i, int* t, int* hq) {
+    if (SEL) {
+        *t = rb / p.head_blocks;
+        *hq = (rb - *t * p.head_blocks) * MB + i;
+        return *hq < p.g;
+    }
+    const int r = rb * MB + i;
+    const bool real = r < rows * p.g;
+    *t = (int)fdiv((uint32_t)(real ? r : 0), p.f_g);
+    *hq = r - *t * p.g;
+    return real;
+}
+
 // Tiles of one unit of class cls of a sequence.  A unit's tile has 2^(TILE_LOG - unit_log) slots: the same bytes for all.
-template <int MB, int TILE_LOG>
+template <int MB, int TILE_LOG, bool SEL = false>
 __device__ __forceinline__ int unit_tiles(const DecodeParams& p, int n, int rows, int shift, int cls) {
     int sum = 0, lo, hi;
-    for (int rb = 0; rb * MB < rows * p.g; ++rb) sum += item_tiles<MB>(p, n, rows, shift, cls, TILE_LOG - p.unit_log[cls], rb, &lo, &hi);
+    for (int rb = 0; has_rows<MB, SEL>(p, rows, rb); ++rb) sum += item_tiles<MB, SEL>(p, n, rows, shift, cls, TILE_LOG - p.unit_log[cls], rb, &lo, &hi);
     return sum;
 }
 
@@ -115,7 +164,7 @@ __device__ __forceinline__ int class_of_unit(const DecodeParams& p, int u, int* 
 }
 
 // A place in the list: an item (a row block of a unit of a sequence) and a tile of it.
-template <int MB, int TILE_LOG>
+template <int MB, int TILE_LOG, bool SEL = false>
 struct TileCursor {
     int b, u, rb, n, rows, shift;
     int cls, log, first_head;    // of the unit; it has 2^log heads
@@ -129,12 +178,12 @@ struct TileCursor {
     __device__ __forceinline__ void enter(const DecodeParams& p, int at) {
         cls = class_of_unit(p, u, &first_head);
         log = p.unit_log[cls];
-        end = item_tiles<MB>(p, n, rows, shift, cls, TILE_LOG - log, rb, &lo, &hi);
+        end = item_tiles<MB, SEL>(p, n, rows, shift, cls, TILE_LOG - log, rb, &lo, &hi);
         tile = at;
     }
     // the item after this one; the caller knows that there is one
     __device__ __forceinline__ void next_item(const DecodeParams& p) {
-        if (++rb * MB >= rows * p.g) {
+        if (!has_rows<MB, SEL>(p, rows, ++rb)) {
             rb = 0;
             if (++u == p.units[0] + p.units[1] + p.units[2]) {
                 u = 0;
@@ -156,7 +205,7 @@ struct TileCursor {
 struct BlockRange {
     int begin, end, per, b, u, rb, tile;
 };
-template <int MB, int TILE_LOG>
+template <int MB, int TILE_LOG, bool SEL = false>
 __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* out, int* warp_sum) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int seg = (p.c.B + kDecThreads - 1) / kDecThreads;
@@ -168,7 +217,7 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
         int sum = 0;
 #pragma unroll
         for (int cls = 0; cls < 3; ++cls)
-            if (p.units[cls]) sum += p.units[cls] * unit_tiles<MB, TILE_LOG>(p, n, rows, shift, cls);
+            if (p.units[cls]) sum += p.units[cls] * unit_tiles<MB, TILE_LOG, SEL>(p, n, rows, shift, cls);
         return sum;
     };
     int mine = 0;
@@ -200,7 +249,7 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
         const int n = seq_len(p.c, b), rows = new_rows(p.c, b), shift = shift_of(p.c, b);
         int u = 0, rb = 0, cls = 0;
         for (;; ++cls) {
-            const int t = p.units[cls] ? unit_tiles<MB, TILE_LOG>(p, n, rows, shift, cls) : 0;
+            const int t = p.units[cls] ? unit_tiles<MB, TILE_LOG, SEL>(p, n, rows, shift, cls) : 0;
             if (off < t * p.units[cls]) {
                 u += off / t;
                 off %= t;
@@ -211,7 +260,7 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
         }
         for (;; ++rb) {
             int lo, hi;
-            const int t = item_tiles<MB>(p, n, rows, shift, cls, TILE_LOG - p.unit_log[cls], rb, &lo, &hi);
+            const int t = item_tiles<MB, SEL>(p, n, rows, shift, cls, TILE_LOG - p.unit_log[cls], rb, &lo, &hi);
             if (off < t) break;
             off -= t;
         }
@@ -325,16 +374,26 @@ constexpr float kDecSlack = 8.f;
 // by an eighth).  So the base is put 2^13 under the maximum, and moved when a weight would pass 2^15, fp16's largest power:
 // weights are exact to fp16's half step down to 2^-27 of the largest.
 constexpr float kHalfRoom = 13.f, kHalfTop = 15.f;
+// With a scale for each block of rows a weight goes into the product with V times its block's scale m 2^e (1 <= m < 2): as
+// m exp2(score + e - base), so that fp16's range is spent on what a weight adds to O and not on the scale, whatever its size.  The
+// sum takes exp2(score + e - base) 2^-e, exactly.  Bases are whole numbers there (e - base is exact), and one lower for m.
+constexpr float kScaledRoom = 12.f, kScaledTop = 14.f;
 
-template <int D, bool FP8, int NT, int WM>
+// BS: a scale for each block of rows (the members of DecodeParams from ks on), for FP8.  SEL: heads with a past read chosen blocks of
+// it and what their own segment and tail show them (from choice_log on); WM = 1.
+template <int D, bool FP8, int NT, int WM, bool BS = false, bool SEL = false>
 __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
     using Sh = DecodeShape<D, FP8, NT, WM>;
+    static_assert(!BS || (FP8 && Sh::KG == 2 && Sh::KP == 2), "the warp's two blocks of 16 slots have a scale each");
+    static_assert(!SEL || WM == 1, "an item's rows all see the same slots");
+    constexpr float kTop = BS ? kScaledTop : kHalfTop;
     constexpr int RB = Sh::RB, C = RB / 16, MB = Sh::MB, WR = Sh::kWR, ST = Sh::kStages, KS = D / 16, MT = D / 16, KG = Sh::KG, KP = Sh::KP;
     extern __shared__ uint8_t smem_raw[];
     __shared__ BlockRange range;
     __shared__ int warp_sum[4];
     __shared__ uint32_t there[ST][4];  // which of a warp's 16 KG slots were loaded, per stage
     __shared__ float2 end_ml[4][8];    // an item's end: base and sum of eight rows of each warp
+    __shared__ float2 block_scale[BS ? ST : 1][4][2];  // of K and V, for each of a warp's blocks of 16 slots
     const uint32_t ring = (smem_u32(smem_raw) + 127u) & ~127u;
     uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q4 = lane & 3, l4 = lane >> 2;
@@ -345,10 +404,10 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
     auto head_of = [&](int first_head, int log) { return (int)p.head_order[first_head + (WM == 1 ? warp & ((1 << log) - 1) : 0)]; };
 
     next_kernel_may_start();
-    find_range<MB, Sh::kTileLog>(p, &range, warp_sum);
+    find_range<MB, Sh::kTileLog, SEL>(p, &range, warp_sum);
     if (range.begin >= range.end) return;
     const int per = range.per;
-    TileCursor<MB, Sh::kTileLog> put, get;  // what is loaded next, and what is computed next
+    TileCursor<MB, Sh::kTileLog, SEL> put, get;  // what is loaded next, and what is computed next
     get.b = range.b;
     get.u = range.u;
     get.rb = range.rb;
@@ -362,21 +421,59 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
     const int r0 = lane / C, ch = lane % C;
     const uint32_t put_lane = swizzled<RB>(r0, ch);
     const char *k_item, *v_item;  // of the item being loaded: this lane's piece of row r0 of page 0
+    const float* s_item = nullptr;  // its scales: of K for lane 0, of V for lane 1
+    int far = 0, off = 0;         // its numbered slots
+    int chosen[SEL ? 4 : 1], n_chosen = 0;  // its blocks, 32 k + lane in chosen[k], and how many of them are in order
     auto enter_item = [&]() {
         const int h = head_of(put.first_head, put.log);
+        if (BS) s_item = lane == 0 ? p.ks + h * p.ks_stride[2] : p.vs + h * p.vs_stride[2];
+        if (SEL) {
+            int lo, hi;
+            const int t = put.rb / p.head_blocks;
+            numbered_slots(p, put.n, put.rows, put.shift, t, put.cls, &lo, &hi, &far, &off);
+            n_chosen = 0;
+            if (far > 0) {
+                // Blocks count while they ascend within the past: none is read twice, nor one that the row sees whole.
+                const int32_t* list = p.chosen + (((long long)put.b * p.c.Lq + t) * p.c.Hkv + h) * p.n_chosen;
+                const int past = (off + far) >> p.choice_log;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) chosen[k] = 32 * k + lane < p.n_chosen ? list[32 * k + lane] : -1;
+                bool more = true;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int last = k ? __shfl_sync(0xffffffffu, chosen[k ? k - 1 : 0], 31) : -1, up = __shfl_up_sync(0xffffffffu, chosen[k], 1);
+                    const bool fine = (unsigned)chosen[k] < (unsigned)past && chosen[k] > (lane ? up : last);
+                    const uint32_t wrong = __ballot_sync(0xffffffffu, !fine);
+                    if (more) {
+                        n_chosen += wrong ? __ffs(wrong) - 1 : 32;
+                        more = wrong == 0;
+                        if (wrong && lane == __ffs(wrong) - 1 && chosen[k] != -1) refuse_input(36);
+                    }
+                }
+            }
+        }
         k_item = p.c.K + r0 * p.c.k_stride[1] + h * p.c.k_stride[2] + ch * 16;
         v_item = p.c.V + r0 * p.c.v_stride[1] + h * p.c.v_stride[2] + ch * 16;
     };
+    // the first slot of 16 that are numbered from v0 on; -1 for those of a block that is not there
+    auto slot_from = [&](int v0) {
+        if (!SEL || v0 >= far) return v0 + (SEL ? off : 0);
+        const int i = v0 >> p.choice_log;
+        const int from = i < 32 ? chosen[0] : i < 64 ? chosen[SEL ? 1 : 0] : i < 96 ? chosen[SEL ? 2 : 0] : chosen[SEL ? 3 : 0];
+        const int block = __shfl_sync(0xffffffffu, from, i & 31);
+        return i < n_chosen ? (block << p.choice_log) + (v0 & ((1 << p.choice_log) - 1)) : -1;
+    };
     // The pages of the tile to be loaded next, looked up one tile ahead: the look-up is a load of its own, and the loads of the
     // rows wait for it.  An entry of the table outside the visible slots is not read.
-    int page_next[KG];
+    int page_next[KG], slot_next[KG];
     auto look_up = [&]() {
         const int slot0 = put.first_slot() + (WM == 1 ? key_group(put.log) : warp) * 16 * KG;
 #pragma unroll
         for (int k = 0; k < KG; ++k) {
             const int s0 = slot0 + 16 * k;
             page_next[k] = -1;
-            if (p.page_whole && s0 >= put.lo && s0 + 16 <= put.hi) page_next[k] = table_entry(p.c, put.b, s0);
+            slot_next[k] = slot_from(s0);
+            if (p.page_whole && s0 >= put.lo && s0 + 16 <= put.hi && (!SEL || slot_next[k] >= 0)) page_next[k] = table_entry(p.c, put.b, slot_next[k]);
         }
     };
     enter_item();
@@ -392,7 +489,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                 int prow, page = page_next[k];
                 if ((unsigned)page < (unsigned)p.c.n_pages) {
                     // 16 visible slots in one page: one look-up, and rows a stride apart
-                    prow = row_in_page(p.c, s0);
+                    prow = row_in_page(p.c, SEL ? slot_next[k] : s0);
                     const char* src = k_item + page * p.c.k_stride[0] + prow * p.c.k_stride[1];
 #pragma unroll
                     for (int i = 0; i < 16 / RPI; ++i) {
@@ -408,19 +505,34 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                     loaded |= 0xffffu << (16 * k);
                 } else {
                     const int slot = s0 + (lane & 15);
-                    long long off = -1;  // of one row: lanes 0-15 in K, 16-31 in V
-                    if (slot >= put.lo && slot < put.hi && (page = page_of(p.c, put.b, slot, &prow)) >= 0) {
+                    long long row_off = -1;  // of one row: lanes 0-15 in K, 16-31 in V
+                    page = -1;
+                    if (slot >= put.lo && slot < put.hi && (!SEL || slot_next[k] >= 0) &&
+                        (page = page_of(p.c, put.b, SEL ? slot_next[k] + (lane & 15) : slot, &prow)) >= 0) {
                         const long long* st = lane < 16 ? p.c.k_stride : p.c.v_stride;
-                        off = page * st[0] + prow * st[1] + head_of(put.first_head, put.log) * st[2];
+                        row_off = page * st[0] + prow * st[1] + head_of(put.first_head, put.log) * st[2];
                     }
-                    loaded |= (__ballot_sync(0xffffffffu, off >= 0) & 0xffffu) << (16 * k);
+                    const uint32_t found = __ballot_sync(0xffffffffu, row_off >= 0);
+                    loaded |= (found & 0xffffu) << (16 * k);
+                    if (BS) {  // 16 slots of one page
+                        const int from = found ? __ffs(found) - 1 : 0;
+                        page = __shfl_sync(0xffffffffu, page, from);
+                        prow = __shfl_sync(0xffffffffu, prow, from);
+                    }
 #pragma unroll 1
                     for (int i = 0; i < 32 / RPI; ++i) {
                         const int row = i * RPI + r0;  // 0-15 of K, then of V
-                        const long long o = __shfl_sync(0xffffffffu, off, row);
+                        const long long o = __shfl_sync(0xffffffffu, row_off, row);
                         cp_async16_if(dst - put_lane + (row >> 4) * 16 * RB + swizzled<RB>(row & 15, ch),
                                       (row & 16 ? p.c.V : p.c.K) + (o >= 0 ? o + ch * 16 : 0), o >= 0);
                     }
+                }
+                if (BS && lane < 2) {
+                    float* to = &block_scale[BS ? s : 0][warp][k].x + lane;
+                    const long long* st = lane == 0 ? p.ks_stride : p.vs_stride;
+                    if ((unsigned)page < (unsigned)p.c.n_pages)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(to)), "l"(s_item + page * st[0] + (prow >> p.scale_log) * st[1]) : "memory");
+                    else *to = 1.f;  // none of the 16 is there
                 }
             }
             if (lane == 0) there[s][warp] = loaded;
@@ -462,9 +574,9 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
         const int cls = get.cls, rows = get.rows * p.g, group = key_group(get.log), head = head_of(get.first_head, get.log);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = get.rb * MB + wrow * WR + nt * 8 + l4;  // the row whose elements this lane holds
-            const bool real = r < rows;
-            const int t = (int)fdiv((uint32_t)(real ? r : 0), p.f_g), qh = head * p.g + (real ? r - t * p.g : 0);
+            int t, hq;  // of the row whose elements this lane holds
+            const bool real = row_of<MB, SEL>(p, get.rows, get.rb, wrow * WR + nt * 8 + l4, &t, &hq);
+            const int qh = head * p.g + (real ? hq : 0);
             const __nv_bfloat16* q = p.Q + get.b * p.q_stride[0] + t * p.q_stride[1] + qh * p.q_stride[2];
             float scale = p.scale_log2;
             if (FP8) {
@@ -490,7 +602,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 const int e = big > 0.f ? min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126) : 0;
                 const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-                scale *= p.k_scale[head] * __uint_as_float((uint32_t)(127 + e) << 23);
+                scale *= (BS ? 1.f : p.k_scale[head]) * __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     qf[k][nt][0] = real ? pack16<true>(x[4 * k] * down, x[4 * k + 1] * down) : 0u;
@@ -507,7 +619,12 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
             for (int e = 0; e < 2; ++e) {
                 const int rc = get.rb * MB + wrow * WR + nt * 8 + 2 * q4 + e;  // a row whose scores this lane holds
                 qscale[nt][e] = FP8 ? __shfl_sync(0xffffffffu, scale, (2 * q4 + e) * 4) : scale;
-                visible_slots(p, get.n, get.rows, get.shift, (int)fdiv((uint32_t)min(rc, rows - 1), p.f_g), cls, &rlo[nt][e], &rhi[nt][e]);
+                if (SEL) {
+                    rlo[nt][e] = get.lo;
+                    rhi[nt][e] = get.hi;
+                } else {
+                    visible_slots(p, get.n, get.rows, get.shift, (int)fdiv((uint32_t)min(rc, rows - 1), p.f_g), cls, &rlo[nt][e], &rhi[nt][e]);
+                }
                 base[nt][e] = l[nt][e] = 0.f;
                 slack[nt][e] = -INFINITY;
             }
@@ -519,8 +636,8 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[k][nt][e] = 0.f;
         // slots that every row of the item sees: no mask there
-        int all_lo, all_hi;
-        {
+        int all_lo = get.lo, all_hi = get.hi;
+        if (!SEL) {
             const int r_last = min((get.rb + 1) * MB, rows) - 1;
             int x;
             visible_slots(p, get.n, get.rows, get.shift, (int)fdiv((uint32_t)r_last, p.f_g), cls, &all_lo, &x);
@@ -592,6 +709,23 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[k][nt][e] = CH == 1 ? s2[0][k][nt][e] : s2[0][k][nt][e] + s2[CH - 1][k][nt][e];
+                float ksc[KP], vsc[KP], vexp[KP], vinv[KP];  // scales of the blocks; m, e and 2^-e of V's
+                if (BS) {
+#pragma unroll
+                    for (int k = 0; k < KP; ++k) {
+                        const float2 sc = block_scale[BS ? stage : 0][from][BS ? k : 0];
+                        const uint32_t bits = __float_as_uint(sc.y);
+                        const int e = min(max((int)((bits >> 23) & 0xffu) - 127, -126), 126);
+                        ksc[k] = sc.x;
+                        vsc[k] = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
+                        vexp[k] = (float)e;
+                        vinv[k] = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) s[k][nt][x] *= ksc[k];
+                    }
+                }
                 // element e of s[k][nt]: slot 16 k + js[e >> 1], row 2 q4 + (e & 1) of the warp's eight; log2 units over the base
                 const bool edge_range = slot0 < all_lo || slot0 + 16 * KP > all_hi;
                 if (scores) {
@@ -613,7 +747,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[k][nt][e] = fmaf(s[k][nt][e], qscale[nt][e & 1], -base[nt][e & 1]);
+                        for (int e = 0; e < 4; ++e) s[k][nt][e] = fmaf(s[k][nt][e], qscale[nt][e & 1], BS ? vexp[k] - base[nt][e & 1] : -base[nt][e & 1]);
                 if (edge_range || have != (KP == 1 ? 0xffffu : 0xffffffffu)) {
 #pragma unroll
                     for (int k = 0; k < KP; ++k)
@@ -647,13 +781,13 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                             // row by row: what one row sees must not move another row's base (and with it its rounding)
                             f[e] = 1.f;
                             if (mx > slack[nt][e]) {
-                                const float moved = base[nt][e] + (FP8 ? mx - kHalfRoom : mx);
+                                const float moved = BS ? floorf(base[nt][e] + (mx - kScaledRoom)) : base[nt][e] + (FP8 ? mx - kHalfRoom : mx);
                                 mx = moved - base[nt][e];  // by what the rounded base has moved: scores and sums follow it
                                 f[e] = slack[nt][e] == -INFINITY ? 0.f : ex2(-mx);
                                 base[nt][e] = moved;
-                                slack[nt][e] = FP8 ? kHalfTop : kDecSlack;
+                                slack[nt][e] = FP8 ? kTop : kDecSlack;
                                 // a base past 2^26 is rounded by whole powers of two: what that leaves over fp16's top is cut
-                                auto over_new_base = [&](float x) { return FP8 && x - mx > kHalfTop ? kHalfTop : x - mx; };
+                                auto over_new_base = [&](float x) { return FP8 && x - mx > kTop ? kTop : x - mx; };
 #pragma unroll
                                 for (int k = 0; k < KP; ++k) {
                                     s[k][nt][e] = over_new_base(s[k][nt][e]);
@@ -676,7 +810,8 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             s[k][nt][e] = ex2(s[k][nt][e]);
-                            l[nt][e & 1] += s[k][nt][e];
+                            l[nt][e & 1] = BS ? fmaf(s[k][nt][e], vinv[k], l[nt][e & 1]) : l[nt][e & 1] + s[k][nt][e];
+                            if (BS) s[k][nt][e] *= vsc[k];
                         }
                         pf[k][nt][0] = movm_t(pack16<FP8>(s[k][nt][0], s[k][nt][1]));
                         pf[k][nt][1] = movm_t(pack16<FP8>(s[k][nt][2], s[k][nt][3]));
@@ -814,7 +949,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
         const int side = WM == 1 ? 1 << get.log : WM;  // warps w, w + side, ... hold parts of the same rows
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            if (nt > 0 && get.rb * MB + nt * 8 >= rows) break;  // none of the warps' rows from here on is there (WM = 1)
+            if (nt > 0 && (SEL ? get.rb % p.head_blocks * MB + nt * 8 >= p.g : get.rb * MB + nt * 8 >= rows)) break;  // none of the warps' rows from here on is there (WM = 1)
             float* mine = reinterpret_cast<float*>(ring_ptr + (size_t)(free_stage * 4 + warp) * Sh::kWarpStage);
             __syncthreads();
             // row r8 at r8 D, its dims XORed with the row so that the lanes' writes fall into different banks
@@ -831,10 +966,10 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
             const int d0 = (threadIdx.x % TPR) * 4;
             for (int i = threadIdx.x / TPR; i < side * 8; i += kDecThreads / TPR) {
                 const int w0 = i >> 3, r8 = i & 7;
-                const int rl = (WM == 1 ? 0 : w0 * WR) + nt * 8 + r8, r = get.rb * MB + rl;
-                if (r >= rows) continue;
+                int t, hq;
+                if (!row_of<MB, SEL>(p, get.rows, get.rb, (WM == 1 ? 0 : w0 * WR) + nt * 8 + r8, &t, &hq)) continue;
                 const int h = p.head_order[get.first_head + (WM == 1 ? w0 : 0)];
-                const float vs = FP8 ? p.v_scale[h] : 1.f;
+                const float vs = FP8 && !BS ? p.v_scale[h] : 1.f;
                 float mm = -INFINITY, ll = 0.f;
                 float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
                 for (int w = w0; w < 4; w += side) mm = fmaxf(mm, end_ml[w][r8].x);
@@ -851,7 +986,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlo
                     x.w += y.w * f;
                 }
                 if (b_first == b_last) {
-                    const int t = (int)fdiv((uint32_t)r, p.f_g), qh = h * p.g + r - t * p.g;
+                    const int qh = h * p.g + hq;
                     const float inv = ll == 0.f ? 0.f : vs / ll;
                     *reinterpret_cast<uint2*>(p.O + get.b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + d0) =
                         make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
@@ -879,13 +1014,13 @@ __host__ __device__ inline bool parts_to_join(int first, int last, int blocks) {
 // Adds the parts of one row of an item that several blocks share; block.x = the item, block.y = the row, a thread one dim.
 // A row has at most as many parts as the grid has blocks: their bases and sums are read by all threads at once, and the first
 // values of O beside them, so that two dependent reads are all the latency there is.
-template <int D>
+template <int D, bool SEL = false>
 __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ DecodeParams p, int MB, int part_rows) {
     constexpr int AHEAD = 8;
     const int rb = blockIdx.x % p.row_blocks, u = blockIdx.x / p.row_blocks, h = u % p.c.Hkv, b = u / p.c.Hkv;
     const int rl = blockIdx.y, r = rb * MB + rl, tid = threadIdx.x;
     after_previous_kernel();
-    if (r >= new_rows(p.c, b) * p.g) return;
+    if (SEL ? rb / p.head_blocks >= new_rows(p.c, b) || rb % p.head_blocks * MB + rl >= p.g : r >= new_rows(p.c, b) * p.g) return;
     const int2 blocks = p.item_blocks[blockIdx.x];
     if (!parts_to_join(blocks.x, blocks.y, p.blocks)) return;
     __shared__ float weight[kDecMaxBlocks];
@@ -924,7 +1059,7 @@ __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ 
         if (k < n) o += ahead[k] * weight[k];
 #pragma unroll 8
     for (int k = AHEAD; k < n; ++k) o += p.part_o[at(k) * D + tid] * weight[k];
-    const int t = (int)fdiv((uint32_t)r, p.f_g), qh = h * p.g + r - t * p.g;
+    const int t = SEL ? rb / p.head_blocks : (int)fdiv((uint32_t)r, p.f_g), qh = h * p.g + (SEL ? rb % p.head_blocks * MB + rl : r - t * p.g);
     p.O[b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + tid] = __float2bfloat16(l == 0.f ? 0.f : o / l);
     if (tid == 0) p.LSE[((long long)b * p.Hq + qh) * p.c.Lq + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }

@@ -13,12 +13,14 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include "block_kernels.cuh"
 #include "bwd_kernels.cuh"
 #include "decode_kernels.cuh"
 #include "decode_rows_kernels.cuh"
 #include "evict_kernels.cuh"
 #include "fwd_kernel.cuh"
 #include "mask.cuh"
+#include "pages_kernels.cuh"
 #include "prefill_kernels.cuh"
 #include "retrieval_kernels.cuh"
 #include "rope_kernels.cuh"
@@ -376,6 +378,7 @@ segattn_status seg_attn_count_pairs(const seg_attn_params* p, const uint8_t* hea
 #include "seg_attn_prefill_api.inc"
 #include "seg_attn_rope_api.inc"
 #include "seg_attn_paged_api.inc"
+#include "seg_attn_blocks_api.inc"
 
 // ---- Self-test of the bounded waits ------------------------------------------------------------
 namespace {

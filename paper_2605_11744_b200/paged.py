@@ -9,7 +9,9 @@ A cache is described by the same tensors in every call:
 ``kv_len``                int32 ``[B]``: rows of every sequence, the call's new ones included
 ``q_len``                 int32 ``[B]`` or None: how many of the ``Lq`` rows given are there (the first ones); None: all
 ``pos_shift``             int32 ``[B]`` or None: rows that evictions have taken out (global position = slot + shift)
-``k_scale``, ``v_scale``  fp32 ``[Hkv]``, for an 8-bit cache only (where its values are read or written)
+``k_scale``, ``v_scale``  for an 8-bit cache only (where its values are read or written): fp32 ``[Hkv]``, or a scale for each
+                          block of rows and head, ``[n_pages, page_size / rows, Hkv]`` with 16, 32, 64 or 128 rows to a block
+                          (any strides), which ``kv_append`` then finds and writes itself
 
 Lengths stay on the device, so that a decoding step can be captured in a CUDA graph and replayed as they grow.
 """
@@ -26,6 +28,8 @@ from .binding import SegAttnError, _mask_arr, lib
 _CACHE = struct.Struct("8i2P6q6P")     # seg_kv_cache
 _STRIDE3 = struct.Struct("3q")
 _SCALING = struct.Struct("i4x6d")      # seg_rope_scaling
+_SCALES = struct.Struct("2P6qi4x")     # seg_block_scales
+_CHOICE = struct.Struct("P2i")         # seg_block_choice
 _LAYOUTS = {"half": 0, "interleaved": 1}
 _KINDS = {"plain": 0, "linear": 1, "by_parts": 2}
 _BF16, _E4M3, _I32, _F32 = torch.bfloat16, torch.float8_e4m3fn, torch.int32, torch.float32
@@ -138,6 +142,28 @@ def _cache(K, V, block_table, kv_len, q_len, pos_shift, k_scale, v_scale, reads_
     return c, B, Hkv, d, page, table[1], dev
 
 
+def _block_scales(k_scale, v_scale, K, dev: int):
+    """seg_block_scales of scales [n_pages, page_size / rows, Hkv] as bytes; None for scales of another form (one to a head, none).
+    `v_scale` may be K's where V is not read."""
+    if k_scale is None or k_scale.dim() != 3:
+        return None
+    shape, pages = k_scale.shape, K.shape
+    for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+        if t is None or t.dtype is not _F32 or t.get_device() != dev or t.shape != shape:
+            raise ValueError("%s must be an fp32 tensor [n_pages, blocks of a page, Hkv] on CUDA device %d" % (what, dev))
+    if K.dtype is not _E4M3 or len(pages) != 4 or shape[0] != pages[0] or shape[2] != pages[2] or shape[1] < 1 or pages[1] % shape[1]:
+        raise ValueError("scales of blocks belong to an 8-bit cache: [n_pages, page_size / rows, Hkv] of its pages")
+    return _SCALES.pack(k_scale.data_ptr(), v_scale.data_ptr(), *k_scale.stride(), *v_scale.stride(), pages[1] // shape[1])
+
+
+def _scaled_cache(K, V, block_table, kv_len, q_len, pos_shift, k_scale, v_scale):
+    """_cache, and seg_block_scales of its scales or None."""
+    sc = _block_scales(k_scale, v_scale, K, K.get_device())
+    if sc is None:
+        return _cache(K, V, block_table, kv_len, q_len, pos_shift, k_scale, v_scale), None
+    return _cache(K, V, block_table, kv_len, q_len, pos_shift, None, None, reads_values=False), sc
+
+
 def _pages(t, B, what: str, dev: int):
     """(B, entries of a row, elements between rows) of a table of page numbers."""
     if t.dtype is not _I32 or t.get_device() != dev or t.dim() != 2 or (B is not None and t.shape[0] != B):
@@ -208,8 +234,9 @@ def kv_append(K_new, V_new, K_pages, V_pages, block_table, kv_len, table: Option
               v_scale=None, stream=None):
     """New rows K_new, V_new [B, Lq, Hkv, d] into the cache; with a table the keys, and the queries Q [B, Lq, Hq, d] if given,
     are rotated at their positions - the C entry point `seg_kv_append`.  Returns the rotated queries (q_out, which may be Q),
-    or None.  kv_len counts the new rows already."""
-    c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, q_len, pos_shift, k_scale, v_scale)
+    or None.  kv_len counts the new rows already.  With scales [n_pages, page_size / rows, Hkv] those of the blocks written into are
+    set, or raised with the rows that such a block has already - the C entry point `seg_blocks_append`."""
+    (c, B, Hkv, d, _, _, dev), sc = _scaled_cache(K_pages, V_pages, block_table, kv_len, q_len, pos_shift, k_scale, v_scale)
     if K_new.dim() != 4:
         raise ValueError("K_new and V_new must be [B, Lq, Hkv, d]")
     Lq = K_new.shape[1]
@@ -230,22 +257,28 @@ def kv_append(K_new, V_new, K_pages, V_pages, block_table, kv_len, table: Option
             raise ValueError("a rotation in place needs the strides of Q")
     elif q_out is not None:
         raise ValueError("q_out needs Q")
-    _call(dev, stream, lib().seg_kv_append, "seg_kv_append", c, Lq, K_new.data_ptr(), kn, V_new.data_ptr(), vn, Hq, _p(Q), qs,
-          _p(q_out), qo, _p(table), n_pos, rot, _layout(layout))
+    args = (Lq, K_new.data_ptr(), kn, V_new.data_ptr(), vn, Hq, _p(Q), qs, _p(q_out), qo, _p(table), n_pos, rot, _layout(layout))
+    if sc is None:
+        _call(dev, stream, lib().seg_kv_append, "seg_kv_append", c, *args)
+    else:
+        _call(dev, stream, lib().seg_blocks_append, "seg_blocks_append", c, sc, *args)
     return q_out
 
 
 @_on_stream
 def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, head_past_mask=None, sm_scale: Optional[float] = None,
                     q_len=None, pos_shift=None, k_scale=None, v_scale=None, weights=None, weights_out=None, out=None, lse=None,
-                    workspace: Optional[torch.Tensor] = None, stream=None):
+                    workspace: Optional[torch.Tensor] = None, blocks: Optional[torch.Tensor] = None, block: int = 0, stream=None):
     """O [B, Lq, Hq, d] bf16 and LSE [B, Hq, Lq] fp32 of the newest rows Q over the cache that holds their keys - the C entry
     point `seg_attn_decode`: row t of sequence b stands at slot kv_len - q_len + t and sees what seg_attn_fwd would show it
     (segments of S, tail T, one head class per KV head).  weights_out [B, Hkv, W] fp32, W >= max_pages * page_size, takes
     every slot's attention weight summed over the rows and query heads of its KV head, added to `weights` if given (which may
     be the same tensor).  Rows from q_len on, in O and in LSE, are left as they were.
-    `out` may be Q, except with weights_out and more than 32 rows to a KV head (Hq/Hkv * Lq) of a bf16 cache."""
-    c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, q_len, pos_shift, k_scale, v_scale)
+    `out` may be Q, except with weights_out and more than 32 rows to a KV head (Hq/Hkv * Lq) of a bf16 cache.
+    `blocks` (int32 [B, Lq, Hkv, n], n <= 128, as blocks_select makes it: ascending, then -1) names blocks of `block` slots: of what lies
+    in front of its segment's tail a head with its past then reads those alone - the C entry point `seg_attn_decode_blocks`, as
+    with scales [n_pages, page_size / rows, Hkv].  No weights_out then."""
+    (c, B, Hkv, d, _, _, dev), sc = _scaled_cache(K_pages, V_pages, block_table, kv_len, q_len, pos_shift, k_scale, v_scale)
     if Q.dim() != 4:
         raise ValueError("Q must be [B, Lq, Hq, d]")
     Lq, Hq = Q.shape[1], Q.shape[2]
@@ -266,15 +299,24 @@ def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, he
             _flat(weights, _F32, (B, Hkv, W), "weights", dev)
     elif weights is not None:
         raise ValueError("weights are added to in weights_out: pass that too (it may be the same tensor)")
+    choice = None
+    if blocks is not None:
+        n = blocks.shape[-1] if blocks.dim() == 4 else 0
+        choice = _CHOICE.pack(_flat(blocks, _I32, (B, Lq, Hkv, n), "blocks", dev).data_ptr(), n, block)
     L = lib()
+    plain = sc is None and choice is None
     if workspace is None:
-        need = L.seg_attn_decode_workspace_bytes(c, Lq, Hq, 0 if weights_out is None else 1)
+        w = 0 if weights_out is None else 1
+        need = L.seg_attn_decode_workspace_bytes(c, Lq, Hq, w) if plain else L.seg_attn_decode_blocks_workspace_bytes(c, sc, choice, Lq, Hq, w)
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=Q.device)
     elif workspace.get_device() != dev:
         raise ValueError("workspace must be on the cache's device")
-    _call(dev, stream, L.seg_attn_decode, "seg_attn_decode", c, Lq, Hq, S, T, d ** -0.5 if sm_scale is None else sm_scale,
-          _mask_bytes(head_past_mask, Hkv), Q.data_ptr(), qs, out.data_ptr(), os_, lse.data_ptr(), _p(weights), _p(weights_out), W,
-          workspace.data_ptr(), workspace.nbytes)
+    args = (Lq, Hq, S, T, d ** -0.5 if sm_scale is None else sm_scale, _mask_bytes(head_past_mask, Hkv), Q.data_ptr(), qs, out.data_ptr(),
+            os_, lse.data_ptr(), _p(weights), _p(weights_out), W, workspace.data_ptr(), workspace.nbytes)
+    if plain:
+        _call(dev, stream, L.seg_attn_decode, "seg_attn_decode", c, *args)
+    else:
+        _call(dev, stream, L.seg_attn_decode_blocks, "seg_attn_decode_blocks", c, sc, choice, *args)
     return out, lse
 
 
