@@ -464,7 +464,7 @@ segattn_status seg_blocks_append(const seg_kv_cache* c, const seg_block_scales* 
  * keys score highest against the query, found when the token is decoded.  (seg_retrieval_select is the paper's own operator, for a
  * segment at a time over keys that lie in one piece; this one is for rows of the paged cache, each with a choice of its own.)
  * Blocks are `block` slots (16, 32, 64 or 128; a divisor of page_size), block j the slots [j block, (j + 1) block) of a sequence.
- *   means   of a full block's keys: with m = their mean in double, rounded to fp32, and scale = max |m| / 127 (fp32), q = m / scale
+ *   means   of a full block's keys: with m = their mean in double, rounded to fp32, and scale = max |m| times 1/127 (in fp32), q = m / scale
  *           (fp32) rounded to the nearest integer.  A block with an infinite or NaN mean gets q = 0 and a NaN scale.
  *           q is int8 contiguous [n_pages][page_size / block][Hkv][d], 16-byte aligned, scale fp32 [n_pages][page_size / block][Hkv]. */
 typedef struct {
@@ -477,7 +477,7 @@ typedef struct {
 segattn_status seg_blocks_summarise(const seg_kv_cache* c, const seg_block_scales* scales, int32_t Lq, const seg_block_means* means, void* stream);
 /* The choice of each new row t and KV head.  For a head of class PAST, with lo the lowest slot that a head of class LOCAL would show
  * the row (seg_attn_decode), blocks j < R = lo / block (rounded down) are to choose from.  The query: the head's query heads summed in
- * double, rounded to fp32 (s), step = max |s| / 127, p = s / step rounded to the nearest integer (0 where s is not finite); block j scores
+ * double, rounded to fp32 (s), step = max |s| times 1/127, p = s / step rounded to the nearest integer (0 where s is not finite); block j scores
  * (float)(sum over p_i q_ji) * scale_j, exact but for that product.  The blocks below `sink` are chosen in any case, and of the others those of the
  * largest scores (equal: lower block; NaN lowest): n together, or all R where there are no more.
  *   idx   int32 contiguous [B][Lq][Hkv][n]: ascending, then -1; all -1 for heads of other classes.  Rows t >= q_len[b] are left as they were.

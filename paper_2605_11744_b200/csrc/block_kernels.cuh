@@ -193,6 +193,8 @@ __global__ void __launch_bounds__(256) append_blocks_kernel(const __grid_constan
     }
 }
 
+constexpr float kOver127 = 1.f / 127.f;  // steps are max / 127 as the product with this number, rounded
+
 // ---- means of blocks --------------------------------------------------------------------------------------------------
 struct SummariseParams {
     PagedView c;
@@ -205,14 +207,21 @@ struct SummariseParams {
     int log, per_page;          // log2 of a block's rows; blocks of a page
 };
 
-// One thread block takes one head's block of rows, if the new rows have filled it: the mean of its keys, in 64 bits from whole
-// products, so that the order of the sum does not show; then c = max |mean| / 127 and the mean in steps of c.
+// A bf16 number times 2^-896, as the upper half of a double: its exponent and mantissa bits where a double has them.  (An infinity or
+// a NaN comes out as a number: they are looked for apart.)
+__device__ __forceinline__ double bf16_in_double(uint32_t b) { return __hiloint2double((int)((b & 0x8000u) << 16 | (b & 0x7fffu) << 13), 0); }
+
+// One thread block takes one head's block of rows, if the new rows have filled it, a warp 16 of them (which have one scale): the mean
+// of its keys in double, then c = max |mean| / 127 and the mean in steps of c.  HBM is to bound it, so a value costs few
+// instructions and hardly any of them in double precision, where a conversion alone takes the time of a dozen others: values of an 8-bit
+// cache are multiples of 2^-9, of which a thread adds up a few in fp32 and a warp 16 rows of them in integers, exactly; bf16 numbers
+// are put into doubles bit by bit.
 template <int D, bool FP8>
-__global__ void __launch_bounds__(128) summarise_kernel(const SummariseParams p) {
-    constexpr int PER = FP8 ? 16 : 8, T = D / PER, RP = 128 / T;  // values of a thread, threads to a row, rows at a time
-    __shared__ double part[RP][D];
-    __shared__ float red[4];
-    const int tid = threadIdx.x;
+__global__ void __launch_bounds__(256) summarise_kernel(const __grid_constant__ SummariseParams p) {
+    constexpr int PER = FP8 ? 16 : 8, T = D / PER, RW = 32 / T, ROWS = 16 / RW;  // values of a thread's piece, lanes to a row, rows at a time, of a thread
+    __shared__ double part[8][D];
+    __shared__ uint32_t red[8];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = 2 << p.log, warps = threads / 32;
     const uint32_t bk = fdiv(blockIdx.x, p.f_heads), b = fdiv(bk, p.f_blocks);
     const int h = (int)(blockIdx.x - bk * p.f_heads.d), k = (int)(bk - b * p.f_blocks.d);
     const int rows = new_rows(p.c, b), n = seq_len(p.c, b);
@@ -222,55 +231,109 @@ __global__ void __launch_bounds__(128) summarise_kernel(const SummariseParams p)
     int prow;
     const int page = page_of(p.c, b, start, &prow);
     if (page < 0) return;
-    const int c = tid % T, r = tid / T;
-    const char* src = p.c.K + page * p.c.k_stride[0] + prow * p.c.k_stride[1] + h * p.c.k_stride[2] + c * 16;
-    double sum[PER];
+    const int c = lane % T, r = warp * 16 + lane / T * ROWS;
+    const char* src = p.c.K + page * p.c.k_stride[0] + (prow + r) * p.c.k_stride[1] + h * p.c.k_stride[2] + c * 16;
+    uint4 v[ROWS];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) sum[e] = 0.0;
-#pragma unroll 4
-    for (int row = r; row < 1 << p.log; row += RP) {
-        const uint4 v = *reinterpret_cast<const uint4*>(src + row * p.c.k_stride[1]);
-        if (FP8) {
-            const double s = p.ks[page * p.ks_stride[0] + ((prow + row) >> p.ks_log) * p.ks_stride[1] + h * p.ks_stride[2]];
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    for (int i = 0; i < ROWS; ++i) v[i] = *reinterpret_cast<const uint4*>(src + i * p.c.k_stride[1]);
+    bool odd = false;  // an infinity or a NaN among the values
+    // The lanes of a row's piece halve their values at every step: what they keep, they add up.
+    constexpr int KEEP = PER / RW;
+    double mine[KEEP];
+    int dim = c * PER;
+    if (FP8) {
+        const double scale = (double)p.ks[page * p.ks_stride[0] + ((prow + warp * 16) >> p.ks_log) * p.ks_stride[1] + h * p.ks_stride[2]] * 0.001953125;
+        float sum[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 uint32_t lo, hi;
                 e4m3x4_to_half(w[q], lo, hi);
                 const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo)), y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                sum[(4 * q) % PER] += s * x.x;
-                sum[(4 * q + 1) % PER] += s * x.y;
-                sum[(4 * q + 2) % PER] += s * y.x;
-                sum[(4 * q + 3) % PER] += s * y.y;
+                sum[4 * q] += x.x;
+                sum[4 * q + 1] += x.y;
+                sum[4 * q + 2] += y.x;
+                sum[4 * q + 3] += y.y;
             }
-        } else {
-            float x[8];
-            unpack8(v, x);
+        }
+        int t[16];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += x[e];
+        for (int e = 0; e < 16; ++e) {
+            odd |= sum[e] != sum[e];
+            t[e] = __float2int_rn(sum[e] * 512.f);
+        }
+#pragma unroll
+        for (int half = 8, x = T; half >= KEEP; half >>= 1, x <<= 1) {
+            const bool upper = lane & x;
+            if (upper) dim += half;
+#pragma unroll
+            for (int e = 0; e < half; ++e) {
+                const int give = upper ? t[e] : t[e + half], keep = upper ? t[e + half] : t[e];
+                t[e] = keep + __shfl_xor_sync(0xffffffffu, give, x);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < KEEP; ++e) mine[e] = scale * (double)t[e];
+    } else {
+        double sum[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = 0.0;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                odd |= (w[q] & 0x7f80u) == 0x7f80u || (w[q] & 0x7f800000u) == 0x7f800000u;
+                sum[(2 * q) % PER] += bf16_in_double(w[q] & 0xffffu);
+                sum[(2 * q + 1) % PER] += bf16_in_double(w[q] >> 16);
+            }
+        }
+#pragma unroll
+        for (int half = 4, x = T; half >= KEEP; half >>= 1, x <<= 1) {
+            const bool upper = lane & x;
+            if (upper) dim += half;
+#pragma unroll
+            for (int e = 0; e < half; ++e) {
+                const double give = upper ? sum[e] : sum[e + half], keep = upper ? sum[e + half] : sum[e];
+                sum[e] = keep + __shfl_xor_sync(0xffffffffu, give, x);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < KEEP; ++e) mine[e] = sum[e % 8];
+    }
+#pragma unroll
+    for (int e = 0; e < KEEP; ++e) part[warp][dim + e] = mine[e];
+    const bool any_odd = __syncthreads_or(odd);
+    float mean[D / 32];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+        const int x = tid + i * threads;
+        if (x < D) {
+            double all = 0.0;
+            for (int w = 0; w < warps; ++w) all += part[w][x];
+            if (!FP8) all *= __hiloint2double((1023 + 896) << 20, 0);
+            mean[i] = (float)(all / (double)(1 << p.log));
+            most = max(most, __float_as_uint(fabsf(mean[i])));
         }
     }
-#pragma unroll
-    for (int e = 0; e < PER; ++e) part[r][c * PER + e] = sum[e];
-    __syncthreads();
-    float mean = 0.f;
-    if (tid < D) {
-        double all = 0.0;
-#pragma unroll
-        for (int k2 = 0; k2 < RP; ++k2) all += part[k2][tid];
-        mean = (float)(all / (double)(1 << p.log));
-    }
-    // |mean| as bits, so that an infinity or a NaN among them is the largest
-    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(mean)));
-    if ((tid & 31) == 0) red[tid >> 5] = __uint_as_float(most);
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) red[warp] = most;
     __syncthreads();
     uint32_t top = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) top = max(top, __float_as_uint(red[w]));
-    const bool fine = top < 0x7f800000u;
-    const float step = fine ? __fdiv_rn(__uint_as_float(top), 127.f) : __uint_as_float(0x7fffffffu);
+    for (int w = 0; w < warps; ++w) top = max(top, red[w]);
+    const bool fine = top < 0x7f800000u && !any_odd;
+    const float step = fine ? __fmul_rn(__uint_as_float(top), kOver127) : __uint_as_float(0x7fffffffu);
     const long long at = ((long long)page * p.per_page + (prow >> p.log)) * p.c.Hkv + h;
-    if (tid < D) p.sums[at * D + tid] = fine && step > 0.f ? (int8_t)__float2int_rn(__fdiv_rn(mean, step)) : (int8_t)0;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+        const int x = tid + i * threads;
+        if (x < D) p.sums[at * D + x] = fine && step > 0.f ? (int8_t)__float2int_rn(__fdiv_rn(mean[i], step)) : (int8_t)0;
+    }
     if (tid == 0) p.sum_scale[at] = step;
 }
 
@@ -284,13 +347,14 @@ struct SelectParams {
     int32_t* idx;               // [B][Lq][Hkv][n]
     FastDiv f_S;
     int S, T, g, n, sink, log, per_page, keys;
-    uint8_t head_class[64];
+    int n_past;                 // heads with a past
+    uint8_t heads[64];          // those, then the others
 };
 
 constexpr int kSelThreads = 512;
 constexpr int kSelBins = 2048;
 constexpr int kSelKeys = 49152;  // blocks that a thread block has room for
-constexpr int kSelSlice = 4096;  // blocks that a thread block of a cluster has at least
+constexpr int kSelSlice = 1024;  // blocks that a thread block of a cluster has at least
 
 // The lowest slot that a row at `slot` sees whole through a head with a past: its tail's start, rounded down to a block.
 __device__ __forceinline__ int whole_from(const SelectParams& p, int slot, int shift) {
@@ -299,7 +363,16 @@ __device__ __forceinline__ int whole_from(const SelectParams& p, int slot, int s
     return (int)max(0ll, max(0ll, start - p.T) - shift) >> p.log << p.log;
 }
 
-// A cluster takes one (new row, KV head).  The query, summed over the head's query heads and brought to 8 bits, against the means
+// Lists of row t of sequence b for the heads from p.heads[from] on: no blocks.
+__device__ __forceinline__ void no_choice(const SelectParams& p, int bt, int from, int tid, int step) {
+    for (int i = tid; i < (p.c.Hkv - from) * p.n; i += step) p.idx[((long long)bt * p.c.Hkv + p.heads[from + i / p.n]) * p.n + i % p.n] = -1;
+}
+__global__ void __launch_bounds__(128) no_choice_kernel(const __grid_constant__ SelectParams p) {
+    const int b = blockIdx.x / p.c.Lq, t = blockIdx.x - b * p.c.Lq;
+    if (t < new_rows(p.c, b)) no_choice(p, blockIdx.x, 0, threadIdx.x, 128);
+}
+
+// A cluster takes one (new row, KV head with a past).  The query, summed over the head's query heads and brought to 8 bits, against the means
 // of the blocks before the row's tail: integer products, so that a score is the same in whatever order it is added up; then the n
 // largest by a radix selection (evict_select_kernel's, with the sums over the cluster's blocks through distributed shared memory)
 // and their numbers in ascending order.
@@ -313,22 +386,28 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
     __shared__ uint32_t red[kSelThreads / 32], seg_gt[kSelThreads / 32], seg_eq[kSelThreads / 32], found[2], totals[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int CS = (int)cluster_size(), rank = (int)cluster_rank(), unit = blockIdx.x / CS;
-    const int h = unit % p.c.Hkv, bt = unit / p.c.Hkv, b = bt / p.c.Lq, t = bt - b * p.c.Lq;
-    const int rows = new_rows(p.c, b);
+    const int which = unit % p.n_past, h = p.heads[which], bt = unit / p.n_past, b = bt / p.c.Lq, t = bt - b * p.c.Lq;
+    const int rows = new_rows(p.c, b), n = seq_len(p.c, b), shift = shift_of(p.c, b);
     if (t >= rows) return;
-    int32_t* out = p.idx + (long long)unit * p.n;
-    const int slot = seq_len(p.c, b) - rows + t;
-    const int m = p.head_class[h] == kHeadPast && slot >= 0 ? whole_from(p, slot, shift_of(p.c, b)) >> p.log : 0;  // blocks to choose from
+    int32_t* out = p.idx + ((long long)bt * p.c.Hkv + h) * p.n;
+    if (which == 0) no_choice(p, bt, p.n_past, rank * kSelThreads + tid, CS * kSelThreads);
+    const int slot = n - rows + t;
+    const int m = slot >= 0 ? whole_from(p, slot, shift) >> p.log : 0;  // blocks to choose from
     if (m <= p.n) {
         for (int i = rank * kSelThreads + tid; i < p.n; i += CS * kSelThreads) out[i] = i < m ? i : -1;
         return;
     }
+
+    // this block's slice, and the pages of its blocks (in the keys' place until the scores take it)
+    const int slice = (((m + CS - 1) / CS + 31) & ~31), j0 = min(rank * slice, m), cnt = min(slice, m - j0);
+    for (int i = tid; i < cnt; i += kSelThreads) keys[i] = (uint32_t)table_entry(p.c, b, (j0 + i) << p.log);
 
     // the query
     float q = 0.f;
     if (tid < D) {
         double sum = 0.0;
         const __nv_bfloat16* at = p.Q + b * p.q_stride[0] + t * p.q_stride[1] + (long long)h * p.g * p.q_stride[2] + tid;
+#pragma unroll 8
         for (int x = 0; x < p.g; ++x) sum += (double)__bfloat162float(at[x * p.q_stride[2]]);
         q = (float)sum;
     }
@@ -337,31 +416,29 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
     for (int i = tid; i < 3 * kSelBins; i += kSelThreads) hist[i] = 0;
     __syncthreads();
     const uint32_t top = __reduce_max_sync(0xffffffffu, lane < D / 32 ? red[lane] : 0u);
-    const float step = __fdiv_rn(__uint_as_float(top), 127.f);
+    const float step = __fmul_rn(__uint_as_float(top), kOver127);
     if (tid < D) query[tid] = top > 0 && top < 0x7f800000u && step > 0.f ? (int8_t)__float2int_rn(__fdiv_rn(q, step)) : (int8_t)0;
     __syncthreads();
     const uint4 q16 = *reinterpret_cast<const uint4*>(query + lane % T * 16);
 
-    // the scores of this block's slice, as unsigned numbers of the same order
-    const int slice = (((m + CS - 1) / CS + 31) & ~31), j0 = min(rank * slice, m), cnt = min(slice, m - j0);
-    constexpr int AHEAD = 4;
-    for (int i0 = warp * PW * AHEAD; i0 < cnt; i0 += kSelThreads / 32 * PW * AHEAD) {
+    // the scores, as unsigned numbers of the same order: every load of a warp's next 8 PW means in flight before the first product
+    constexpr int AHEAD = 8, STEP = kSelThreads / 32 * PW * AHEAD;
+    for (int i0 = warp * PW * AHEAD; i0 < cnt; i0 += STEP) {
         uint4 k16[AHEAD];
         float sc[AHEAD];
 #pragma unroll
         for (int y = 0; y < AHEAD; ++y) {
             const int i = i0 + y * PW + lane / T;
+            const uint32_t page = i < cnt ? keys[i] : 0xffffffffu;
             k16[y] = make_uint4(0, 0, 0, 0);
-            sc[y] = 0.f;
-            if (i < cnt) {
-                int prow;
-                const int page = page_of(p.c, b, (j0 + i) << p.log, &prow);
-                sc[y] = __uint_as_float(0x7fffffffu);  // of a page that is not there: lowest
-                if (page >= 0) {
-                    const long long at = ((long long)page * p.per_page + (prow >> p.log)) * p.c.Hkv + h;
-                    k16[y] = *reinterpret_cast<const uint4*>(p.sums + at * D + lane % T * 16);
-                    sc[y] = p.sum_scale[at];
-                }
+            sc[y] = __uint_as_float(0x7fffffffu);  // of a page that is not there: lowest
+            if (page < (uint32_t)p.c.n_pages) {
+                const int prow = row_in_page(p.c, (j0 + i) << p.log) >> p.log;
+                const long long at = ((long long)page * p.per_page + prow) * p.c.Hkv + h;
+                k16[y] = *reinterpret_cast<const uint4*>(p.sums + at * D + lane % T * 16);
+                sc[y] = p.sum_scale[at];
+            } else if (i < cnt) {
+                refuse_input(33);
             }
         }
 #pragma unroll

@@ -91,7 +91,7 @@ def means(x, block):
         m = (x.sum(0) / block).astype(np.float32)
         top = np.abs(m).max(-1)
         fine = np.isfinite(m).all(-1)
-        scale = np.where(fine, top / np.float32(127), np.float32(np.nan)).astype(np.float32)
+        scale = np.where(fine, top * (np.float32(1) / np.float32(127)), np.float32(np.nan)).astype(np.float32)
         q = np.where((fine & (scale > 0))[:, None], np.rint(m / scale[:, None]), 0)
     return np.nan_to_num(q, nan=0.0).astype(np.int8), scale
 
@@ -115,7 +115,7 @@ def select(Q, sums, scale, table, n, q_len, S, T, mask, page, block, count, sink
                 continue
             s = Q[t, h * g:(h + 1) * g].sum(0).astype(np.float32)
             top = np.abs(s).max()
-            step = top / np.float32(127)
+            step = top * (np.float32(1) / np.float32(127))
             p = np.rint(s / step).astype(np.int64) if np.isfinite(top) and step > 0 else np.zeros(len(s), np.int64)
             j = np.arange(room)
             pg = np.asarray(table)[j * block // page]
