@@ -433,7 +433,8 @@ segattn_status seg_kv_evict(const seg_kv_cache* c, const float* weights, int32_t
  * A sequence grows by at most Lq rows.  One out of range (want < 0 or past max_pages * page_size, a larger growth, a kv_len out of
  * range) stays as it is, a free_count outside [0, n_pages] is cut, a page number outside [0, n_pages) comes out as -1 in the table
  * and the slots: each makes the next seg_attn_poll_status return SEGATTN_ERR_INVALID.  B <= 65535, max_pages * page_size <= 2^30.
- * `workspace`: DEVICE, 256-byte aligned, seg_pages_workspace_bytes(B) bytes (0: invalid B), scratch.  One or two kernels. */
+ * `workspace`: DEVICE, 256-byte aligned, seg_pages_workspace_bytes(B) bytes (0: invalid B), scratch; not looked at, and may be NULL,
+ * where B <= 1024 and B * Lq <= 4096 (one kernel; two elsewhere). */
 size_t seg_pages_workspace_bytes(int32_t B);
 segattn_status seg_pages_resize(int32_t B, int32_t Lq, int32_t page_size, int32_t n_pages, const int32_t* want, int32_t* block_table,
                                 int32_t max_pages, int32_t table_stride, const int32_t* kv_len, const int32_t* pos_shift,

@@ -39,18 +39,21 @@ def pages_resize(want, block_table, kv_len, free_pages, free_count, page_size: i
     _flat(free_count, _I32, (1,), "free_count", dev)
     if pos_shift is not None:
         _flat(pos_shift, _I32, (B,), "pos_shift", dev)
-    new = lambda given, kind, shape, what: torch.empty(shape, dtype=kind, device=want.device) if given is None else _flat(given, kind, shape, what, dev)  # noqa: E731
-    kv_len_out, free_count_out = new(kv_len_out, _I32, (B,), "kv_len_out"), new(free_count_out, _I32, (1,), "free_count_out")
-    q_len = new(q_len, _I32, (B,), "q_len")
-    slots, positions = new(slots, torch.int64, (B, max(Lq, 0)), "slots"), new(positions, _I32, (B, max(Lq, 0)), "positions")
+    kv_len_out = torch.empty_like(kv_len) if kv_len_out is None else _flat(kv_len_out, _I32, (B,), "kv_len_out", dev)
+    free_count_out = torch.empty_like(free_count) if free_count_out is None else _flat(free_count_out, _I32, (1,), "free_count_out", dev)
+    q_len = torch.empty_like(kv_len) if q_len is None else _flat(q_len, _I32, (B,), "q_len", dev)
+    rows = (B, max(Lq, 0))
+    slots = want.new_empty(rows, dtype=torch.int64) if slots is None else _flat(slots, torch.int64, rows, "slots", dev)
+    positions = want.new_empty(rows) if positions is None else _flat(positions, _I32, rows, "positions", dev)
     L = lib()
     if workspace is None:
-        workspace = torch.empty(max(L.seg_pages_workspace_bytes(B), 256), dtype=torch.uint8, device=want.device)
+        if B > 1024 or B * Lq > 4096:      # smaller calls need none
+            workspace = torch.empty(max(L.seg_pages_workspace_bytes(B), 256), dtype=torch.uint8, device=want.device)
     elif workspace.get_device() != dev:
         raise ValueError("workspace must be on the tables' device")
     _call(dev, stream, L.seg_pages_resize, "seg_pages_resize", B, Lq, page_size, n_pages, want.data_ptr(), block_table.data_ptr(), per, stride,
           kv_len.data_ptr(), _p(pos_shift), free_pages.data_ptr(), free_count.data_ptr(), kv_len_out.data_ptr(), free_count_out.data_ptr(),
-          q_len.data_ptr(), slots.data_ptr(), positions.data_ptr(), workspace.data_ptr(), workspace.nbytes)
+          q_len.data_ptr(), slots.data_ptr(), positions.data_ptr(), _p(workspace), workspace.nbytes if workspace is not None else 0)
     return kv_len_out, free_count_out, q_len, slots, positions
 
 

@@ -116,18 +116,13 @@ __global__ void __launch_bounds__(256) append_blocks_kernel(const __grid_constan
     if (hi - lo < rows && k == 0 && hh == 0 && tid == 0) refuse_input(35);
     const int start = ((lo >> p.log) + k) << p.log, from = max(lo, start), to = (int)min((long long)hi, (long long)start + (1 << p.log));
     if (from >= to) return;
-    int prow;
-    const int page = page_of(a.c, b, start, &prow);
-    if (page < 0) return;
 
+    // the new rows, whose places do not depend on the page: on their way while it is looked up
     int e0, e1;  // this thread's two halves of a row
     unit_offsets<INTERLEAVED>(u, val ? 0 : a.rot, &e0, &e1);
     const __nv_bfloat16* src = val ? a.Vn + b * a.vn_stride[0] + h * a.vn_stride[2] : a.Kn + b * a.kn_stride[0] + h * a.kn_stride[2];
     const long long src_row = val ? a.vn_stride[1] : a.kn_stride[1], dst_row = val ? a.c.v_stride[1] : a.c.k_stride[1];
     const bool turns = !val && a.table && u * 16 < a.rot;
-    float* scale_at = val ? p.vs + page * p.vs_stride[0] + (prow >> p.log) * p.vs_stride[1] + h * p.vs_stride[2]
-                          : p.ks + page * p.ks_stride[0] + (prow >> p.log) * p.ks_stride[1] + h * p.ks_stride[2];
-    const float old = start < lo ? *scale_at : 0.f;
     uint4 raw[STEPS][2];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
@@ -138,6 +133,12 @@ __global__ void __launch_bounds__(256) append_blocks_kernel(const __grid_constan
             raw[s][1] = *reinterpret_cast<const uint4*>(x + e1);
         }
     }
+    int prow;
+    const int page = page_of(a.c, b, start, &prow);
+    if (page < 0) return;
+    float* scale_at = val ? p.vs + page * p.vs_stride[0] + (prow >> p.log) * p.vs_stride[1] + h * p.vs_stride[2]
+                          : p.ks + page * p.ks_stride[0] + (prow >> p.log) * p.ks_stride[1] + h * p.ks_stride[2];
+    const float old = start < lo ? *scale_at : 0.f;
     float x[STEPS][16], top = 0.f;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
@@ -204,6 +205,7 @@ struct SummariseParams {
     int8_t* sums;               // [n_pages][blocks of a page][Hkv][D]
     float* sum_scale;           // [n_pages][blocks of a page][Hkv]
     FastDiv f_heads, f_blocks;  // Hkv; blocks that the new rows of a sequence can touch
+    uint32_t units;             // B * blocks * Hkv
     int log, per_page;          // log2 of a block's rows; blocks of a page
 };
 
@@ -211,19 +213,27 @@ struct SummariseParams {
 // a NaN comes out as a number: they are looked for apart.)
 __device__ __forceinline__ double bf16_in_double(uint32_t b) { return __hiloint2double((int)((b & 0x8000u) << 16 | (b & 0x7fffu) << 13), 0); }
 
-// One thread block takes one head's block of rows, if the new rows have filled it, a warp 16 of them (which have one scale): the mean
-// of its keys in double, then c = max |mean| / 127 and the mean in steps of c.  HBM is to bound it, so a value costs few
-// instructions and hardly any of them in double precision, where a conversion alone takes the time of a dozen others: values of an 8-bit
-// cache are multiples of 2^-9, of which a thread adds up a few in fp32 and a warp 16 rows of them in integers, exactly; bf16 numbers
-// are put into doubles bit by bit.
+// sum + the two fp16 numbers of a register, exactly as long as the sum has room
+__device__ __forceinline__ void add_halves(float& lo, float& hi, uint32_t x) {
+    asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.f32.f16 %0, a, %0;\n\tadd.f32.f16 %1, b, %1;\n\t}" : "+f"(lo), "+f"(hi) : "r"(x));
+}
+
+// A warp takes one head's block of rows, if the new rows have filled it, 16 rows (which have one scale) at a time: the mean of its
+// keys in double, then c = max |mean| / 127 and the mean in steps of c.  HBM is to bound it, so a value costs few instructions and
+// hardly any of them in double precision, where a conversion alone takes the time of a dozen others: values of an 8-bit cache are
+// multiples of 2^-9, of which a lane adds up 32 at most in fp32, and the lanes their sums as integers, exactly; bf16 numbers are put
+// into doubles bit by bit.
+constexpr int kSumWarps = 8;
 template <int D, bool FP8>
-__global__ void __launch_bounds__(256) summarise_kernel(const __grid_constant__ SummariseParams p) {
-    constexpr int PER = FP8 ? 16 : 8, T = D / PER, RW = 32 / T, ROWS = 16 / RW;  // values of a thread's piece, lanes to a row, rows at a time, of a thread
-    __shared__ double part[8][D];
-    __shared__ uint32_t red[8];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = 2 << p.log, warps = threads / 32;
-    const uint32_t bk = fdiv(blockIdx.x, p.f_heads), b = fdiv(bk, p.f_blocks);
-    const int h = (int)(blockIdx.x - bk * p.f_heads.d), k = (int)(bk - b * p.f_blocks.d);
+__global__ void __launch_bounds__(32 * kSumWarps) summarise_kernel(const __grid_constant__ SummariseParams p) {
+    constexpr int PER = FP8 ? 16 : 8, T = D / PER, RW = 32 / T, ROWS = 16 / RW;  // values of a lane's piece, lanes to a row, rows at a time, of a lane
+    constexpr int KEEP = PER / RW;  // dims a lane has in the end
+    constexpr int AHEAD = 16 / ROWS;  // groups of 16 rows whose loads are in flight together
+    const int lane = threadIdx.x & 31;
+    const uint32_t unit = blockIdx.x * kSumWarps + (threadIdx.x >> 5);
+    if (unit >= p.units) return;
+    const uint32_t bk = fdiv(unit, p.f_heads), b = fdiv(bk, p.f_blocks);
+    const int h = (int)(unit - bk * p.f_heads.d), k = (int)(bk - b * p.f_blocks.d);
     const int rows = new_rows(p.c, b), n = seq_len(p.c, b);
     if (rows == 0) return;
     const int start = ((max(n - rows, 0) >> p.log) + k) << p.log;
@@ -231,110 +241,126 @@ __global__ void __launch_bounds__(256) summarise_kernel(const __grid_constant__ 
     int prow;
     const int page = page_of(p.c, b, start, &prow);
     if (page < 0) return;
-    const int c = lane % T, r = warp * 16 + lane / T * ROWS;
-    const char* src = p.c.K + page * p.c.k_stride[0] + (prow + r) * p.c.k_stride[1] + h * p.c.k_stride[2] + c * 16;
-    uint4 v[ROWS];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) v[i] = *reinterpret_cast<const uint4*>(src + i * p.c.k_stride[1]);
+    const int c = lane % T;
+    const char* src = p.c.K + page * p.c.k_stride[0] + (prow + lane / T * ROWS) * p.c.k_stride[1] + h * p.c.k_stride[2] + c * 16;
+    const float* scale_at = FP8 ? p.ks + page * p.ks_stride[0] + h * p.ks_stride[2] : nullptr;
     bool odd = false;  // an infinity or a NaN among the values
-    // The lanes of a row's piece halve their values at every step: what they keep, they add up.
-    constexpr int KEEP = PER / RW;
     double mine[KEEP];
+#pragma unroll
+    for (int e = 0; e < KEEP; ++e) mine[e] = 0.0;
+    // The lanes with the same piece of different rows halve their values at every step: what they keep, they add up.
     int dim = c * PER;
-    if (FP8) {
-        const double scale = (double)p.ks[page * p.ks_stride[0] + ((prow + warp * 16) >> p.ks_log) * p.ks_stride[1] + h * p.ks_stride[2]] * 0.001953125;
-        float sum[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+    for (int half = PER / 2, x = T; half >= KEEP; half >>= 1, x <<= 1)
+        if (lane & x) dim += half;
+    auto gather = [&](auto& t) {
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint32_t lo, hi;
-                e4m3x4_to_half(w[q], lo, hi);
-                const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo)), y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                sum[4 * q] += x.x;
-                sum[4 * q + 1] += x.y;
-                sum[4 * q + 2] += y.x;
-                sum[4 * q + 3] += y.y;
-            }
-        }
-        int t[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            odd |= sum[e] != sum[e];
-            t[e] = __float2int_rn(sum[e] * 512.f);
-        }
-#pragma unroll
-        for (int half = 8, x = T; half >= KEEP; half >>= 1, x <<= 1) {
+        for (int half = PER / 2, x = T; half >= KEEP; half >>= 1, x <<= 1) {
             const bool upper = lane & x;
-            if (upper) dim += half;
 #pragma unroll
             for (int e = 0; e < half; ++e) {
-                const int give = upper ? t[e] : t[e + half], keep = upper ? t[e + half] : t[e];
+                const auto give = upper ? t[e] : t[e + half], keep = upper ? t[e + half] : t[e];
                 t[e] = keep + __shfl_xor_sync(0xffffffffu, give, x);
             }
         }
+    };
+    auto load = [&](auto& v, int r0) {
 #pragma unroll
-        for (int e = 0; e < KEEP; ++e) mine[e] = scale * (double)t[e];
+        for (int g = 0; g < AHEAD; ++g)
+            if (r0 + 16 * g < 1 << p.log) {
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) v[g][i] = *reinterpret_cast<const uint4*>(src + (r0 + 16 * g + i) * p.c.k_stride[1]);
+            }
+    };
+    if (FP8) {
+        float sum[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+        float scale = scale_at[(prow >> p.ks_log) * p.ks_stride[1]];
+        auto flush = [&]() {
+            int t[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                odd |= sum[e] != sum[e];
+                t[e] = __float2int_rn(sum[e] * 512.f);
+                sum[e] = 0.f;
+            }
+            gather(t);
+#pragma unroll
+            for (int e = 0; e < KEEP; ++e) mine[e] += (double)scale * 0.001953125 * (double)t[e];
+        };
+        for (int r0 = 0; r0 < 1 << p.log; r0 += 16 * AHEAD) {
+            uint4 v[AHEAD][ROWS];
+            float next[AHEAD];
+            load(v, r0);
+#pragma unroll
+            for (int g = 0; g < AHEAD; ++g)
+                if (r0 + 16 * g < 1 << p.log) next[g] = scale_at[((prow + r0 + 16 * g) >> p.ks_log) * p.ks_stride[1]];
+#pragma unroll
+            for (int g = 0; g < AHEAD; ++g) {
+                if (r0 + 16 * g >= 1 << p.log) break;
+                if (__float_as_uint(next[g]) != __float_as_uint(scale)) {
+                    flush();
+                    scale = next[g];
+                }
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    const uint32_t w[4] = {v[g][i].x, v[g][i].y, v[g][i].z, v[g][i].w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t lo, hi;
+                        e4m3x4_to_half(w[q], lo, hi);
+                        add_halves(sum[4 * q], sum[4 * q + 1], lo);
+                        add_halves(sum[4 * q + 2], sum[4 * q + 3], hi);
+                    }
+                }
+            }
+        }
+        flush();
     } else {
         double sum[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] = 0.0;
+        for (int r0 = 0; r0 < 1 << p.log; r0 += 16 * AHEAD) {
+            uint4 v[AHEAD][ROWS];
+            load(v, r0);
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            for (int g = 0; g < AHEAD; ++g) {
+                if (r0 + 16 * g >= 1 << p.log) break;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                odd |= (w[q] & 0x7f80u) == 0x7f80u || (w[q] & 0x7f800000u) == 0x7f800000u;
-                sum[(2 * q) % PER] += bf16_in_double(w[q] & 0xffffu);
-                sum[(2 * q + 1) % PER] += bf16_in_double(w[q] >> 16);
+                for (int i = 0; i < ROWS; ++i) {
+                    const uint32_t w[4] = {v[g][i].x, v[g][i].y, v[g][i].z, v[g][i].w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        odd |= (w[q] & 0x7f80u) == 0x7f80u || (w[q] & 0x7f800000u) == 0x7f800000u;
+                        sum[2 * q] += bf16_in_double(w[q] & 0xffffu);
+                        sum[2 * q + 1] += bf16_in_double(w[q] >> 16);
+                    }
+                }
             }
         }
+        gather(sum);
 #pragma unroll
-        for (int half = 4, x = T; half >= KEEP; half >>= 1, x <<= 1) {
-            const bool upper = lane & x;
-            if (upper) dim += half;
-#pragma unroll
-            for (int e = 0; e < half; ++e) {
-                const double give = upper ? sum[e] : sum[e + half], keep = upper ? sum[e + half] : sum[e];
-                sum[e] = keep + __shfl_xor_sync(0xffffffffu, give, x);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < KEEP; ++e) mine[e] = sum[e % 8];
+        for (int e = 0; e < KEEP; ++e) mine[e] = sum[e] * __hiloint2double((1023 + 896) << 20, 0);
     }
-#pragma unroll
-    for (int e = 0; e < KEEP; ++e) part[warp][dim + e] = mine[e];
-    const bool any_odd = __syncthreads_or(odd);
-    float mean[D / 32];
+    float mean[KEEP];
     uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        const int x = tid + i * threads;
-        if (x < D) {
-            double all = 0.0;
-            for (int w = 0; w < warps; ++w) all += part[w][x];
-            if (!FP8) all *= __hiloint2double((1023 + 896) << 20, 0);
-            mean[i] = (float)(all / (double)(1 << p.log));
-            most = max(most, __float_as_uint(fabsf(mean[i])));
-        }
+    for (int e = 0; e < KEEP; ++e) {
+        mean[e] = (float)(mine[e] * __hiloint2double((1023 - p.log) << 20, 0));  // over a power of two
+        most = max(most, __float_as_uint(fabsf(mean[e])));                       // as bits: an infinity or a NaN is the largest
     }
     most = __reduce_max_sync(0xffffffffu, most);
-    if (lane == 0) red[warp] = most;
-    __syncthreads();
-    uint32_t top = 0;
-    for (int w = 0; w < warps; ++w) top = max(top, red[w]);
-    const bool fine = top < 0x7f800000u && !any_odd;
-    const float step = fine ? __fmul_rn(__uint_as_float(top), kOver127) : __uint_as_float(0x7fffffffu);
+    const bool fine = most < 0x7f800000u && !__any_sync(0xffffffffu, odd);
+    const float step = fine ? __fmul_rn(__uint_as_float(most), kOver127) : __uint_as_float(0x7fffffffu);
     const long long at = ((long long)page * p.per_page + (prow >> p.log)) * p.c.Hkv + h;
+    uint32_t q = 0;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        const int x = tid + i * threads;
-        if (x < D) p.sums[at * D + x] = fine && step > 0.f ? (int8_t)__float2int_rn(__fdiv_rn(mean[i], step)) : (int8_t)0;
-    }
-    if (tid == 0) p.sum_scale[at] = step;
+    for (int e = 0; e < KEEP; ++e) q |= (fine && step > 0.f ? (uint32_t)__float2int_rn(__fdiv_rn(mean[e], step)) & 0xffu : 0u) << (8 * e);
+    int8_t* out = p.sums + at * D + dim;
+    if (KEEP == 4) *reinterpret_cast<uint32_t*>(out) = q;
+    else *reinterpret_cast<uint16_t*>(out) = (uint16_t)q;
+    if (lane == 0) p.sum_scale[at] = step;
 }
 
 // ---- the choice of blocks ---------------------------------------------------------------------------------------------
@@ -353,6 +379,8 @@ struct SelectParams {
 
 constexpr int kSelThreads = 512;
 constexpr int kSelBins = 2048;
+constexpr int kSelFew = 256;              // as many are compared with each other one by one
+constexpr uint32_t kSinkKey = 0xfffffffeu;  // above every score's
 constexpr int kSelKeys = 49152;  // blocks that a thread block has room for
 constexpr int kSelSlice = 1024;  // blocks that a thread block of a cluster has at least
 
@@ -377,13 +405,12 @@ __global__ void __launch_bounds__(128) no_choice_kernel(const __grid_constant__ 
 // largest by a radix selection (evict_select_kernel's, with the sums over the cluster's blocks through distributed shared memory)
 // and their numbers in ascending order.
 template <int D>
-__global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_constant__ SelectParams p) {
-    constexpr int T = D / 16, PW = 32 / T;  // lanes to a mean, means of a warp's load
+__global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_constant__ SelectParams p) {
     extern __shared__ uint32_t sel_smem[];
     uint32_t* hist = sel_smem;                 // [3][kSelBins]
     uint32_t* keys = sel_smem + 3 * kSelBins;  // [p.keys]
     __shared__ __align__(16) int8_t query[D];
-    __shared__ uint32_t red[kSelThreads / 32], seg_gt[kSelThreads / 32], seg_eq[kSelThreads / 32], found[2], totals[2];
+    __shared__ uint32_t red[kSelThreads / 32], seg_gt[kSelThreads / 32], seg_eq[kSelThreads / 32], found[3], totals[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int CS = (int)cluster_size(), rank = (int)cluster_rank(), unit = blockIdx.x / CS;
     const int which = unit % p.n_past, h = p.heads[which], bt = unit / p.n_past, b = bt / p.c.Lq, t = bt - b * p.c.Lq;
@@ -419,39 +446,57 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
     const float step = __fmul_rn(__uint_as_float(top), kOver127);
     if (tid < D) query[tid] = top > 0 && top < 0x7f800000u && step > 0.f ? (int8_t)__float2int_rn(__fdiv_rn(q, step)) : (int8_t)0;
     __syncthreads();
-    const uint4 q16 = *reinterpret_cast<const uint4*>(query + lane % T * 16);
 
-    // the scores, as unsigned numbers of the same order: every load of a warp's next 8 PW means in flight before the first product
-    constexpr int AHEAD = 8, STEP = kSelThreads / 32 * PW * AHEAD;
-    for (int i0 = warp * PW * AHEAD; i0 < cnt; i0 += STEP) {
-        uint4 k16[AHEAD];
-        float sc[AHEAD];
+    // The scores, as unsigned numbers of the same order.  A lane takes a whole mean, with the query in registers: the 32 lines that
+    // a load of the warp touches are all used by the loads beside it, and nothing is left to add up across lanes (eight lanes to a
+    // mean took four times the instructions).
+    constexpr int N16 = D / 16;
+    uint4 q16[N16];
 #pragma unroll
-        for (int y = 0; y < AHEAD; ++y) {
-            const int i = i0 + y * PW + lane / T;
-            const uint32_t page = i < cnt ? keys[i] : 0xffffffffu;
-            k16[y] = make_uint4(0, 0, 0, 0);
-            sc[y] = __uint_as_float(0x7fffffffu);  // of a page that is not there: lowest
-            if (page < (uint32_t)p.c.n_pages) {
-                const int prow = row_in_page(p.c, (j0 + i) << p.log) >> p.log;
-                const long long at = ((long long)page * p.per_page + prow) * p.c.Hkv + h;
-                k16[y] = *reinterpret_cast<const uint4*>(p.sums + at * D + lane % T * 16);
-                sc[y] = p.sum_scale[at];
-            } else if (i < cnt) {
-                refuse_input(33);
+    for (int x = 0; x < N16; ++x) q16[x] = reinterpret_cast<const uint4*>(query)[x];
+    for (int i = tid; i < cnt; i += kSelThreads) {
+        const uint32_t page = keys[i];
+        float score = __uint_as_float(0x7fffffffu);  // of a page that is not there: lowest
+        if (page < (uint32_t)p.c.n_pages) {
+            const long long at = ((long long)page * p.per_page + (row_in_page(p.c, (j0 + i) << p.log) >> p.log)) * p.c.Hkv + h;
+            const uint4* src = reinterpret_cast<const uint4*>(p.sums + at * D);
+            const float scale = p.sum_scale[at];
+            uint4 k16[N16];
+#pragma unroll
+            for (int x = 0; x < N16; ++x) k16[x] = src[x];
+            int s[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int x = 0; x < N16; ++x) {
+                s[0] = __dp4a((int)k16[x].x, (int)q16[x].x, s[0]);
+                s[1] = __dp4a((int)k16[x].y, (int)q16[x].y, s[1]);
+                s[2] = __dp4a((int)k16[x].z, (int)q16[x].z, s[2]);
+                s[3] = __dp4a((int)k16[x].w, (int)q16[x].w, s[3]);
             }
+            score = __fmul_rn((float)(s[0] + s[1] + s[2] + s[3]), scale);
+        } else {
+            refuse_input(33);
         }
-#pragma unroll
-        for (int y = 0; y < AHEAD; ++y) {
-            int s = __dp4a((int)k16[y].x, (int)q16.x, __dp4a((int)k16[y].y, (int)q16.y, __dp4a((int)k16[y].z, (int)q16.z, __dp4a((int)k16[y].w, (int)q16.w, 0))));
-#pragma unroll
-            for (int x = 1; x < T; x <<= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-            const int i = i0 + y * PW + lane / T;
-            if (lane % T == 0 && i < cnt) keys[i] = j0 + i < p.sink ? 0xffffffffu : weight_key(__fmul_rn((float)s, sc[y]));
-        }
+        keys[i] = j0 + i < p.sink ? kSinkKey : weight_key(score);
     }
     __syncthreads();
 
+    // Few of them: a key is chosen if fewer than n are in front of it.  A thread holds one and reads the others, which costs less
+    // than the barriers of the selection below.
+    if (CS == 1 && cnt <= kSelFew) {
+        const uint32_t mine = tid < cnt ? keys[tid] : 0u;
+        int front = 0;
+        if (warp * 32 < cnt) {
+#pragma unroll 8
+            for (int i = 0; i < cnt; ++i) front += keys[i] + (i < tid) > mine;  // an equal key is in front if its block is
+        }
+        const bool taken = tid < cnt && front < p.n;
+        const uint32_t votes = __ballot_sync(0xffffffffu, taken);
+        if (lane == 0) red[warp] = __popc(votes);
+        __syncthreads();
+        const int at = __reduce_add_sync(0xffffffffu, lane < warp ? red[lane] : 0u) + __popc(votes & ((1u << lane) - 1));
+        if (taken) out[at] = j0 + tid;
+        return;
+    }
     // the n-th largest key
     uint32_t prefix = 0, need = p.n;
 #pragma unroll 1
@@ -488,12 +533,18 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
             if (need > before && need <= before + c[k]) {
                 found[0] = kSelBins - 1 - 4 * tid - k;
                 found[1] = need - before;
+                found[2] = need - before == c[k];
             }
             before += c[k];
         }
         __syncthreads();
         prefix = (prefix << bits) | found[0];
         need = found[1];
+        if (found[2]) {  // all keys that begin like this are chosen (prefix > 0, since some are not)
+            prefix = (prefix << shift) - 1;
+            need = 0;
+            break;
+        }
     }
     // keys above `prefix` are all chosen, of those equal to it the first `need`; each warp has a segment of the slice
     const int seg = (((cnt + kSelThreads / 32 - 1) / (kSelThreads / 32)) + 31) & ~31, s0 = min(warp * seg, cnt), s1 = min(s0 + seg, cnt);

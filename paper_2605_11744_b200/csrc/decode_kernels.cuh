@@ -349,16 +349,17 @@ struct Flag {
     static constexpr bool value = V;
 };
 
-template <int D, bool FP8, int NT, int WM>
+template <int D, bool FP8, int NT, int WM, bool BS = false, bool SEL = false>
 struct DecodeShape {
     static constexpr int RB = D * (FP8 ? 1 : 2);           // bytes of a cache row
     static constexpr int KG = RB == 256 ? 1 : 2;           // blocks of 16 slots of a warp in a tile
     static constexpr int kTileLog = KG == 1 ? 6 : 7;       // log2 of 64 KG, slots of a tile of one head
     static constexpr int kBlock = 2 * 16 * RB;             // 16 K rows and 16 V rows
     static constexpr int kWarpStage = KG * kBlock;
-    static constexpr int kBlocksPerSm = RB == 64 && NT == 1 ? 3 : 2;
+    static constexpr bool kThree = (BS || SEL) && RB == 128 && NT == 1 && FP8;
+    static constexpr int kBlocksPerSm = kThree || (RB == 64 && NT == 1) ? 3 : 2;
     static constexpr int KP = KG == 2 || WM > 1 ? 2 : 1;   // blocks of 16 slots taken through the products at once
-    static constexpr int kStages = RB == 64 ? (NT == 1 ? 4 : 6) : 3;
+    static constexpr int kStages = kThree ? 2 : RB == 64 ? (NT == 1 ? 4 : 6) : 3;
     static constexpr int kWR = 8 * NT;                     // rows of a warp
     static constexpr int MB = kWR * WM;                    // rows of an item, of each of its heads
     static constexpr int kPartRows = WM == 1 ? 4 * kWR : MB;  // rows of a unit's item
@@ -382,8 +383,8 @@ constexpr float kScaledRoom = 12.f, kScaledTop = 14.f;
 // BS: a scale for each block of rows (the members of DecodeParams from ks on), for FP8.  SEL: heads with a past read chosen blocks of
 // it and what their own segment and tail show them (from choice_log on); WM = 1.
 template <int D, bool FP8, int NT, int WM, bool BS = false, bool SEL = false>
-__global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM>::kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
-    using Sh = DecodeShape<D, FP8, NT, WM>;
+__global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, SEL>::kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
+    using Sh = DecodeShape<D, FP8, NT, WM, BS, SEL>;
     static_assert(!BS || (FP8 && Sh::KG == 2 && Sh::KP == 2), "the warp's two blocks of 16 slots have a scale each");
     static_assert(!SEL || WM == 1, "an item's rows all see the same slots");
     constexpr float kTop = BS ? kScaledTop : kHalfTop;

@@ -34,25 +34,33 @@ struct ResizeParams {
 
 __device__ __forceinline__ int pages_for(const ResizeParams& p, int rows) { return (int)fdiv((uint32_t)rows + p.f_page.d - 1, p.f_page); }
 
-// Sum over the block's threads, and over those before this one.  In 64 bits: lengths that make no sense may add up past 32.
-__device__ __forceinline__ long long block_scan(long long x, long long* total, long long* red) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    auto scan = [&](long long v) {
+// Sums of two numbers over the block's threads, and over those before this one.  In 64 bits: lengths that make no sense may add up
+// past 32.
+struct Pair {
+    long long x, y;
+};
+__device__ __forceinline__ Pair block_scan(Pair v, Pair* total, Pair* red) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    auto scan = [&](Pair s) {
 #pragma unroll
         for (int k = 1; k < 32; k <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, v, k);
-            if (lane >= k) v += y;
+            const long long x = __shfl_up_sync(0xffffffffu, s.x, k), y = __shfl_up_sync(0xffffffffu, s.y, k);
+            if (lane >= k) {
+                s.x += x;
+                s.y += y;
+            }
         }
-        return v;
+        return s;
     };
-    const long long incl = scan(x);
+    const Pair incl = scan(v);
     __syncthreads();
     if (lane == 31) red[warp] = incl;
     __syncthreads();
-    const long long warps = scan(red[lane]);
-    *total = __shfl_sync(0xffffffffu, warps, 31);
-    const long long before = __shfl_sync(0xffffffffu, warps, warp ? warp - 1 : 0);
-    return incl - x + (warp ? before : 0);
+    const Pair all = scan(lane < warps ? red[lane] : Pair{0, 0});
+    total->x = __shfl_sync(0xffffffffu, all.x, 31);
+    total->y = __shfl_sync(0xffffffffu, all.y, 31);
+    const long long x = __shfl_sync(0xffffffffu, all.x, warp ? warp - 1 : 0), y = __shfl_sync(0xffffffffu, all.y, warp ? warp - 1 : 0);
+    return Pair{incl.x - v.x + (warp ? x : 0), incl.y - v.y + (warp ? y : 0)};
 }
 
 // What a sequence asks for, checked: its rows before and after (equal where a number is out of range).
@@ -68,49 +76,54 @@ __device__ __forceinline__ void asked(const ResizeParams& p, int b, int* n_old, 
     }
 }
 
-// The whole plan, by one block of kPlanThreads.
-__device__ __forceinline__ void plan_pages(const ResizeParams& p, PagePlan* plan, long long* red, long long* counts) {
-    const int tid = threadIdx.x;
+// The whole plan, by one block.
+__device__ __forceinline__ void plan_pages(const ResizeParams& p, PagePlan* plan, Pair* red, long long* counts) {
+    const int tid = threadIdx.x, threads = blockDim.x;
     int count = *p.free_count;
     if (count < 0 || count > p.n_pages) {
         if (tid == 0) refuse_input(38);
         count = min(max(count, 0), p.n_pages);
     }
     auto pages = [&](int rows) { return rows < 0 ? 0 : pages_for(p, rows); };
-    long long back = 0, total;
-    for (int b = tid; b < p.B; b += kPlanThreads) {
-        int o, n;
-        asked(p, b, &o, &n);
-        back += max(pages(o) - pages(n), 0);
+    long long there = 0;  // pages on the list, those given back among them
+    if (p.B > threads) {  // else one scan gives their number as well
+        Pair back{0, 0}, total;
+        for (int b = tid; b < p.B; b += threads) {
+            int o, n;
+            asked(p, b, &o, &n);
+            back.y += max(pages(o) - pages(n), 0);
+        }
+        block_scan(back, &total, red);
+        there = count + total.y;
     }
-    block_scan(back, &total, red);
-    const long long there = count + total;
-    long long take_before = 0, back_before = 0, taken = 0;
-    for (int b0 = 0; b0 < p.B; b0 += kPlanThreads) {
+    Pair before{0, 0};
+    for (int b0 = 0; b0 < p.B; b0 += threads) {
         const int b = b0 + tid;
         int o = 0, n = 0;
         if (b < p.B) asked(p, b, &o, &n);
         const int more = pages(n) - pages(o), t = max(more, 0);
-        long long sum;
-        const long long tb = take_before + block_scan(t, &sum, red);
-        take_before += sum;
-        const bool served = t == 0 || tb + t <= there;
-        const long long gb = back_before + block_scan(max(-more, 0), &sum, red);
-        back_before += sum;
-        block_scan(served ? t : 0, &sum, red);
-        taken += sum;
+        Pair sum;
+        Pair at = block_scan(Pair{t, max(-more, 0)}, &sum, red);
+        at.x += before.x;
+        at.y += before.y;
+        before.x += sum.x;
+        before.y += sum.y;
+        if (p.B <= threads) there = count + sum.y;
+        const bool served = t == 0 || at.x + t <= there;
+        if (!served && at.x <= there) counts[2] = there - at.x;  // the first that has to wait: what those before it leave
         if (b < p.B) {
             if (!served) n = o;
-            plan[b] = PagePlan{o, n, tb, gb};
+            plan[b] = PagePlan{o, n, at.x, at.y};
             p.kv_len_out[b] = o < 0 ? p.kv_len[b] : n;
             p.q_len[b] = max(n - o, 0);
         }
     }
+    if (tid == 0 && before.x <= there) counts[2] = there - before.x;
+    __syncthreads();
     if (tid == 0) {
-        const long long left = there - taken;
+        const long long left = counts[2];
         counts[0] = count;
         counts[1] = there;
-        counts[2] = left;
         if (left > p.n_pages) refuse_input(38);
         *p.free_count_out = (int)min(left, (long long)p.n_pages);
     }
@@ -168,7 +181,8 @@ __device__ __forceinline__ void fill_sequence(const ResizeParams& p, const PageP
 // FILL: the same block does the second part, a warp to a sequence, with the plan in shared memory.
 template <bool FILL>
 __global__ void __launch_bounds__(kPlanThreads) pages_plan_kernel(const ResizeParams p) {
-    __shared__ long long red[32], counts[3];
+    __shared__ Pair red[32];
+    __shared__ long long counts[3];
     extern __shared__ uint8_t plan_smem[];
     PagePlan* shared_plan = reinterpret_cast<PagePlan*>(plan_smem);
     next_kernel_may_start();
@@ -178,7 +192,7 @@ __global__ void __launch_bounds__(kPlanThreads) pages_plan_kernel(const ResizePa
     }
     plan_pages(p, shared_plan, red, counts);
     __syncthreads();
-    for (int b = threadIdx.x >> 5; b < p.B; b += kPlanThreads / 32) fill_sequence(p, shared_plan, counts, b, threadIdx.x & 31, 32);
+    for (int b = threadIdx.x >> 5; b < p.B; b += blockDim.x >> 5) fill_sequence(p, shared_plan, counts, b, threadIdx.x & 31, 32);
 }
 
 __global__ void __launch_bounds__(256) pages_fill_kernel(const ResizeParams p) {

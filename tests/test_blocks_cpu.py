@@ -149,7 +149,7 @@ def test_selections_past_the_limits_are_refused():
 def test_bad_resizes_are_refused(bad):
     assert resize(**bad) == 1
     for kw in (dict(ws=None), dict(ws=OK + 16), dict(ws_bytes=8)):
-        assert resize(**kw) == 5
+        assert resize(Lq=2049, **kw) == 5 and resize(B=1025, Lq=1, **kw) == 5
     L = sa.lib()
     assert L.seg_pages_workspace_bytes(-1) == 0 and L.seg_pages_workspace_bytes(65536) == 0 and L.seg_pages_workspace_bytes(0) > 0
 
