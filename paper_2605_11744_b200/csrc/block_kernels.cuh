@@ -223,12 +223,12 @@ __device__ __forceinline__ void add_halves(float& lo, float& hi, uint32_t x) {
 // hardly any of them in double precision, where a conversion alone takes the time of a dozen others: values of an 8-bit cache are
 // multiples of 2^-9, of which a lane adds up 32 at most in fp32, and the lanes their sums as integers, exactly; bf16 numbers are put
 // into doubles bit by bit.
-constexpr int kSumWarps = 8;
+constexpr int kSumWarps = 4;
 template <int D, bool FP8>
-__global__ void __launch_bounds__(32 * kSumWarps) summarise_kernel(const __grid_constant__ SummariseParams p) {
+__global__ void __launch_bounds__(32 * kSumWarps, 6) summarise_kernel(const __grid_constant__ SummariseParams p) {
     constexpr int PER = FP8 ? 16 : 8, T = D / PER, RW = 32 / T, ROWS = 16 / RW;  // values of a lane's piece, lanes to a row, rows at a time, of a lane
     constexpr int KEEP = PER / RW;  // dims a lane has in the end
-    constexpr int AHEAD = 16 / ROWS;  // groups of 16 rows whose loads are in flight together
+    constexpr int AHEAD = 8 / ROWS;  // groups of 16 rows whose loads are in flight together
     const int lane = threadIdx.x & 31;
     const uint32_t unit = blockIdx.x * kSumWarps + (threadIdx.x >> 5);
     if (unit >= p.units) return;
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(128) no_choice_kernel(const __grid_constant__ 
 // largest by a radix selection (evict_select_kernel's, with the sums over the cluster's blocks through distributed shared memory)
 // and their numbers in ascending order.
 template <int D>
-__global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_constant__ SelectParams p) {
+__global__ void __launch_bounds__(kSelThreads, 2) select_kernel(const __grid_constant__ SelectParams p) {
     extern __shared__ uint32_t sel_smem[];
     uint32_t* hist = sel_smem;                 // [3][kSelBins]
     uint32_t* keys = sel_smem + 3 * kSelBins;  // [p.keys]
@@ -414,6 +414,14 @@ __global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_con
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int CS = (int)cluster_size(), rank = (int)cluster_rank(), unit = blockIdx.x / CS;
     const int which = unit % p.n_past, h = p.heads[which], bt = unit / p.n_past, b = bt / p.c.Lq, t = bt - b * p.c.Lq;
+    float q = 0.f;  // the query; asked for before anything that depends on the lengths
+    if (tid < D) {
+        double sum = 0.0;
+        const __nv_bfloat16* at = p.Q + b * p.q_stride[0] + t * p.q_stride[1] + (long long)h * p.g * p.q_stride[2] + tid;
+#pragma unroll 8
+        for (int x = 0; x < p.g; ++x) sum += (double)__bfloat162float(at[x * p.q_stride[2]]);
+        q = (float)sum;
+    }
     const int rows = new_rows(p.c, b), n = seq_len(p.c, b), shift = shift_of(p.c, b);
     if (t >= rows) return;
     int32_t* out = p.idx + ((long long)bt * p.c.Hkv + h) * p.n;
@@ -427,67 +435,86 @@ __global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_con
 
     // this block's slice, and the pages of its blocks (in the keys' place until the scores take it)
     const int slice = (((m + CS - 1) / CS + 31) & ~31), j0 = min(rank * slice, m), cnt = min(slice, m - j0);
+    if (tid < 4) keys[cnt + tid] = 0;  // (there is room for 32 more)
     for (int i = tid; i < cnt; i += kSelThreads) keys[i] = (uint32_t)table_entry(p.c, b, (j0 + i) << p.log);
 
-    // the query
-    float q = 0.f;
-    if (tid < D) {
-        double sum = 0.0;
-        const __nv_bfloat16* at = p.Q + b * p.q_stride[0] + t * p.q_stride[1] + (long long)h * p.g * p.q_stride[2] + tid;
-#pragma unroll 8
-        for (int x = 0; x < p.g; ++x) sum += (double)__bfloat162float(at[x * p.q_stride[2]]);
-        q = (float)sum;
-    }
     const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(q)));
     if (lane == 0) red[warp] = most;
-    for (int i = tid; i < 3 * kSelBins; i += kSelThreads) hist[i] = 0;
+    const bool few = CS == 1 && cnt <= kSelFew;
+    if (!few)
+        for (int i = tid; i < 3 * kSelBins; i += kSelThreads) hist[i] = 0;
     __syncthreads();
     const uint32_t top = __reduce_max_sync(0xffffffffu, lane < D / 32 ? red[lane] : 0u);
     const float step = __fmul_rn(__uint_as_float(top), kOver127);
     if (tid < D) query[tid] = top > 0 && top < 0x7f800000u && step > 0.f ? (int8_t)__float2int_rn(__fdiv_rn(q, step)) : (int8_t)0;
     __syncthreads();
 
-    // The scores, as unsigned numbers of the same order.  A lane takes a whole mean, with the query in registers: the 32 lines that
-    // a load of the warp touches are all used by the loads beside it, and nothing is left to add up across lanes (eight lanes to a
-    // mean took four times the instructions).
-    constexpr int N16 = D / 16;
-    uint4 q16[N16];
+    // The scores, as unsigned numbers of the same order.  T lanes read a mean, so that a load of the warp touches few lines (a lane
+    // to a mean touches 32, and their look-ups took three times as long as the bytes); a lane's partial sums of its T means are then
+    // handed on by halves, after which it has the sum of one.
+    constexpr int T = D / 16, PW = 32 / T;  // lanes to a mean, means of a load
+    const uint4 q16 = reinterpret_cast<const uint4*>(query)[lane % T];
+    for (int i0 = warp * 32; i0 < cnt; i0 += kSelThreads) {
+        uint4 k16[T];
 #pragma unroll
-    for (int x = 0; x < N16; ++x) q16[x] = reinterpret_cast<const uint4*>(query)[x];
-    for (int i = tid; i < cnt; i += kSelThreads) {
-        const uint32_t page = keys[i];
-        float score = __uint_as_float(0x7fffffffu);  // of a page that is not there: lowest
-        if (page < (uint32_t)p.c.n_pages) {
-            const long long at = ((long long)page * p.per_page + (row_in_page(p.c, (j0 + i) << p.log) >> p.log)) * p.c.Hkv + h;
-            const uint4* src = reinterpret_cast<const uint4*>(p.sums + at * D);
-            const float scale = p.sum_scale[at];
-            uint4 k16[N16];
-#pragma unroll
-            for (int x = 0; x < N16; ++x) k16[x] = src[x];
-            int s[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int x = 0; x < N16; ++x) {
-                s[0] = __dp4a((int)k16[x].x, (int)q16[x].x, s[0]);
-                s[1] = __dp4a((int)k16[x].y, (int)q16[x].y, s[1]);
-                s[2] = __dp4a((int)k16[x].z, (int)q16[x].z, s[2]);
-                s[3] = __dp4a((int)k16[x].w, (int)q16[x].w, s[3]);
+        for (int y = 0; y < T; ++y) {
+            const int i = i0 + y * PW + lane / T;
+            const uint32_t page = i < cnt ? keys[i] : 0xffffffffu;
+            k16[y] = make_uint4(0, 0, 0, 0);
+            if (page < (uint32_t)p.c.n_pages) {
+                const long long at = ((long long)page * p.per_page + (row_in_page(p.c, (j0 + i) << p.log) >> p.log)) * p.c.Hkv + h;
+                k16[y] = reinterpret_cast<const uint4*>(p.sums + at * D)[lane % T];
             }
-            score = __fmul_rn((float)(s[0] + s[1] + s[2] + s[3]), scale);
-        } else {
-            refuse_input(33);
         }
-        keys[i] = j0 + i < p.sink ? kSinkKey : weight_key(score);
+        const int i = i0 + lane % T * PW + lane / T;  // this lane's mean
+        float scale = __uint_as_float(0x7fffffffu);   // of a page that is not there: lowest
+        if (i < cnt) {
+            const uint32_t page = keys[i];
+            if (page < (uint32_t)p.c.n_pages)
+                scale = p.sum_scale[((long long)page * p.per_page + (row_in_page(p.c, (j0 + i) << p.log) >> p.log)) * p.c.Hkv + h];
+            else refuse_input(33);
+        }
+        int s[T];
+#pragma unroll
+        for (int y = 0; y < T; ++y)
+            s[y] = __dp4a((int)k16[y].x, (int)q16.x, __dp4a((int)k16[y].y, (int)q16.y, __dp4a((int)k16[y].z, (int)q16.z, __dp4a((int)k16[y].w, (int)q16.w, 0))));
+#pragma unroll
+        for (int half = T / 2; half >= 1; half >>= 1) {
+            const bool upper = lane & half;
+#pragma unroll
+            for (int y = 0; y < half; ++y) {
+                const int give = upper ? s[y] : s[y + half], keep = upper ? s[y + half] : s[y];
+                s[y] = keep + __shfl_xor_sync(0xffffffffu, give, half);
+            }
+        }
+        __syncwarp();
+        if (i < cnt) keys[i] = j0 + i < p.sink ? kSinkKey : weight_key(__fmul_rn((float)s[0], scale));
+        __syncwarp();
     }
     __syncthreads();
 
     // Few of them: a key is chosen if fewer than n are in front of it.  A thread holds one and reads the others, which costs less
     // than the barriers of the selection below.
-    if (CS == 1 && cnt <= kSelFew) {
+    if (few) {
         const uint32_t mine = tid < cnt ? keys[tid] : 0u;
         int front = 0;
         if (warp * 32 < cnt) {
-#pragma unroll 8
-            for (int i = 0; i < cnt; ++i) front += keys[i] + (i < tid) > mine;  // an equal key is in front if its block is
+            // an equal key is in front if its block is; what lies behind the last key is zero
+#pragma unroll 4
+            for (int i = 0; i < warp * 32; i += 4) {
+                const uint4 k = *reinterpret_cast<const uint4*>(keys + i);
+                front += (k.x >= mine) + (k.y >= mine) + (k.z >= mine) + (k.w >= mine);
+            }
+#pragma unroll
+            for (int x = 1; x < 32; ++x) {
+                const uint32_t k = __shfl_xor_sync(0xffffffffu, mine, x);
+                front += (lane ^ x) < lane ? k >= mine : k > mine;
+            }
+#pragma unroll 4
+            for (int i = warp * 32 + 32; i < cnt; i += 4) {
+                const uint4 k = *reinterpret_cast<const uint4*>(keys + i);
+                front += (k.x > mine) + (k.y > mine) + (k.z > mine) + (k.w > mine);
+            }
         }
         const bool taken = tid < cnt && front < p.n;
         const uint32_t votes = __ballot_sync(0xffffffffu, taken);
@@ -498,6 +525,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_con
         return;
     }
     // the n-th largest key
+    constexpr int BT = kSelBins / kSelThreads;
     uint32_t prefix = 0, need = p.n;
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
@@ -507,15 +535,19 @@ __global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_con
             if (pass == 0 || keys[i] >> (shift + bits) == prefix) atomicAdd(mh + ((keys[i] >> shift) & ((1u << bits) - 1)), 1u);
         __syncthreads();
         if (CS > 1) cluster_sync();
-        // bins from the top down, four to a thread
-        uint32_t c[4], before = 0;
+        // bins from the top down, BT to a thread
+        uint32_t c[BT], before = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t* at = mh + kSelBins - 1 - 4 * tid - k;
-            c[k] = 0;
-            if (CS == 1) c[k] = *at;
-            else
-                for (int r = 0; r < CS; ++r) c[k] += load_from_block(at, r);
+        for (int k = 0; k < BT; ++k) {
+            const uint32_t* at = mh + kSelBins - 1 - BT * tid - k;
+            c[k] = CS == 1 ? *at : 0u;
+            if (CS > 1) {
+                uint32_t v[8];  // all of them on their way at once
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] = r < CS ? load_from_block(at, r) : 0u;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) c[k] += v[r];
+            }
             before += c[k];
         }
         const uint32_t mine = before;
@@ -529,9 +561,9 @@ __global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_con
         __syncthreads();
         before += __reduce_add_sync(0xffffffffu, lane < warp ? red[lane] : 0u);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < BT; ++k) {
             if (need > before && need <= before + c[k]) {
-                found[0] = kSelBins - 1 - 4 * tid - k;
+                found[0] = kSelBins - 1 - BT * tid - k;
                 found[1] = need - before;
                 found[2] = need - before == c[k];
             }

@@ -207,21 +207,19 @@ struct BlockRange {
 };
 template <int MB, int TILE_LOG, bool SEL = false>
 __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* out, int* warp_sum) {
+    // A thread takes a run of (sequence, class) pairs, four to a sequence (the last is empty), so that for up to 32 sequences none
+    // has more than one of them: this part of the kernel is a chain of few instructions on data that nothing waits beside.
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int seg = (p.c.B + kDecThreads - 1) / kDecThreads;
-    const int b0 = min(tid * seg, p.c.B), b1 = min(b0 + seg, p.c.B);
-    auto tiles_of = [&](int b) {
+    const int pairs = 4 * p.c.B, seg = (pairs + kDecThreads - 1) / kDecThreads;
+    const int e0 = min(tid * seg, pairs), e1 = min(e0 + seg, pairs);
+    auto tiles_of = [&](int e) {
+        const int b = e >> 2, cls = e & 3;
+        if (cls == 3 || p.units[cls] == 0) return 0;
         const int rows = new_rows(p.c, b);
-        if (rows == 0) return 0;
-        const int n = seq_len(p.c, b), shift = shift_of(p.c, b);
-        int sum = 0;
-#pragma unroll
-        for (int cls = 0; cls < 3; ++cls)
-            if (p.units[cls]) sum += p.units[cls] * unit_tiles<MB, TILE_LOG, SEL>(p, n, rows, shift, cls);
-        return sum;
+        return rows == 0 ? 0 : p.units[cls] * unit_tiles<MB, TILE_LOG, SEL>(p, seq_len(p.c, b), rows, shift_of(p.c, b), cls);
     };
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += tiles_of(b);
+    for (int e = e0; e < e1; ++e) mine += tiles_of(e);
     int before = mine;
 #pragma unroll
     for (int x = 1; x < 32; x <<= 1) {
@@ -240,24 +238,20 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
     const int per = max(1, (total + (int)gridDim.x - 1) / (int)gridDim.x);
     const int begin = min((int)blockIdx.x * per, total), end = min(begin + per, total);
     if (begin < end && begin >= before && begin < before + mine) {
-        int off = begin - before, b = b0;
-        for (;; ++b) {
-            const int t = tiles_of(b);
-            if (off < t) break;
-            off -= t;
-        }
-        const int n = seq_len(p.c, b), rows = new_rows(p.c, b), shift = shift_of(p.c, b);
-        int u = 0, rb = 0, cls = 0;
-        for (;; ++cls) {
-            const int t = p.units[cls] ? unit_tiles<MB, TILE_LOG, SEL>(p, n, rows, shift, cls) : 0;
-            if (off < t * p.units[cls]) {
-                u += off / t;
-                off %= t;
-                break;
+        int off = begin - before, e = e0, t = mine;
+        if (seg > 1)
+            for (;; ++e) {
+                t = tiles_of(e);
+                if (off < t) break;
+                off -= t;
             }
-            off -= t * p.units[cls];
-            u += p.units[cls];
-        }
+        const int b = e >> 2, cls = e & 3;
+        const int n = seq_len(p.c, b), rows = new_rows(p.c, b), shift = shift_of(p.c, b);
+        int u = cls > 0 ? p.units[0] : 0, rb = 0;
+        if (cls > 1) u += p.units[1];
+        t /= p.units[cls];  // of one unit
+        u += off / t;
+        off %= t;
         for (;; ++rb) {
             int lo, hi;
             const int t = item_tiles<MB, SEL>(p, n, rows, shift, cls, TILE_LOG - p.unit_log[cls], rb, &lo, &hi);
@@ -273,6 +267,20 @@ __device__ __forceinline__ void find_range(const DecodeParams& p, BlockRange* ou
         out->tile = off;
     }
     __syncthreads();
+}
+
+// The block table and the lists of chosen blocks, on their way to L2 while a block finds its range: each is the next link of a chain
+// of dependent reads (length, list, page, rows) that the first tile waits for, and all but the length's would come from DRAM.  A
+// few KB to a block at most: a table with much more room than the sequences fill is left alone.
+__device__ __forceinline__ void prefetch_numbers(const DecodeParams& p) {
+    auto fetch = [](const void* at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at)); };
+    const int i0 = blockIdx.x * kDecThreads + threadIdx.x, step = gridDim.x * kDecThreads;
+    const int row = (p.c.max_pages + 31) / 32;  // lines of 128 bytes
+    if ((long long)p.c.B * row <= step)
+        for (int i = i0; i < p.c.B * row; i += step) fetch(p.c.block_table + (long long)(i / row) * p.c.table_stride + i % row * 32);
+    const long long lines = p.chosen ? ((long long)p.c.B * p.c.Lq * p.c.Hkv * p.n_chosen + 31) / 32 : 0;
+    if (lines <= step)
+        for (int i = i0; i < (int)lines; i += step) fetch(p.chosen + i * 32);
 }
 
 // ---- shared memory and operand fragments -----------------------------------------------------------------------------
@@ -405,6 +413,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
     auto head_of = [&](int first_head, int log) { return (int)p.head_order[first_head + (WM == 1 ? warp & ((1 << log) - 1) : 0)]; };
 
     next_kernel_may_start();
+    if (BS || SEL) prefetch_numbers(p);
     find_range<MB, Sh::kTileLog, SEL>(p, &range, warp_sum);
     if (range.begin >= range.end) return;
     const int per = range.per;
@@ -442,6 +451,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                 bool more = true;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
+                    if (32 * k >= p.n_chosen) break;
                     const int last = k ? __shfl_sync(0xffffffffu, chosen[k ? k - 1 : 0], 31) : -1, up = __shfl_up_sync(0xffffffffu, chosen[k], 1);
                     const bool fine = (unsigned)chosen[k] < (unsigned)past && chosen[k] > (lane ? up : last);
                     const uint32_t wrong = __ballot_sync(0xffffffffu, !fine);
@@ -710,22 +720,23 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[k][nt][e] = CH == 1 ? s2[0][k][nt][e] : s2[0][k][nt][e] + s2[CH - 1][k][nt][e];
-                float ksc[KP], vsc[KP], vexp[KP], vinv[KP];  // scales of the blocks; m, e and 2^-e of V's
-                if (BS) {
+                // score scales of the rows in each block of slots; m, e and 2^-e of V's scales
+                float qs[KP][NT][2], vsc[KP], vexp[KP], vinv[KP];
 #pragma unroll
-                    for (int k = 0; k < KP; ++k) {
-                        const float2 sc = block_scale[BS ? stage : 0][from][BS ? k : 0];
+                for (int k = 0; k < KP; ++k) {
+                    float2 sc = make_float2(1.f, 1.f);
+                    if (BS) {
+                        sc = block_scale[BS ? stage : 0][from][BS ? k : 0];
                         const uint32_t bits = __float_as_uint(sc.y);
                         const int e = min(max((int)((bits >> 23) & 0xffu) - 127, -126), 126);
-                        ksc[k] = sc.x;
                         vsc[k] = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
                         vexp[k] = (float)e;
                         vinv[k] = __uint_as_float((uint32_t)(127 - e) << 23);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) s[k][nt][x] *= ksc[k];
                     }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) qs[k][nt][e] = BS ? qscale[nt][e] * sc.x : qscale[nt][e];
                 }
                 // element e of s[k][nt]: slot 16 k + js[e >> 1], row 2 q4 + (e & 1) of the warp's eight; log2 units over the base
                 const bool edge_range = slot0 < all_lo || slot0 + 16 * KP > all_hi;
@@ -739,7 +750,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
 #pragma unroll
                                 for (int k = 0; k < KP; ++k)
                                     scores[(long long)r * p.pitch + slot0 + 16 * k + js[e >> 1]] =
-                                        (have >> (16 * k + js[e >> 1])) & 1 ? s[k][nt][e] * qscale[nt][e & 1] : -INFINITY;
+                                        (have >> (16 * k + js[e >> 1])) & 1 ? s[k][nt][e] * qs[k][nt][e & 1] : -INFINITY;
                         }
                 }
                 bool grows = false;
@@ -748,7 +759,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[k][nt][e] = fmaf(s[k][nt][e], qscale[nt][e & 1], BS ? vexp[k] - base[nt][e & 1] : -base[nt][e & 1]);
+                        for (int e = 0; e < 4; ++e) s[k][nt][e] = fmaf(s[k][nt][e], qs[k][nt][e & 1], BS ? vexp[k] - base[nt][e & 1] : -base[nt][e & 1]);
                 if (edge_range || have != (KP == 1 ? 0xffffu : 0xffffffffu)) {
 #pragma unroll
                     for (int k = 0; k < KP; ++k)
@@ -804,6 +815,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     }
                 }
                 uint32_t pf[KP][NT][2];
+                const bool fractions = BS && (vsc[0] != 1.f || vsc[KP - 1] != 1.f);  // scales that are no powers of two
 #pragma unroll
                 for (int k = 0; k < KP; ++k)
 #pragma unroll
@@ -812,7 +824,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                         for (int e = 0; e < 4; ++e) {
                             s[k][nt][e] = ex2(s[k][nt][e]);
                             l[nt][e & 1] = BS ? fmaf(s[k][nt][e], vinv[k], l[nt][e & 1]) : l[nt][e & 1] + s[k][nt][e];
-                            if (BS) s[k][nt][e] *= vsc[k];
+                            if (BS && fractions) s[k][nt][e] *= vsc[k];
                         }
                         pf[k][nt][0] = movm_t(pack16<FP8>(s[k][nt][0], s[k][nt][1]));
                         pf[k][nt][1] = movm_t(pack16<FP8>(s[k][nt][2], s[k][nt][3]));
@@ -965,8 +977,10 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
             __syncthreads();
             constexpr int TPR = D / 4;  // threads to a row
             const int d0 = (threadIdx.x % TPR) * 4;
-            for (int i = threadIdx.x / TPR; i < side * 8; i += kDecThreads / TPR) {
-                const int w0 = i >> 3, r8 = i & 7;
+            // rows of the eight that are there, the same for all heads of the unit (with several warps to a tile they differ)
+            const int there8 = WM > 1 ? 8 : min(8, SEL ? p.g - get.rb % p.head_blocks * MB - nt * 8 : rows - get.rb * MB - nt * 8);
+            for (int i = threadIdx.x / TPR; i < side * there8; i += kDecThreads / TPR) {
+                const int w0 = i / there8, r8 = i - w0 * there8;
                 int t, hq;
                 if (!row_of<MB, SEL>(p, get.rows, get.rb, (WM == 1 ? 0 : w0 * WR) + nt * 8 + r8, &t, &hq)) continue;
                 const int h = p.head_order[get.first_head + (WM == 1 ? w0 : 0)];
