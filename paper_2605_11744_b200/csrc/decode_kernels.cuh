@@ -66,6 +66,7 @@ struct DecodeParams {
     // blocks of 2^choice_log slots that heads with a past read of what lies behind their tail
     int choice_log, n_chosen;
     const int32_t* chosen;           // [B][Lq][Hkv][n_chosen]; null: no choice, the whole past
+    int page_pair;                   // 32 slots or numbers from a multiple of 32 on lie in one page, one after the other
     int head_blocks;                 // ceil(g / (rows of an item)), an item being of one new row
 };
 
@@ -297,6 +298,12 @@ __device__ __forceinline__ void cp_async16_if(uint32_t dst, const void* src, boo
     // without `there` nothing is read and the 16 bytes become zero
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async16_hint(uint32_t dst, const void* src, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() {
@@ -402,7 +409,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
     __shared__ int warp_sum[4];
     __shared__ uint32_t there[ST][4];  // which of a warp's 16 KG slots were loaded, per stage
     __shared__ float2 end_ml[4][8];    // an item's end: base and sum of eight rows of each warp
-    __shared__ float2 block_scale[BS ? ST : 1][4][2];  // of K and V, for each of a warp's blocks of 16 slots
+    __shared__ __align__(16) float block_scale[(BS ? ST : 1) * 16];  // of K and V, for each of a warp's blocks of 16 slots: [ST][4][2][2]
     const uint32_t ring = (smem_u32(smem_raw) + 127u) & ~127u;
     uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q4 = lane & 3, l4 = lane >> 2;
@@ -431,12 +438,17 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
     const int r0 = lane / C, ch = lane % C;
     const uint32_t put_lane = swizzled<RB>(r0, ch);
     const char *k_item, *v_item;  // of the item being loaded: this lane's piece of row r0 of page 0
-    const float* s_item = nullptr;  // its scales: of K for lane 0, of V for lane 1
+    const float* s_item = nullptr;  // its scales: of K for even lanes, of V for odd ones
     int far = 0, off = 0;         // its numbered slots
+    uint64_t read_once = 0, read_again = 0;
+    if (SEL) {
+        asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(read_once));
+        asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(read_again));
+    }
     int chosen[SEL ? 4 : 1], n_chosen = 0;  // its blocks, 32 k + lane in chosen[k], and how many of them are in order
     auto enter_item = [&]() {
         const int h = head_of(put.first_head, put.log);
-        if (BS) s_item = lane == 0 ? p.ks + h * p.ks_stride[2] : p.vs + h * p.vs_stride[2];
+        if (BS) s_item = (lane & 1) == 0 ? p.ks + h * p.ks_stride[2] : p.vs + h * p.vs_stride[2];
         if (SEL) {
             int lo, hi;
             const int t = put.rb / p.head_blocks;
@@ -479,6 +491,17 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
     int page_next[KG], slot_next[KG];
     auto look_up = [&]() {
         const int slot0 = put.first_slot() + (WM == 1 ? key_group(put.log) : warp) * 16 * KG;
+        if ((BS || SEL) && KG == 2 && p.page_pair) {
+            // one look-up for both blocks of 16, if either is needed
+            const int from = slot_from(slot0);
+            const bool full0 = slot0 >= put.lo && slot0 + 16 <= put.hi, full1 = slot0 + 16 >= put.lo && slot0 + 32 <= put.hi;
+            const int page = from >= 0 && (full0 || full1) ? table_entry(p.c, put.b, from) : -1;
+            slot_next[0] = from;
+            slot_next[KG - 1] = from >= 0 ? from + 16 : -1;
+            page_next[0] = full0 ? page : -1;
+            page_next[KG - 1] = full1 ? page : -1;
+            return;
+        }
 #pragma unroll
         for (int k = 0; k < KG; ++k) {
             const int s0 = slot0 + 16 * k;
@@ -493,33 +516,53 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
         if (put_left > 0) {
             const int slot0 = put.first_slot() + (WM == 1 ? key_group(put.log) : warp) * 16 * KG;
             uint32_t loaded = 0;
+            constexpr bool PAIR = (BS || SEL) && KG == 2;
+            // chosen blocks are read once; what a sequence's rows see whole is read again by the next of them, and stays in L2
+            const uint64_t policy = SEL ? (slot0 < far ? read_once : read_again) : 0;
+            auto rows_from = [&](uint32_t dst, const char* src, long long stride) {
 #pragma unroll
-            for (int k = 0; k < KG; ++k) {
+                for (int i = 0; i < 16 / RPI; ++i) {
+                    const uint32_t to = (dst ^ swizzled<RB>(i * RPI, 0) % RB) + i * RPI * RB;
+                    if (SEL) cp_async16_hint(to, src, policy);
+                    else cp_async16(to, src);
+                    src += RPI * stride;
+                }
+                return src;
+            };
+            const bool both = PAIR && p.page_pair && (unsigned)page_next[0] < (unsigned)p.c.n_pages && page_next[0] == page_next[KG - 1];
+            if (both) {
+                const int page = page_next[0], prow = row_in_page(p.c, slot_next[0]);
+                const uint32_t dst = ring + (uint32_t)(s * 4 + warp) * Sh::kWarpStage + put_lane;
+                const char* src = rows_from(dst, k_item + page * p.c.k_stride[0] + prow * p.c.k_stride[1], p.c.k_stride[1]);
+                rows_from(dst + Sh::kBlock, src, p.c.k_stride[1]);
+                src = rows_from(dst + 16 * RB, v_item + page * p.c.v_stride[0] + prow * p.c.v_stride[1], p.c.v_stride[1]);
+                rows_from(dst + Sh::kBlock + 16 * RB, src, p.c.v_stride[1]);
+                loaded = 0xffffffffu;
+                if (BS && lane < 4) {
+                    const long long* st = lane & 1 ? p.vs_stride : p.ks_stride;
+                    cp_async4(smem_u32(block_scale) + (s * 16 + warp * 4 + lane) * 4,
+                              s_item + page * st[0] + ((prow + 16 * (lane >> 1)) >> p.scale_log) * st[1]);
+                }
+            }
+            constexpr int APART = PAIR ? 1 : KG;  // blocks of 16 side by side in the code: seldom ones take turns
+#pragma unroll APART
+            for (int k = both ? KG : 0; k < KG; ++k) {
                 const int s0 = slot0 + 16 * k;
                 const uint32_t dst = ring + (uint32_t)((s * 4 + warp) * KG + k) * Sh::kBlock + put_lane;
-                int prow, page = page_next[k];
+                const int slot_k = k == 0 ? slot_next[0] : slot_next[KG - 1];
+                int prow, page = k == 0 ? page_next[0] : page_next[KG - 1];
                 if ((unsigned)page < (unsigned)p.c.n_pages) {
                     // 16 visible slots in one page: one look-up, and rows a stride apart
-                    prow = row_in_page(p.c, SEL ? slot_next[k] : s0);
-                    const char* src = k_item + page * p.c.k_stride[0] + prow * p.c.k_stride[1];
-#pragma unroll
-                    for (int i = 0; i < 16 / RPI; ++i) {
-                        cp_async16((dst ^ swizzled<RB>(i * RPI, 0) % RB) + i * RPI * RB, src);
-                        src += RPI * p.c.k_stride[1];
-                    }
-                    src = v_item + page * p.c.v_stride[0] + prow * p.c.v_stride[1];
-#pragma unroll
-                    for (int i = 0; i < 16 / RPI; ++i) {
-                        cp_async16((dst ^ swizzled<RB>(i * RPI, 0) % RB) + (16 + i * RPI) * RB, src);
-                        src += RPI * p.c.v_stride[1];
-                    }
+                    prow = row_in_page(p.c, SEL ? slot_k : s0);
+                    rows_from(dst, k_item + page * p.c.k_stride[0] + prow * p.c.k_stride[1], p.c.k_stride[1]);
+                    rows_from(dst + 16 * RB, v_item + page * p.c.v_stride[0] + prow * p.c.v_stride[1], p.c.v_stride[1]);
                     loaded |= 0xffffu << (16 * k);
                 } else {
                     const int slot = s0 + (lane & 15);
                     long long row_off = -1;  // of one row: lanes 0-15 in K, 16-31 in V
                     page = -1;
-                    if (slot >= put.lo && slot < put.hi && (!SEL || slot_next[k] >= 0) &&
-                        (page = page_of(p.c, put.b, SEL ? slot_next[k] + (lane & 15) : slot, &prow)) >= 0) {
+                    if (slot >= put.lo && slot < put.hi && (!SEL || slot_k >= 0) &&
+                        (page = page_of(p.c, put.b, SEL ? slot_k + (lane & 15) : slot, &prow)) >= 0) {
                         const long long* st = lane < 16 ? p.c.k_stride : p.c.v_stride;
                         row_off = page * st[0] + prow * st[1] + head_of(put.first_head, put.log) * st[2];
                     }
@@ -539,11 +582,10 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     }
                 }
                 if (BS && lane < 2) {
-                    float* to = &block_scale[BS ? s : 0][warp][k].x + lane;
+                    const int to = s * 16 + warp * 4 + 2 * k + lane;
                     const long long* st = lane == 0 ? p.ks_stride : p.vs_stride;
-                    if ((unsigned)page < (unsigned)p.c.n_pages)
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(to)), "l"(s_item + page * st[0] + (prow >> p.scale_log) * st[1]) : "memory");
-                    else *to = 1.f;  // none of the 16 is there
+                    if ((unsigned)page < (unsigned)p.c.n_pages) cp_async4(smem_u32(block_scale) + to * 4, s_item + page * st[0] + (prow >> p.scale_log) * st[1]);
+                    else block_scale[to] = 1.f;  // none of the 16 is there
                 }
             }
             if (lane == 0) there[s][warp] = loaded;
@@ -726,7 +768,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                 for (int k = 0; k < KP; ++k) {
                     float2 sc = make_float2(1.f, 1.f);
                     if (BS) {
-                        sc = block_scale[BS ? stage : 0][from][BS ? k : 0];
+                        sc = *reinterpret_cast<const float2*>(block_scale + stage * 16 + from * 4 + 2 * k);
                         const uint32_t bits = __float_as_uint(sc.y);
                         const int e = min(max((int)((bits >> 23) & 0xffu) - 127, -126), 126);
                         vsc[k] = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
