@@ -482,7 +482,7 @@ segattn_status seg_blocks_summarise(const seg_kv_cache* c, const seg_block_scale
  * (float)(sum over p_i q_ji) * scale_j, exact but for that product.  The blocks below `sink` are chosen in any case, and of the others those of the
  * largest scores (equal: lower block; NaN lowest): n together, or all R where there are no more.
  *   idx   int32 contiguous [B][Lq][Hkv][n]: ascending, then -1; all -1 for heads of other classes.  Rows t >= q_len[b] are left as they were.
- * K, V and their strides in c are not used.  1 <= n <= 128, 0 <= sink <= n; max_pages * page_size / block at most 393000.  One kernel. */
+ * K, V and their strides in c are not used.  1 <= n <= 128, 0 <= sink <= n; max_pages * page_size / block at most 49152.  One kernel. */
 segattn_status seg_blocks_select(const seg_kv_cache* c, int32_t Lq, int32_t Hq, int32_t S, int32_t T, const uint8_t* head_past_mask,
                                  const void* Q, const int64_t q_stride[3], const seg_block_means* means, int32_t n, int32_t sink,
                                  int32_t* idx, void* stream);

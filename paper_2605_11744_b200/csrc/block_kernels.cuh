@@ -379,10 +379,12 @@ struct SelectParams {
 
 constexpr int kSelThreads = 512;
 constexpr int kSelBins = 2048;
-constexpr int kSelFew = 256;              // as many are compared with each other one by one
-constexpr uint32_t kSinkKey = 0xfffffffeu;  // above every score's
-constexpr int kSelKeys = 49152;  // blocks that a thread block has room for
-constexpr int kSelSlice = 1024;  // blocks that a thread block of a cluster has at least
+constexpr int kSelFew = 256;                // as many are compared with each other one by one
+constexpr int kSelMost = 128;               // blocks that can be chosen
+constexpr int kSelKeys = 49152;             // blocks to choose from
+constexpr int kSelSlice = 1024;             // blocks that a thread block of a cluster has at least
+constexpr uint32_t kSinkKey = 0xffffffffu;  // above every score's
+static_assert(kSelKeys / 32 <= kSelBins, "a bin for 32 neighbouring blocks");
 
 // The lowest slot that a row at `slot` sees whole through a head with a past: its tail's start, rounded down to a block.
 __device__ __forceinline__ int whole_from(const SelectParams& p, int slot, int shift) {
@@ -400,17 +402,33 @@ __global__ void __launch_bounds__(128) no_choice_kernel(const __grid_constant__ 
     if (t < new_rows(p.c, b)) no_choice(p, blockIdx.x, 0, threadIdx.x, 128);
 }
 
-// A cluster takes one (new row, KV head with a past).  The query, summed over the head's query heads and brought to 8 bits, against the means
-// of the blocks before the row's tail: integer products, so that a score is the same in whatever order it is added up; then the n
-// largest by a radix selection (evict_select_kernel's, with the sums over the cluster's blocks through distributed shared memory)
-// and their numbers in ascending order.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// into the same place of another block's shared memory
+__device__ __forceinline__ void store_to_block(uint32_t* shared, uint32_t rank, uint32_t v) {
+    uint32_t addr;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_u32(shared)), "r"(rank));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+// A cluster takes one (new row, KV head with a past).  The query, summed over the head's query heads and brought to 8 bits, against
+// the means of the blocks before the row's tail: integer products, so that a score is the same in whatever order it is added up.
+// Then the first block of the cluster chooses: digits of the keys (11, 11 and 10 bits, then the block's number over 32, lower numbers
+// first) narrow down where the n-th lies until few keys are left there, most times after one of them; those are compared one by
+// one, and the chosen numbers put in order in the same way.  Barriers and dependent reads are what it costs (16 x 4 heads of 2800-4000
+// blocks: 16 us for 28 MB of means), so there are few of them; a selection over histograms of the whole cluster, with ordered scans
+// for the numbers, was 20% slower.
 template <int D>
 __global__ void __launch_bounds__(kSelThreads, 2) select_kernel(const __grid_constant__ SelectParams p) {
     extern __shared__ uint32_t sel_smem[];
-    uint32_t* hist = sel_smem;                 // [3][kSelBins]
-    uint32_t* keys = sel_smem + 3 * kSelBins;  // [p.keys]
+    uint32_t* hist = sel_smem;             // [kSelBins]
+    uint32_t* keys = sel_smem + kSelBins;  // [p.keys]
     __shared__ __align__(16) int8_t query[D];
-    __shared__ uint32_t red[kSelThreads / 32], seg_gt[kSelThreads / 32], seg_eq[kSelThreads / 32], found[3], totals[2];
+    __shared__ __align__(16) uint32_t near[kSelFew];    // keys about the n-th, then zeros
+    __shared__ int32_t near_at[kSelFew];                // their blocks
+    __shared__ __align__(16) int32_t chosen[kSelMost];  // the chosen blocks, then larger numbers
+    __shared__ uint32_t red[kSelThreads / 32], found[3];
+    __shared__ int n_chosen, n_near;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int CS = (int)cluster_size(), rank = (int)cluster_rank(), unit = blockIdx.x / CS;
     const int which = unit % p.n_past, h = p.heads[which], bt = unit / p.n_past, b = bt / p.c.Lq, t = bt - b * p.c.Lq;
@@ -432,22 +450,24 @@ __global__ void __launch_bounds__(kSelThreads, 2) select_kernel(const __grid_con
         for (int i = rank * kSelThreads + tid; i < p.n; i += CS * kSelThreads) out[i] = i < m ? i : -1;
         return;
     }
+    if (CS > 1) cluster_arrive();
 
-    // this block's slice, and the pages of its blocks (in the keys' place until the scores take it)
+    // this block's slice, and the pages of its blocks (in the keys' place, in the first block of the cluster until the scores take it)
     const int slice = (((m + CS - 1) / CS + 31) & ~31), j0 = min(rank * slice, m), cnt = min(slice, m - j0);
-    if (tid < 4) keys[cnt + tid] = 0;  // (there is room for 32 more)
     for (int i = tid; i < cnt; i += kSelThreads) keys[i] = (uint32_t)table_entry(p.c, b, (j0 + i) << p.log);
 
     const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(q)));
     if (lane == 0) red[warp] = most;
-    const bool few = CS == 1 && cnt <= kSelFew;
-    if (!few)
-        for (int i = tid; i < 3 * kSelBins; i += kSelThreads) hist[i] = 0;
+    if (tid == 0) n_chosen = n_near = 0;
+    if (tid < kSelFew) near[tid] = 0;
+    if (tid < kSelMost) chosen[tid] = 0x7fffffff;
+    for (int i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
     __syncthreads();
     const uint32_t top = __reduce_max_sync(0xffffffffu, lane < D / 32 ? red[lane] : 0u);
     const float step = __fmul_rn(__uint_as_float(top), kOver127);
     if (tid < D) query[tid] = top > 0 && top < 0x7f800000u && step > 0.f ? (int8_t)__float2int_rn(__fdiv_rn(q, step)) : (int8_t)0;
     __syncthreads();
+    if (CS > 1) cluster_wait();  // the first block is there
 
     // The scores, as unsigned numbers of the same order.  T lanes read a mean, so that a load of the warp touches few lines (a lane
     // to a mean touches 32, and their look-ups took three times as long as the bytes); a lane's partial sums of its T means are then
@@ -488,68 +508,46 @@ __global__ void __launch_bounds__(kSelThreads, 2) select_kernel(const __grid_con
             }
         }
         __syncwarp();
-        if (i < cnt) keys[i] = j0 + i < p.sink ? kSinkKey : weight_key(__fmul_rn((float)s[0], scale));
+        if (i < cnt) {
+            const uint32_t key = j0 + i < p.sink ? kSinkKey : weight_key(__fmul_rn((float)s[0], scale));
+            if (rank == 0) keys[i] = key;
+            else store_to_block(keys + j0 + i, 0, key);
+        }
         __syncwarp();
     }
-    __syncthreads();
-
-    // Few of them: a key is chosen if fewer than n are in front of it.  A thread holds one and reads the others, which costs less
-    // than the barriers of the selection below.
-    if (few) {
-        const uint32_t mine = tid < cnt ? keys[tid] : 0u;
-        int front = 0;
-        if (warp * 32 < cnt) {
-            // an equal key is in front if its block is; what lies behind the last key is zero
-#pragma unroll 4
-            for (int i = 0; i < warp * 32; i += 4) {
-                const uint4 k = *reinterpret_cast<const uint4*>(keys + i);
-                front += (k.x >= mine) + (k.y >= mine) + (k.z >= mine) + (k.w >= mine);
-            }
-#pragma unroll
-            for (int x = 1; x < 32; ++x) {
-                const uint32_t k = __shfl_xor_sync(0xffffffffu, mine, x);
-                front += (lane ^ x) < lane ? k >= mine : k > mine;
-            }
-#pragma unroll 4
-            for (int i = warp * 32 + 32; i < cnt; i += 4) {
-                const uint4 k = *reinterpret_cast<const uint4*>(keys + i);
-                front += (k.x > mine) + (k.y > mine) + (k.z > mine) + (k.w > mine);
-            }
-        }
-        const bool taken = tid < cnt && front < p.n;
-        const uint32_t votes = __ballot_sync(0xffffffffu, taken);
-        if (lane == 0) red[warp] = __popc(votes);
+    if (CS > 1) {
+        cluster_sync();
+        if (rank > 0) return;
+    } else {
         __syncthreads();
-        const int at = __reduce_add_sync(0xffffffffu, lane < warp ? red[lane] : 0u) + __popc(votes & ((1u << lane) - 1));
-        if (taken) out[at] = j0 + tid;
-        return;
     }
-    // the n-th largest key
+
+    // Where the n-th is: among `about` keys that share the digits found so far, the need-th of them.
     constexpr int BT = kSelBins / kSelThreads;
     uint32_t prefix = 0, need = p.n;
+    int done = 32, numbers = -1, about = m;  // bits of a key that are left, the bin of the numbers once there are none
+    auto place = [&](int i, uint32_t key) {  // 2: in front of them, 1: one of them, 0: behind
+        if (done == 32) return 1;
+        const uint32_t d = key >> done;
+        if (d != prefix) return d > prefix ? 2 : 0;
+        return numbers < 0 || i >> 5 == numbers ? 1 : i >> 5 < numbers ? 2 : 0;
+    };
 #pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        uint32_t* mh = hist + pass * kSelBins;
-        for (int i = tid; i < cnt; i += kSelThreads)
-            if (pass == 0 || keys[i] >> (shift + bits) == prefix) atomicAdd(mh + ((keys[i] >> shift) & ((1u << bits) - 1)), 1u);
-        __syncthreads();
-        if (CS > 1) cluster_sync();
-        // bins from the top down, BT to a thread
-        uint32_t c[BT], before = 0;
-#pragma unroll
-        for (int k = 0; k < BT; ++k) {
-            const uint32_t* at = mh + kSelBins - 1 - BT * tid - k;
-            c[k] = CS == 1 ? *at : 0u;
-            if (CS > 1) {
-                uint32_t v[8];  // all of them on their way at once
-#pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] = r < CS ? load_from_block(at, r) : 0u;
-#pragma unroll
-                for (int r = 0; r < 8; ++r) c[k] += v[r];
-            }
-            before += c[k];
+    for (int pass = 0; about > kSelFew; ++pass) {  // four at most: 32 numbers to a bin
+        const int bits = pass < 2 ? 11 : 10, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        if (pass > 0) {
+            for (int i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
+            __syncthreads();
         }
+        for (int i = tid; i < m; i += kSelThreads) {
+            const uint32_t key = keys[i];
+            if (place(i, key) == 1) atomicAdd(hist + (pass < 3 ? (key >> shift) & ((1u << bits) - 1) : (uint32_t)(kSelBins - 1 - (i >> 5))), 1u);
+        }
+        __syncthreads();
+        // bins from the top down, BT to a thread
+        const uint4 v = *reinterpret_cast<const uint4*>(hist + kSelBins - BT - BT * tid);
+        const uint32_t c[BT] = {v.w, v.z, v.y, v.x};
+        uint32_t before = c[0] + c[1] + c[2] + c[3];
         const uint32_t mine = before;
 #pragma unroll
         for (int x = 1; x < 32; x <<= 1) {
@@ -565,59 +563,54 @@ __global__ void __launch_bounds__(kSelThreads, 2) select_kernel(const __grid_con
             if (need > before && need <= before + c[k]) {
                 found[0] = kSelBins - 1 - BT * tid - k;
                 found[1] = need - before;
-                found[2] = need - before == c[k];
+                found[2] = c[k];
             }
             before += c[k];
         }
         __syncthreads();
-        prefix = (prefix << bits) | found[0];
-        need = found[1];
-        if (found[2]) {  // all keys that begin like this are chosen (prefix > 0, since some are not)
-            prefix = (prefix << shift) - 1;
-            need = 0;
-            break;
+        if (pass < 3) {
+            prefix = (prefix << bits) | found[0];
+            done = shift;
+        } else {
+            numbers = kSelBins - 1 - (int)found[0];
         }
+        need = found[1];
+        about = (int)found[2];
     }
-    // keys above `prefix` are all chosen, of those equal to it the first `need`; each warp has a segment of the slice
-    const int seg = (((cnt + kSelThreads / 32 - 1) / (kSelThreads / 32)) + 31) & ~31, s0 = min(warp * seg, cnt), s1 = min(s0 + seg, cnt);
-    uint32_t gt = 0, eq = 0;
-    for (int i = s0 + lane; i < s1; i += 32) {
-        gt += keys[i] > prefix;
-        eq += keys[i] == prefix;
-    }
-    gt = __reduce_add_sync(0xffffffffu, gt);
-    eq = __reduce_add_sync(0xffffffffu, eq);
-    if (lane == 0) {
-        seg_gt[warp] = gt;
-        seg_eq[warp] = eq;
+    for (int i = tid; i < m; i += kSelThreads) {
+        const uint32_t key = keys[i];
+        const int at = place(i, key);
+        if (at == 2) chosen[atomicAdd(&n_chosen, 1)] = i;
+        if (at == 1) {
+            const int k = atomicAdd(&n_near, 1);
+            near[k] = key;
+            near_at[k] = i;
+        }
     }
     __syncthreads();
-    constexpr int W = kSelThreads / 32;
-    uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? seg_gt[lane] : 0u);
-    uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? seg_eq[lane] : 0u);
-    if (CS > 1) {
-        const uint32_t gt_all = __reduce_add_sync(0xffffffffu, lane < W ? seg_gt[lane] : 0u), eq_all = __reduce_add_sync(0xffffffffu, lane < W ? seg_eq[lane] : 0u);
-        if (tid == 0) {
-            totals[0] = gt_all;
-            totals[1] = eq_all;
+    const uint32_t mine = tid < about ? near[tid] : 0u;
+    uint32_t front = 0;
+    if (warp * 32 < about)
+#pragma unroll 4
+        for (int i = 0; i < about; i += 4) {
+            const uint4 k = *reinterpret_cast<const uint4*>(near + i);
+            front += (k.x > mine) + (k.y > mine) + (k.z > mine) + (k.w > mine);
         }
-        cluster_sync();
-        for (int r = 0; r < rank; ++r) {
-            gt_before += load_from_block(totals, r);
-            eq_before += load_from_block(totals + 1, r);
+    const bool may = tid < about && front < need;
+    if (__syncthreads_count(may) > (int)need && may)  // equal ones on the border: the lower blocks
+        for (int i = 0; i < about; ++i) front += near[i] == mine && near_at[i] < near_at[tid];
+    if (may && front < need) chosen[atomicAdd(&n_chosen, 1)] = near_at[tid];
+    __syncthreads();
+    if (tid < p.n) {
+        const int32_t number = chosen[tid];
+        int at = 0;
+#pragma unroll 4
+        for (int i = 0; i < p.n; i += 4) {
+            const int4 k = *reinterpret_cast<const int4*>(chosen + i);
+            at += (k.x < number) + (k.y < number) + (k.z < number) + (k.w < number);
         }
+        out[at] = number;
     }
-    for (int i0 = s0; i0 < s1; i0 += 32) {
-        const int i = i0 + lane;
-        const uint32_t key = i < s1 ? keys[i] : 0u;
-        const uint32_t above = __ballot_sync(0xffffffffu, i < s1 && key > prefix), same = __ballot_sync(0xffffffffu, i < s1 && key == prefix);
-        const uint32_t below = (1u << lane) - 1;
-        const uint32_t g_at = gt_before + __popc(above & below), e_at = eq_before + __popc(same & below);
-        if (((above >> lane) & 1) || (((same >> lane) & 1) && e_at < need)) out[g_at + min(e_at, need)] = j0 + i;
-        gt_before += __popc(above);
-        eq_before += __popc(same);
-    }
-    if (CS > 1) cluster_sync();  // the others may still read this block's totals
 }
 
 }  // namespace segattn
