@@ -433,8 +433,8 @@ segattn_status seg_kv_evict(const seg_kv_cache* c, const float* weights, int32_t
  * A sequence grows by at most Lq rows.  One out of range (want < 0 or past max_pages * page_size, a larger growth, a kv_len out of
  * range) stays as it is, a free_count outside [0, n_pages] is cut, a page number outside [0, n_pages) comes out as -1 in the table
  * and the slots: each makes the next seg_attn_poll_status return SEGATTN_ERR_INVALID.  B <= 65535, max_pages * page_size <= 2^30.
- * `workspace`: DEVICE, 256-byte aligned, seg_pages_workspace_bytes(B) bytes (0: invalid B), scratch; not looked at, and may be NULL,
- * where B <= 1024 and B * Lq <= 4096 (one kernel; two elsewhere). */
+ * `workspace`: DEVICE, 256-byte aligned, seg_pages_workspace_bytes(B) bytes (0: invalid B), scratch (calls that may run
+ * at the same time, captured ones too, need one each); not looked at, and may be NULL, where B <= 1024 and B * Lq <= 4096 (one kernel; two elsewhere). */
 size_t seg_pages_workspace_bytes(int32_t B);
 segattn_status seg_pages_resize(int32_t B, int32_t Lq, int32_t page_size, int32_t n_pages, const int32_t* want, int32_t* block_table,
                                 int32_t max_pages, int32_t table_stride, const int32_t* kv_len, const int32_t* pos_shift,
@@ -460,6 +460,13 @@ segattn_status seg_blocks_append(const seg_kv_cache* c, const seg_block_scales* 
                                  const int64_t kn_stride[3], const void* V_new, const int64_t vn_stride[3], int32_t Hq, const void* Q,
                                  const int64_t q_stride[3], void* Q_out, const int64_t qo_stride[3], const float* table,
                                  int32_t n_pos, int32_t rot_dim, int32_t layout, void* stream);
+
+/* seg_kv_evict (same arguments, same rows kept) for such a cache: the kept rows' new blocks take the largest of their rows' scales, and
+ * a row whose scale was smaller is brought to it as above.  Scales must not share elements, neither here nor in the append (a zero stride
+ * is SEGATTN_ERR_INVALID).  (seg_kv_evict itself moves rows as they are, without their blocks' scales.)  Two kernels. */
+segattn_status seg_blocks_evict(const seg_kv_cache* c, const seg_block_scales* scales, const float* weights, int32_t W, int32_t sink,
+                                int32_t recent, int32_t heavy, const int32_t* dst_table, int32_t dst_max_pages, int32_t dst_stride,
+                                int32_t* idx, int32_t* kv_len_out, int32_t* pos_shift_out, float* weights_out, void* stream);
 
 /* ---- Sparse attention over the far past: a head of class PAST reads, of everything before its segment's tail, the n blocks whose mean
  * keys score highest against the query, found when the token is decoded.  (seg_retrieval_select is the paper's own operator, for a

@@ -95,6 +95,7 @@ def lib():
         L.seg_pages_workspace_bytes.argtypes = [i32]
         L.seg_pages_resize.argtypes = [i32] * 4 + [vp, vp, i32, i32] + [vp] * 10 + [ctypes.c_size_t, vp]
         L.seg_blocks_append.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, i32, i32, vp]
+        L.seg_blocks_evict.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp]
         L.seg_blocks_summarise.argtypes = [vp, vp, i32, vp, vp]
         L.seg_blocks_select.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, i32, i32, vp, vp]
         L.seg_attn_decode_blocks_workspace_bytes.restype = ctypes.c_size_t

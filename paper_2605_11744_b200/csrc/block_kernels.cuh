@@ -194,6 +194,90 @@ __global__ void __launch_bounds__(256) append_blocks_kernel(const __grid_constan
     }
 }
 
+// ---- eviction from a cache with a scale for each block -------------------------------------------------------------------
+struct EvictBlocksParams {
+    EvictParams e;
+    float *ks, *vs;
+    long long ks_stride[3], vs_stride[3];
+    int log;
+};
+
+// A warp writes one block of the compacted cache for one head: its rows come from blocks of all kinds, so it takes the largest of their
+// scales, and a row whose scale was smaller is brought to it (exactly but at the lowest octave, as in an append; no row's largest value
+// has to be looked for).  Runs after evict_select_kernel; the lengths and shifts are written here as in evict_move_kernel.
+template <int D>
+__global__ void __launch_bounds__(256) evict_move_blocks_kernel(const __grid_constant__ EvictBlocksParams p) {
+    const EvictParams& prm = p.e;
+    after_previous_kernel();
+    const int b = blockIdx.y, lane = threadIdx.x & 31;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        const int n = seq_len(prm.c, b), m = min(n, prm.budget), s = shift_of(prm.c, b);
+        prm.kv_len_out[b] = m;
+        prm.pos_shift_out[b] = s + n - m;
+    }
+    const uint32_t unit = blockIdx.x * 8 + (threadIdx.x >> 5), k = fdiv(unit, prm.f_heads);
+    const int h = (int)(unit - k * prm.f_heads.d), r0 = (int)(k << p.log);
+    if (r0 >= prm.budget) return;
+    const int rows = min(1 << p.log, prm.budget - r0);
+    const int32_t* idx = prm.idx + ((long long)b * prm.c.Hkv + h) * prm.budget + r0;
+    // rows 32 j + lane: where they are (-1: nowhere, -2: on a page that is not there), and their scales
+    int page[4], row[4];
+    float ks[4], vs[4], k_top = 0.f, v_top = 0.f;
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = 32 * j + lane, slot = r < rows ? idx[r] : -1;
+        page[j] = -1;
+        row[j] = 0;
+        ks[j] = vs[j] = 0.f;
+        if (slot >= 0) {
+            any = true;
+            page[j] = page_of(prm.c, b, slot, &row[j]);
+            if (page[j] < 0) {
+                page[j] = -2;
+            } else {
+                ks[j] = p.ks[page[j] * p.ks_stride[0] + (row[j] >> p.log) * p.ks_stride[1] + h * p.ks_stride[2]];
+                vs[j] = p.vs[page[j] * p.vs_stride[0] + (row[j] >> p.log) * p.vs_stride[1] + h * p.vs_stride[2]];
+            }
+        }
+        k_top = fmaxf(k_top, ks[j]);
+        v_top = fmaxf(v_top, vs[j]);
+    }
+    if (!__any_sync(0xffffffffu, any)) return;
+    const int entry = (int)fdiv((uint32_t)r0, prm.c.f_page), first = r0 - entry * (int)prm.c.f_page.d;
+    const int to = prm.dst_table[(long long)b * prm.dst_stride + entry];
+    if ((unsigned)to >= (unsigned)prm.c.n_pages) {
+        if (lane == 0) refuse_input(36);
+        return;
+    }
+    constexpr float kLeast = 9.094947017729282e-13f;  // 2^-40, where no row had a page
+    k_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(k_top))), kLeast);
+    v_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v_top))), kLeast);
+    if (lane == 0) {
+        p.ks[to * p.ks_stride[0] + (first >> p.log) * p.ks_stride[1] + h * p.ks_stride[2]] = k_top;
+        p.vs[to * p.vs_stride[0] + (first >> p.log) * p.vs_stride[1] + h * p.vs_stride[2]] = v_top;
+    }
+    constexpr int U = D / 16, RP = 32 / U;  // lanes to a row, rows at a time
+    const int e = lane % U * 16;
+#pragma unroll 4
+    for (int r = lane / U; r - lane / U < rows; r += RP) {
+        const int from = r & 31, j = r >> 5;
+        auto of = [&](auto (&v)[4]) { return __shfl_sync(0xffffffffu, j == 0 ? v[0] : j == 1 ? v[1] : j == 2 ? v[2] : v[3], from); };
+        const int pg = of(page), rw = of(row);
+        const float kr = of(ks), vr = of(vs);
+        if (pg == -1) continue;
+        uint4 kx = make_uint4(0, 0, 0, 0), vx = kx;
+        if (pg >= 0) {
+            kx = *reinterpret_cast<const uint4*>(prm.c.K + pg * prm.c.k_stride[0] + rw * prm.c.k_stride[1] + h * prm.c.k_stride[2] + e);
+            vx = *reinterpret_cast<const uint4*>(prm.c.V + pg * prm.c.v_stride[0] + rw * prm.c.v_stride[1] + h * prm.c.v_stride[2] + e);
+            if (kr != k_top) kx = rescale16(kx, __fdiv_rn(kr, k_top));
+            if (vr != v_top) vx = rescale16(vx, __fdiv_rn(vr, v_top));
+        }
+        *reinterpret_cast<uint4*>(prm.c.K + to * prm.c.k_stride[0] + (first + r) * prm.c.k_stride[1] + h * prm.c.k_stride[2] + e) = kx;
+        *reinterpret_cast<uint4*>(prm.c.V + to * prm.c.v_stride[0] + (first + r) * prm.c.v_stride[1] + h * prm.c.v_stride[2] + e) = vx;
+    }
+}
+
 constexpr float kOver127 = 1.f / 127.f;  // steps are max / 127 as the product with this number, rounded
 
 // ---- means of blocks --------------------------------------------------------------------------------------------------

@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     if (more) {
                         n_chosen += wrong ? __ffs(wrong) - 1 : 32;
                         more = wrong == 0;
-                        if (wrong && lane == __ffs(wrong) - 1 && chosen[k] != -1) refuse_input(36);
+                        if (wrong && lane == __ffs(wrong) - 1 && chosen[k] != -1) refuse_input(39);
                     }
                 }
             }

@@ -322,14 +322,16 @@ def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, he
 
 @_on_stream
 def kv_evict(weights, K_pages, V_pages, block_table, kv_len, dst_table, sink: int, recent: int, heavy: int, pos_shift=None,
-             weights_out=None, kv_len_out=None, pos_shift_out=None, stream=None):
+             weights_out=None, kv_len_out=None, pos_shift_out=None, k_scale=None, v_scale=None, stream=None):
     """Brings every sequence of more than sink + recent + heavy rows down to that many per KV head: the first `sink`, the last
     `recent` and the `heavy` rows of largest accumulated weight between them, copied in order to the pages of dst_table (int32
     [B, pages], none of them a page the sequence has now) - the C entry point `seg_kv_evict`.  Rows are moved as they are: an
-    8-bit cache's scales are not needed.  weights is fp32 [B, Hkv, W] as
+    8-bit cache's scales are not needed, unless it has one for each block of rows and head: those go with the rows (`k_scale`,
+    `v_scale`; the C entry point `seg_blocks_evict`).  weights is fp32 [B, Hkv, W] as
     seg_attn_decode gathers it.  Returns (idx int32 [B, Hkv, budget] (the slots kept, then -1), kv_len, pos_shift, weights) of
     the evicted cache, whose block table is dst_table; kv_len_out may be kv_len and pos_shift_out pos_shift."""
     c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, None, pos_shift, None, None, reads_values=False)
+    sc = _block_scales(k_scale, v_scale, K_pages, dev)
     _, dst_pages, dst_stride = _pages(dst_table, B, "dst_table", dev)
     W = weights.shape[-1] if weights.dim() == 3 else 0
     _flat(weights, _F32, (B, Hkv, W), "weights", dev)
@@ -340,6 +342,10 @@ def kv_evict(weights, K_pages, V_pages, block_table, kv_len, dst_table, sink: in
     weights_out = torch.empty_like(weights) if weights_out is None else _flat(weights_out, _F32, (B, Hkv, W), "weights_out", dev)
     kv_len_out = torch.empty_like(kv_len) if kv_len_out is None else _flat(kv_len_out, _I32, (B,), "kv_len_out", dev)
     pos_shift_out = torch.empty_like(kv_len) if pos_shift_out is None else _flat(pos_shift_out, _I32, (B,), "pos_shift_out", dev)
-    _call(dev, stream, lib().seg_kv_evict, "seg_kv_evict", c, weights.data_ptr(), W, sink, recent, heavy, dst_table.data_ptr(), dst_pages,
-          dst_stride, idx.data_ptr(), kv_len_out.data_ptr(), pos_shift_out.data_ptr(), weights_out.data_ptr())
+    args = (weights.data_ptr(), W, sink, recent, heavy, dst_table.data_ptr(), dst_pages, dst_stride, idx.data_ptr(), kv_len_out.data_ptr(),
+            pos_shift_out.data_ptr(), weights_out.data_ptr())
+    if sc is None:
+        _call(dev, stream, lib().seg_kv_evict, "seg_kv_evict", c, *args)
+    else:
+        _call(dev, stream, lib().seg_blocks_evict, "seg_blocks_evict", c, sc, *args)
     return idx, kv_len_out, pos_shift_out, weights_out

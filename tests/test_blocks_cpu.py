@@ -59,6 +59,10 @@ def select(c, m, Lq=1, Hq=4, S=64, T=16, mask=b"\0\1", Q=OK, qs=ST, n=4, sink=1,
     return sa.lib().seg_blocks_select(c, Lq, Hq, S, T, mask + bytes(64), Q, qs, m, n, sink, idx, None)
 
 
+def evict(c, sc, w=OK, W=128, sink=1, recent=20, heavy=10, dst=OK, pages=2, stride=2, idx=OK << 3, n=OK, s=OK, wo=OK << 4):
+    return sa.lib().seg_blocks_evict(c, sc, w, W, sink, recent, heavy, dst, pages, stride, idx, n, s, wo, None)
+
+
 def resize(B=2, Lq=4, page=16, n_pages=40, want=OK, table=OK, per=8, stride=8, n=OK, shift=None, free=OK, count=OK, n_out=OK, c_out=OK, q=OK, slots=OK,
            pos=OK, ws=OK, ws_bytes=1 << 30):
     return sa.lib().seg_pages_resize(B, Lq, page, n_pages, want, table, per, stride, n, shift, free, count, n_out, c_out, q, slots, pos, ws, ws_bytes, None)
@@ -69,7 +73,7 @@ def test_bad_caches_are_refused(bad):
     L = sa.lib()
     if "dtype" not in bad:
         c = eight(**bad)
-        assert decode(c, scales(), None) == 1 and append(c, scales()) == 1 and L.seg_attn_decode_blocks_workspace_bytes(c, scales(), None, 1, 4, 0) == 0
+        assert decode(c, scales(), None) == 1 and append(c, scales()) == 1 and evict(c, scales()) == 1 and L.seg_attn_decode_blocks_workspace_bytes(c, scales(), None, 1, 4, 0) == 0
         if "v_stride" not in bad and bad != dict(V=OK + 8):      # a summary reads keys alone
             assert summarise(c, scales(), means()) == 1
     c = cache(**bad)
@@ -81,7 +85,7 @@ def test_bad_caches_are_refused(bad):
 @pytest.mark.parametrize("bad", [dict(k=0), dict(v=0), dict(k=OK + 2), dict(v=OK + 1), dict(ks=(-8, 2, 1)), dict(vs=(8, 2, -1)), dict(rows=0), dict(rows=8),
                                  dict(rows=32), dict(rows=48), dict(rows=256)], ids=str)
 def test_bad_scales_are_refused(bad):
-    assert decode(eight(), scales(**bad), None) == 1 and append(eight(), scales(**bad)) == 1
+    assert decode(eight(), scales(**bad), None) == 1 and append(eight(), scales(**bad)) == 1 and evict(eight(), scales(**bad)) == 1
     if "v" not in bad and "vs" not in bad:
         assert summarise(eight(), scales(**bad), means()) == 1
 
@@ -89,7 +93,20 @@ def test_bad_scales_are_refused(bad):
 def test_scales_of_blocks_belong_to_an_8_bit_cache_without_others():
     for c in (cache(), cache(dtype=1, k_scale=OK, v_scale=OK), cache(dtype=1, k_scale=OK)):
         assert decode(c, scales(), None) == 1 and append(c, scales()) == 1 and summarise(c, scales(), means()) == 1
-    assert append(eight(), None) == 1 and decode(eight(), None, None) == 1
+    assert append(eight(), None) == 1 and decode(eight(), None, None) == 1 and evict(eight(), None) == 1
+
+
+@pytest.mark.parametrize("bad", [dict(ks=(0, 2, 1)), dict(ks=(8, 2, 0)), dict(vs=(8, 0, 1))], ids=str)
+def test_scales_that_are_written_are_apart(bad):
+    c = eight(page_size=32)
+    assert append(c, scales(**bad)) == 1 and evict(c, scales(**bad)) == 1
+    assert decode(c, scales(**bad), None, ws=None) == 5      # reading them is fine
+
+
+@pytest.mark.parametrize("bad", [dict(w=None), dict(W=127), dict(sink=-1), dict(sink=0, recent=0, heavy=0), dict(heavy=12), dict(dst=None), dict(stride=1),
+                                 dict(idx=None), dict(n=None), dict(wo=OK), dict(idx=OK)], ids=str)
+def test_bad_evictions_are_refused(bad):
+    assert evict(eight(), scales(), **bad) == 1
 
 
 @pytest.mark.parametrize("bad", [dict(idx=0), dict(idx=OK + 2), dict(n=0), dict(n=129), dict(n=-1), dict(block=0), dict(block=8), dict(block=32), dict(block=48)],
@@ -155,6 +172,7 @@ def test_bad_resizes_are_refused(bad):
 
 
 def test_nothing_to_do_is_fine_without_a_device():
+    assert evict(eight(B=0), scales()) == 0
     assert resize(B=0) == 0 and append(eight(B=0), scales()) == 0 and append(eight(), scales(), Lq=0) == 0
     assert decode(eight(B=0), scales(), None) == 0 and decode(cache(), None, choice(), Lq=0) == 0
     assert summarise(cache(B=0), None, means()) == 0 and summarise(cache(), None, means(), Lq=0) == 0 and summarise(cache(n_pages=0), None, means()) == 0

@@ -412,6 +412,50 @@ def test_rows_nobody_sees_do_not_matter(Lq, Hq, d):
         assert torch.equal(l2, lse) and torch.equal(O[:, :last], clean[:, :last]) and not torch.isfinite(O[:, last:].float()).any()
 
 
+# ---- eviction ---------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d,page,rows,lens,sink,recent,heavy", [(64, 16, 16, [200, 10, 40], 2, 20, 18), (128, 64, 32, [500, 131], 0, 64, 33), (128, 128, 128, [700], 4, 100, 200),
+                                                               (64, 96, 32, [300, 299], 1, 0, 98), (128, 32, 16, [90], 0, 45, 0)])
+def test_evicted_rows_keep_their_values(d, page, rows, lens, sink, recent, heavy):
+    B, Hkv, budget = len(lens), 3, sink + recent + heavy
+    need = -(-budget // page)
+    c = br.ScaledCache(lens, Hkv, d, page, rows, seed=d, spread=5, spare=3 + B * need)
+    dst = torch.tensor(c.spare[:B * need], dtype=torch.int32).view(B, need)
+    W = c.max_pages * page
+    w = torch.rand(B, Hkv, max(W, budget), generator=torch.Generator().manual_seed(1)).cuda()
+    old = [x.cpu().clone() for x in (c.K, c.V, c.scales["k_scale"], c.scales["v_scale"])]
+    idx, n2, s2, w2 = sa.kv_evict(w, c.K, c.V, dst_table=dst.cuda(), sink=sink, recent=recent, heavy=heavy, **c.dev, **c.scales)
+    sa.poll_status()
+    want = [x.clone() for x in old]
+    for b, n in enumerate(lens):
+        for h in range(Hkv):
+            keep = ref.evict_choice(w[b, h].tolist(), n, sink, recent, heavy)
+            assert idx[b, h].tolist() == keep + [-1] * (budget - len(keep))
+            for x, s in ((0, 2), (1, 3)):
+                for r0 in range(0, len(keep), rows):
+                    at = [(int(c.table[b, j // page]), j % page) for j in keep[r0:r0 + rows]]
+                    src = torch.stack([old[s][p, q // rows, h] for p, q in at])
+                    to, first = int(dst[b, r0 // page]), r0 % page
+                    want[s][to, first // rows, h] = src.max()
+                    y = torch.stack([old[x][p, q, h].float() for p, q in at]) * (src / src.max())[:, None]
+                    br.bits(want[x])[to, first:first + len(at), h] = br.bits(y.to(E4M3))
+        assert n2[b].item() == min(n, budget) and s2[b].item() == n - min(n, budget)
+    assert same8(c.K, want[0]) and same8(c.V, want[1])
+    for x, y in (("k_scale", want[2]), ("v_scale", want[3])):
+        assert torch.equal(torch.nan_to_num(c.scales[x].cpu(), nan=-1.0), torch.nan_to_num(y, nan=-1.0))
+    # and the attention goes on over the compacted cache
+    Q = rand(B, 1, 6, d)
+    O, lse = sa.seg_attn_decode(Q, c.K, c.V, dst.cuda(), n2, 1 << 30, 0, [1] * Hkv, **c.scales)
+    sa.poll_status()
+    x = br.attend(f64(Q), *c.values(), dst.numpy(), n2.tolist(), [1] * B, 1 << 30, 0, [1] * Hkv, d ** -0.5, page, v_scale=br.by_row(c.scales["v_scale"], page))
+    check(O, lse, x, [1] * B, d, True)
+    bad = c.dev["block_table"].clone()
+    bad[0, 0], d2 = -9, dst.clone()
+    d2[-1, 0] = 1 << 20
+    sa.kv_evict(w, c.K, c.V, bad, c.dev["kv_len"], d2.cuda(), sink, recent, heavy, **c.scales)
+    refused()
+
+
 # ---- means of blocks --------------------------------------------------------------------------------------------------------
 
 MEANS = [
