@@ -148,9 +148,9 @@ def _block_scales(k_scale, v_scale, K, dev: int):
     if k_scale is None or k_scale.dim() != 3:
         return None
     shape, pages = k_scale.shape, K.shape
-    for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-        if t is None or t.dtype is not _F32 or t.get_device() != dev or t.shape != shape:
-            raise ValueError("%s must be an fp32 tensor [n_pages, blocks of a page, Hkv] on CUDA device %d" % (what, dev))
+    if v_scale is None or k_scale.dtype is not _F32 or v_scale.dtype is not _F32 or k_scale.get_device() != dev or v_scale.get_device() != dev or \
+            v_scale.shape != shape:
+        raise ValueError("k_scale and v_scale must be fp32 tensors [n_pages, blocks of a page, Hkv] on CUDA device %d" % dev)
     if K.dtype is not _E4M3 or len(pages) != 4 or shape[0] != pages[0] or shape[2] != pages[2] or shape[1] < 1 or pages[1] % shape[1]:
         raise ValueError("scales of blocks belong to an 8-bit cache: [n_pages, page_size / rows, Hkv] of its pages")
     return _SCALES.pack(k_scale.data_ptr(), v_scale.data_ptr(), *k_scale.stride(), *v_scale.stride(), pages[1] // shape[1])
@@ -308,7 +308,7 @@ def seg_attn_decode(Q, K_pages, V_pages, block_table, kv_len, S: int, T: int, he
     if workspace is None:
         w = 0 if weights_out is None else 1
         need = L.seg_attn_decode_workspace_bytes(c, Lq, Hq, w) if plain else L.seg_attn_decode_blocks_workspace_bytes(c, sc, choice, Lq, Hq, w)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=Q.device)
+        workspace = Q.new_empty((max(need, 256),), dtype=torch.uint8)
     elif workspace.get_device() != dev:
         raise ValueError("workspace must be on the cache's device")
     args = (Lq, Hq, S, T, d ** -0.5 if sm_scale is None else sm_scale, _mask_bytes(head_past_mask, Hkv), Q.data_ptr(), qs, out.data_ptr(),

@@ -145,6 +145,19 @@ def test_resize_refuses_numbers_out_of_range(Lq):
     sa.poll_status()
 
 
+def test_resize_writes_the_lengths_where_they_were_asked_for():
+    B, page, per, n_pages = 1500, 16, 6, 5000
+    lens, table, free = pool(B, page, per, n_pages, 1)
+    r = random.Random(2)
+    want = [r.choice([0, x, min(per * page, x + 9)]) for x in lens]
+    n, t, f, c = device_pool(lens, table, free, n_pages)
+    w = ints(want)
+    got = sa.pages_resize(w, t, n, f, c, page, 9, kv_len_out=w, free_count_out=c)
+    sa.poll_status()
+    T, N, F, q, slots, pos = br.resize(want, table, lens, free, len(free), page, 9)
+    assert got[0] is w and w.tolist() == N and c.item() == len(F) and got[2].tolist() == q and got[3].tolist() == slots
+
+
 def test_resize_without_pages_or_sequences():
     e = torch.empty(0, dtype=torch.int32, device="cuda")
     got = sa.pages_resize(ints([3, 0]), torch.empty(2, 0, dtype=torch.int32, device="cuda"), ints([0, 0]), e, ints([0]), 16, 4)
@@ -454,6 +467,97 @@ def test_evicted_rows_keep_their_values(d, page, rows, lens, sink, recent, heavy
     d2[-1, 0] = 1 << 20
     sa.kv_evict(w, c.K, c.V, bad, c.dev["kv_len"], d2.cuda(), sink, recent, heavy, **c.scales)
     refused()
+
+
+# ---- layouts, empty caches, numbers out of range ------------------------------------------------------------------------------
+
+def test_layouts_and_strides():
+    lens, mask, S, T, block, n, page = [330, 147], [0, 1, 1, 1], 64, 16, 32, 3, 64
+    for kind in ("bf16", "heads", "blocks"):      # pages by heads, queries as a slice, outputs of their own strides
+        c = cache_of(kind, lens, 4, 64, page, block, seed=4, head_major=True)
+        Q = rand(2, 3, 8, 64, pad=2)
+        idx = random_choice(lens, [3, 3], 3, 4, S, T, block, n, seed=5)
+        a = run_chosen(c, Q, S, T, mask, idx, block)
+        wide = torch.full((2, c.max_pages + 5), -1, dtype=torch.int32, device="cuda")
+        wide[:, :c.max_pages] = c.dev["block_table"]
+        out = torch.zeros(2, 8, 3, 64, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+        _, lse = sa.seg_attn_decode(Q, c.K, c.V, wide[:, :c.max_pages], c.dev["kv_len"], S, T, mask, blocks=torch.from_numpy(idx).cuda(), block=block, out=out,
+                                    **c.scales)
+        assert torch.equal(out, a[0]) and torch.equal(lse, a[1])
+        sums, scale = old_means(c, block)
+        sa.blocks_summarise(c.K, wide[:, :c.max_pages], c.dev["kv_len"], 400, sums, scale, k_scale=c.scales.get("k_scale"))
+        X = br.dequantised(c.K, c.scales.get("k_scale"))
+        got = sa.blocks_select(Q, sums, scale, wide[:, :c.max_pages], c.dev["kv_len"], page, S, T, n, head_past_mask=mask)
+        for b, m in enumerate(lens):
+            for k in range(m // block):
+                at, row = int(c.table[b, k * block // page]), k * block % page
+                mq, ms = br.means(X[at, row:row + block], block)
+                assert np.array_equal(sums[at, row // block].cpu().numpy(), mq) and np.array_equal(scale[at, row // block].cpu().numpy(), ms)
+            want = br.select(f64(Q[b]), sums.cpu().numpy(), scale.cpu().numpy(), c.table[b].tolist(), m, 3, S, T, mask, page, block, n, 0)
+            assert np.array_equal(got[b].cpu().numpy(), want)
+        if kind == "blocks":
+            run_scaled(c, Q, S, T, mask, shift=[70, 0])
+            new = rand(2, 5, 4, 64, seed=8), rand(2, 5, 4, 64, seed=9)
+            flat = [x.contiguous() for x in (c.K, c.V, c.scales["k_scale"], c.scales["v_scale"])]
+            sa.kv_append(*new, c.K, c.V, **c.dev, **c.scales)
+            sa.kv_append(*new, flat[0], flat[1], k_scale=flat[2], v_scale=flat[3], **c.dev)
+            assert same8(c.K, flat[0]) and same8(c.V, flat[1]) and torch.equal(torch.nan_to_num(c.scales["k_scale"]), torch.nan_to_num(flat[2]))
+    sa.poll_status()
+
+
+def test_caches_without_pages_and_rows_before_the_first_slot():
+    e = torch.empty(3, 0, dtype=torch.int32, device="cuda")
+    z = ints([0, 0, 0])
+    for Lq in (1, 2):
+        idx = torch.full((3, Lq, 2, 4), -1, dtype=torch.int32, device="cuda")
+        for kind in (torch.bfloat16, E4M3):
+            K = torch.empty(0, 32, 2, 64, device="cuda").to(kind)
+            s = {} if kind == torch.bfloat16 else dict(k_scale=torch.ones(0, 2, 2, device="cuda"), v_scale=torch.ones(0, 2, 2, device="cuda"))
+            O, lse = sa.seg_attn_decode(rand(3, Lq, 4, 64), K, K, e, z, 64, 16, [0, 1], blocks=idx, block=16, **s)
+            sa.poll_status()
+            assert not O.any() and (lse == -math.inf).all()
+            sa.blocks_summarise(K, e, z, 5, torch.empty(0, 2, 2, 64, dtype=torch.int8, device="cuda"), torch.empty(0, 2, 2, device="cuda"), k_scale=s.get("k_scale"))
+            if s:
+                O, lse = sa.seg_attn_decode(rand(3, Lq, 4, 64), K, K, e, z, 64, 16, [0, 1], **s)
+                assert not O.any() and (lse == -math.inf).all()
+        got = sa.blocks_select(rand(3, Lq, 4, 64), torch.empty(0, 2, 2, 64, dtype=torch.int8, device="cuda"), torch.empty(0, 2, 2, device="cuda"), e, z, 32, 64, 16, 4,
+                               head_past_mask=[1, 1])
+        assert (got == -1).all()
+    sa.poll_status()
+    for kind in ("bf16", "blocks"):      # more new rows than slots: the first see nothing
+        c = cache_of(kind, [2, 40], 1, 64, 32, 16, seed=1)
+        idx = random_choice([2, 40], [4, 4], 4, 1, 8, 4, 16, 2, seed=1)
+        O, lse = run_chosen(c, rand(2, 4, 2, 64), 8, 4, [1], idx, 16)
+        assert not O[0, :2].any() and (lse[0, :, :2] == -math.inf).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "blocks"])
+def test_numbers_out_of_range_are_reported_and_not_followed(kind):
+    lens, S, T, block, n, page = [300, 200], 64, 16, 16, 4, 32
+    c = cache_of(kind, lens, 2, 64, page, block, seed=9)
+    idx = random_choice(lens, [1, 1], 1, 2, S, T, block, n, seed=2)
+    Q, mask = rand(2, 1, 4, 64), [1, 0]
+    clean, l0 = run_chosen(c, Q, S, T, mask, idx, block)
+    sums, scale = (x.cuda() for x in random_means(c, block, 1))
+    want = sa.blocks_select(Q, sums, scale, c.dev["block_table"], c.dev["kv_len"], page, S, T, n, head_past_mask=mask)
+    full = c.table.clone().clamp(min=0).cuda()
+    for bad_len, q in ((-1, 1), (c.max_pages * page + 1, 1), (300, -1), (300, 2)):
+        kw = dict(q_len=ints([q, 1]))
+        O, lse = sa.seg_attn_decode(Q, c.K, c.V, full, ints([bad_len, 200]), S, T, mask, blocks=torch.from_numpy(idx).cuda(), block=block, **kw, **c.scales)
+        refused()
+        assert torch.equal(O[1], clean[1]) and torch.equal(lse[1], l0[1])
+        got = sa.blocks_select(Q, sums, scale, full, ints([bad_len, 200]), page, S, T, n, head_past_mask=mask, **kw)
+        refused()
+        assert torch.equal(got[1], want[1])
+        before = sums.clone()
+        sa.blocks_summarise(c.K, full, ints([bad_len, 200]), 1, before, scale.clone(), k_scale=c.scales.get("k_scale"), **kw)
+        refused()
+        if kind == "blocks":
+            O, lse = sa.seg_attn_decode(Q, c.K, c.V, full, ints([bad_len, 200]), S, T, mask, **kw, **c.scales)
+            refused()
+            a, b = sa.seg_attn_decode(Q, c.K, c.V, S=S, T=T, head_past_mask=mask, **c.dev, **c.scales)
+            assert torch.equal(O[1], a[1]) and torch.equal(lse[1], b[1])
+    sa.poll_status()
 
 
 # ---- means of blocks --------------------------------------------------------------------------------------------------------
