@@ -29,6 +29,8 @@ def pages_resize(want, block_table, kv_len, free_pages, free_count, page_size: i
     free_count), the new rows of every sequence, and for each of them, [B, Lq], its row in the pages taken as one (int64, -1: not there) and
     its position (int32, pos_shift added), as kv_append and rope_rotate take them."""
     dev = want.get_device()
+    if dev < 0:
+        raise ValueError("pages are handed out on a CUDA device: want and the others lie there")
     B, per, stride = _pages(block_table, None, "block_table", dev)
     _flat(want, _I32, (B,), "want", dev)
     _flat(kv_len, _I32, (B,), "kv_len", dev)

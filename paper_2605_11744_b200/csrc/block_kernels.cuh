@@ -470,7 +470,7 @@ constexpr int kSelBins = 2048;
 constexpr int kSelFew = 256;                // as many are compared with each other one by one
 constexpr int kSelMost = 128;               // blocks that can be chosen
 constexpr int kSelKeys = 49152;             // blocks to choose from
-constexpr int kSelSlice = 1024;             // blocks that a thread block of a cluster has at least
+constexpr int kSelSlice = 512;              // blocks that a thread block of a cluster has at least
 constexpr uint32_t kSinkKey = 0xffffffffu;  // above every score's
 static_assert(kSelKeys / 32 <= kSelBins, "a bin for 32 neighbouring blocks");
 

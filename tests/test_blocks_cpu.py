@@ -194,8 +194,8 @@ def test_wrappers_refuse_what_is_not_a_cache():
         sa.blocks_summarise(K, t, n, 1, sums, sc)
     with pytest.raises(ValueError, match="CUDA|contiguous"):
         sa.blocks_select(torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16), sums, sc, t, n, 32, 64, 16, 4)
-    with pytest.raises(ValueError):
-        sa.pages_resize(n.long(), t, n, n, n, 16, 1)
+    with pytest.raises(ValueError, match="CUDA"):
+        sa.pages_resize(n, t, n, n, n, 16, 1)
     with pytest.raises(ValueError, match="8-bit"):
         paged._block_scales(sc, sc, K, -1)
     with pytest.raises(ValueError, match="8-bit"):

@@ -520,6 +520,10 @@ def test_caches_without_pages_and_rows_before_the_first_slot():
             if s:
                 O, lse = sa.seg_attn_decode(rand(3, Lq, 4, 64), K, K, e, z, 64, 16, [0, 1], **s)
                 assert not O.any() and (lse == -math.inf).all()
+            if s:      # rows without a place are reported, with queries and without
+                for q in (None, rand(3, Lq, 4, 64)):
+                    sa.kv_append(rand(3, Lq, 2, 64), rand(3, Lq, 2, 64), K, K, e, ints([1, 0, 2]), table=sa.rope_table_scaled(8, 64), Q=q, **s)
+                    refused()
         got = sa.blocks_select(rand(3, Lq, 4, 64), torch.empty(0, 2, 2, 64, dtype=torch.int8, device="cuda"), torch.empty(0, 2, 2, device="cuda"), e, z, 32, 64, 16, 4,
                                head_past_mask=[1, 1])
         assert (got == -1).all()
