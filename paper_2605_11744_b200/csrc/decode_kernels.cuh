@@ -400,6 +400,14 @@ constexpr float kHalfRoom = 13.f, kHalfTop = 15.f;
 // m exp2(score + e - base), so that fp16's range is spent on what a weight adds to O and not on the scale, whatever its size.  The
 // sum takes exp2(score + e - base) 2^-e, exactly.  Bases are whole numbers there (e - base is exact), and one lower for m.
 constexpr float kScaledRoom = 12.f, kScaledTop = 14.f;
+// LSE of a row from its base (log2 units) and sum.  A base with scales lies as far from the scores as the scales' exponents: it is a whole
+// number, and so is the sum's exponent, so these are added up first (as they stand, 2^-18 of a sum of 2^30 would be lost).
+__device__ __forceinline__ float lse_of(float base, float sum, bool scaled) {
+    const uint32_t bits = __float_as_uint(sum);
+    if (scaled && bits - 0x00800000u < 0x7f000000u)  // a normal number
+        return (base + (float)((int)(bits >> 23) - 127) + log2f(__uint_as_float((bits & 0x7fffffu) | 0x3f800000u))) * 0.6931471805599453f;
+    return sum == 0.f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
+}
 
 // BS: a scale for each block of rows (the members of DecodeParams from ks on), for FP8.  SEL: heads with a past read chosen blocks of
 // it and what their own segment and tail show them (from choice_log on); WM = 1.
@@ -621,7 +629,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
     const uint32_t v_lane = 16 * RB + (FP8 ? swizzled<RB>(lane & 15, lane >> 4) : swizzled<RB>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1));
 
     float o[MT][NT][4];        // O^T: (dim l4, row 2 q4), (dim l4, row 2 q4 + 1), (dim l4 + 8, ...) of 16-dim tiles
-    // A row's weights are exp2(score - base) so far: the base (0 until the row has seen a key), the sum over this lane's slots,
+    // A row's weights are exp2(score - base) so far: the base (0, or a scale's exponent, until the row has seen a key), the sum over this lane's slots,
     // and how far over the base a score has to be for the base to move (-inf until the row has seen a key).
     float base[NT][2], l[NT][2], slack[NT][2];
     uint32_t qf[KS][NT][2];
@@ -705,6 +713,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
         float* scores = p.scores;
         if (scores) scores += (((long long)get.b * p.c.Hkv + head) * p.g * p.c.Lq + get.rb * MB + wrow * WR) * p.pitch;
 
+        bool fresh = BS;  // no scale of the piece has been seen
         for (int left = count; left > 0; --left) {
             cp_async_wait<ST - 2>();
             if (WM == 1) __syncwarp();
@@ -785,6 +794,11 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) qs[k][nt][e] = BS ? qscale[nt][e] * sc.x : qscale[nt][e];
+                }
+                if (fresh) {  // bases begin where the scales are: a score is not rounded by how far that is from zero
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) base[nt][0] = base[nt][1] = vexp[0];
+                    fresh = false;
                 }
                 // element e of s[k][nt]: slot 16 k + js[e >> 1], row 2 q4 + (e & 1) of the warp's eight; log2 units over the base
                 const bool edge_range = slot0 < all_lo || slot0 + 16 * KP > all_hi;
@@ -1054,7 +1068,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     *reinterpret_cast<uint2*>(p.O + get.b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + d0) =
                         make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
                     if (d0 == 0)
-                        p.LSE[((long long)get.b * p.Hq + qh) * p.c.Lq + t] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
+                        p.LSE[((long long)get.b * p.Hq + qh) * p.c.Lq + t] = lse_of(mm, ll, BS);
                 } else {
                     // a part: slot 0 where the block's range begins inside the item, else slot 1
                     const long long at = ((long long)blockIdx.x * 2 + (first == 0 ? 1 : 0)) * Sh::kPartRows + w0 * WR + nt * 8 + r8;
@@ -1124,7 +1138,7 @@ __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ 
     for (int k = AHEAD; k < n; ++k) o += p.part_o[at(k) * D + tid] * weight[k];
     const int t = SEL ? rb / p.head_blocks : (int)fdiv((uint32_t)r, p.f_g), qh = h * p.g + (SEL ? rb % p.head_blocks * MB + rl : r - t * p.g);
     p.O[b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + tid] = __float2bfloat16(l == 0.f ? 0.f : o / l);
-    if (tid == 0) p.LSE[((long long)b * p.Hq + qh) * p.c.Lq + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    if (tid == 0) p.LSE[((long long)b * p.Hq + qh) * p.c.Lq + t] = lse_of(m, l, p.ks != nullptr);
 }
 
 // Attention weight of every slot, from the scores and the finished LSE: a block takes 256 slots of one (sequence, KV head), a

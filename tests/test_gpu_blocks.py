@@ -368,6 +368,22 @@ def test_scales_far_apart(d, Lq):
     run_scaled(c, 0.05 * rand(2, Lq, 4, d), 1 << 30, 0, [1, 1])
 
 
+@pytest.mark.parametrize("e", [-38, -20, 0, 25])
+def test_the_lse_does_not_lose_what_the_scales_of_v_are_away(e):
+    # scores near zero, so that the LSE is near ln n; a sum over 2^e in fp32 would be off by 2^-18 and more of it
+    for n, parts in ((1, False), (3, False), (700, True)):
+        c = br.ScaledCache([n] * 2, 2, 64, 16, 16, seed=n)
+        for x, s in (("k_scale", 2.0 ** -12), ("v_scale", 2.0 ** e)):
+            c.scales[x].fill_(s)
+        Q = rand(2, 1, 4, 64)
+        O, lse = sa.seg_attn_decode(Q, c.K, c.V, S=1 << 30, T=0, head_past_mask=[1, 1], **c.dev, **c.scales)
+        sa.poll_status()
+        want = br.attend(f64(Q), *c.values(), c.table.numpy(), c.lens, [1, 1], 1 << 30, 0, [1, 1], 64 ** -0.5, 16)
+        # a score's error, and a few roundings of numbers below log2 n + 1: of the sum, its logarithm and the conversion
+        bound = (64 + 8) * ref.FP32 * want[3] + 16 * ref.FP32 * (math.log(n) + 1)
+        assert (np.abs(lse.cpu().double().numpy() - want[1]) <= bound).all()
+
+
 def test_small_weights_beside_a_dominant_key():
     # 32K slots of which the first takes all but a thousandth of the weight and has no value: what comes out is the small weights' work.
     # Its own block's scale is the largest of all, or the smallest.
