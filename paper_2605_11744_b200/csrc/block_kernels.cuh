@@ -504,7 +504,7 @@ __device__ __forceinline__ void store_to_block(uint32_t* shared, uint32_t rank, 
 // Then the first block of the cluster chooses: digits of the keys (11, 11 and 10 bits, then the block's number over 32, lower numbers
 // first) narrow down where the n-th lies until few keys are left there, most times after one of them; those are compared one by
 // one, and the chosen numbers put in order in the same way.  Barriers and dependent reads are what it costs (16 x 4 heads of 2800-4000
-// blocks: 14 us for 28 MB of means, of which reading them takes 5), so there are few of them; a selection over histograms of the
+// blocks: 13.8 us for 28 MB of means, of which reading them takes 5), so there are few of them; a selection over histograms of the
 // whole cluster, with ordered scans for the numbers, took 17.5.
 template <int D>
 __global__ void __launch_bounds__(kSelThreads, 2) select_kernel(const __grid_constant__ SelectParams p) {

@@ -377,6 +377,8 @@ struct DecodeShape {
     static constexpr int kTileLog = KG == 1 ? 6 : 7;       // log2 of 64 KG, slots of a tile of one head
     static constexpr int kBlock = 2 * 16 * RB;             // 16 K rows and 16 V rows
     static constexpr int kWarpStage = KG * kBlock;
+    // with scales or a choice there are more instructions to a row and less of a warp's time is waiting for loads: a third warp to
+    // a scheduler, for a stage less (16 x 4 rows of chosen blocks 150 -> 139 us, 8 x 100-131K slots with scales 174 -> 172)
     static constexpr bool kThree = (BS || SEL) && RB == 128 && NT == 1 && FP8;
     static constexpr int kBlocksPerSm = kThree || (RB == 64 && NT == 1) ? 3 : 2;
     static constexpr int KP = KG == 2 || WM > 1 ? 2 : 1;   // blocks of 16 slots taken through the products at once
