@@ -91,7 +91,7 @@ __device__ __forceinline__ void rotate_queries(const AppendParams& prm, uint32_t
 // brought to the new one: by a power of two, which costs a value nothing but at the lowest octave of its range.  A stream over HBM:
 // 12K rows of 8 heads with 32 query heads take 55 us for 281 MB (5.1 TB/s; 43 us at the rate of a copy), with issue slots half used and
 // loads waited for; five and six thread blocks to an SM (51 and 42 registers) took 56 and 71 us, the queries' blocks first or in turn
-// with the others 56 and 61.  64 sequences' tokens: 3.5 us.
+// with the others 56 and 61.  64 sequences' tokens: 2.8 us.
 template <int D, bool INTERLEAVED, int G, int STEPS>
 __global__ void __launch_bounds__(256) append_blocks_kernel(const __grid_constant__ AppendBlocksParams p) {
     const AppendParams& a = p.a;
