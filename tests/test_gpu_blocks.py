@@ -368,6 +368,60 @@ def test_scales_far_apart(d, Lq):
     run_scaled(c, 0.05 * rand(2, Lq, 4, d), 1 << 30, 0, [1, 1])
 
 
+@pytest.mark.parametrize("e", [-30, 3])
+@pytest.mark.parametrize("Hq", [4, 16, 64])
+def test_scores_too_large_for_a_fraction(Hq, e):
+    # scores of 2e9, whose fp32 steps are 128: a base is rounded by more than the room above it, and nothing may overflow for it
+    n, d, page = 300, 64, 16
+    c = br.ScaledCache([n], 1, d, page, 16, seed=2)
+    br.bits(c.K)[:] = br.bits(torch.full((1,), 1.0).to(E4M3)).item()
+    for j, x in ((7, 448.0), (130, 448.0), (131, 416.0)):
+        c.K[c.table[0, j // page].long(), j % page] = torch.full((1, d), x, device="cuda").to(E4M3)
+    c.scales["k_scale"].fill_(8.0)
+    c.scales["v_scale"].fill_(2.0 ** e)
+    Q = torch.full((1, 1, Hq, d), 65536.0, dtype=torch.bfloat16, device="cuda")
+    O, lse = sa.seg_attn_decode(Q, c.K, c.V, S=1 << 30, T=0, head_past_mask=[1], **c.dev, **c.scales)
+    sa.poll_status()
+    # which of the two equal keys wins is within the scores' rounding; the row is their mean with some weights
+    vals = ref.rows_of(c.V, c.table[0].numpy(), n, page)[[7, 130], 0] * 2.0 ** e
+    slack = (2 * ref.FP16 + 1.02 * ref.BF16) * np.abs(vals).max(0)
+    got = f64(O)[0, 0]
+    assert (got >= vals.min(0) - slack).all() and (got <= vals.max(0) + slack).all()
+    top = d * 65536.0 * 448 * 8 * d ** -0.5
+    assert (np.abs(lse.cpu().double().numpy() - top) <= 8 * ref.FP32 * top).all()
+
+
+def test_two_streams_at_once():
+    # the same calls on two streams with buffers of their own, and a captured step replayed beside them
+    lens, S, T, block, n, page = [3000, 2000, 900], 64, 16, 16, 8, 64
+    c = br.ScaledCache(lens, 2, 128, page, 16, seed=2)
+    Qs = [rand(3, 2, 16, 128, seed=k) for k in range(3)]
+    outs = [old_means(c, block) for _ in range(3)]
+
+    def step(k):
+        sa.blocks_summarise(c.K, c.dev["block_table"], c.dev["kv_len"], 3000, *outs[k], k_scale=c.scales["k_scale"])
+        idx = sa.blocks_select(Qs[k], *outs[k], c.dev["block_table"], c.dev["kv_len"], page, S, T, n, head_past_mask=[1, 1])
+        return (idx,) + sa.seg_attn_decode(Qs[k], c.K, c.V, S=S, T=T, head_past_mask=[1, 1], blocks=idx, block=block, **c.dev, **c.scales)
+    want = [[x.clone() for x in step(k)] for k in range(3)]
+    torch.cuda.synchronize()
+    streams, gr = [torch.cuda.Stream() for _ in range(3)], torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr, stream=streams[2]):
+        kept = step(2)
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(25):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(step(k))
+        with torch.cuda.stream(streams[2]):
+            gr.replay()
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(a, b) for x in got[k] for a, b in zip(x, want[k]))
+    assert all(torch.equal(a, b) for a, b in zip(kept, want[2]))
+    sa.poll_status()
+
+
 @pytest.mark.parametrize("e", [-38, -20, 0, 25])
 def test_the_lse_does_not_lose_what_the_scales_of_v_are_away(e):
     # scores near zero, so that the LSE is near ln n; a sum over 2^e in fp32 would be off by 2^-18 and more of it
