@@ -504,7 +504,9 @@ typedef struct {
 /* seg_attn_decode over a cache with a scale for each block (scales, or NULL: as c says) and, or, with chosen blocks (choice, or NULL).
  * With a choice a head of class PAST sees the slots of its row's blocks and every slot from R block (see above) to the row's own; the other classes see
  * what they do without one, and weights_out must be NULL.  Each new row's choice is its own: a call of many rows reads the
- * slots they all see once for each.  Scales of V should lie within a factor of 2^100 of each other; those of unread blocks may hold anything.
+ * slots they all see once for each.  Scales may be any numbers, zero and negative ones too; those of V that are not zero should lie
+ * within a factor of 2^100 of each other, wherever that is.  One of V that is not finite makes O of the rows that see its block not finite, all of it
+ * (where their weight of the block is not below fp32's range), and leaves the LSE alone.  Those of unread blocks may hold anything.
  * Everything else is seg_attn_decode's, its workspace excepted: seg_attn_decode_blocks_workspace_bytes(...) of the same arguments. */
 size_t seg_attn_decode_blocks_workspace_bytes(const seg_kv_cache* c, const seg_block_scales* scales, const seg_block_choice* choice,
                                               int32_t Lq, int32_t Hq, int32_t with_weights);

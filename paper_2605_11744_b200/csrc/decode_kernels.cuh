@@ -398,18 +398,19 @@ constexpr float kDecSlack = 8.f;
 // by an eighth).  So the base is put 2^13 under the maximum, and moved when a weight would pass 2^15, fp16's largest power:
 // weights are exact to fp16's half step down to 2^-27 of the largest.
 constexpr float kHalfRoom = 13.f, kHalfTop = 15.f;
-// With a scale for each block of rows a weight goes into the product with V times its block's scale m 2^e (1 <= m < 2): as
+// With a scale for each block of rows a weight goes into the product with V times its block's scale m 2^e (1 <= |m| < 2): as
 // m exp2(score + e - base), so that fp16's range is spent on what a weight adds to O and not on the scale, whatever its size.  The
-// sum takes exp2(score + e - base) 2^-e, exactly.  Bases are whole numbers there (e - base is exact), and one lower for m.
+// sum takes exp2(score + e - base) 2^(ref - e), exactly, ref being the smallest e that the warp has met in the item: no weight adds more
+// than 2^14, so the sum cannot overflow wherever the scales lie.  Bases are whole numbers there (e - base is exact), and one lower for m.
+// A scale that has no such form - zero, an infinity, NaN - goes into the product as it is, at e = ref; a subnormal one has e = -126.
 constexpr float kScaledRoom = 12.f, kScaledTop = 14.f;
-// LSE of a row from its base (log2 units) and sum.  A base with scales lies as far from the scores as the scales' exponents: it is a whole
-// number, and so is the sum's exponent, so these are added up first (as they stand, 2^-18 of a sum of 2^30 would be lost).
-__device__ __forceinline__ float lse_of(float base, float sum, bool scaled) {
-    const uint32_t bits = __float_as_uint(sum);
-    if (scaled && bits - 0x00800000u < 0x7f000000u)  // a normal number
-        return (base + (float)((int)(bits >> 23) - 127) + log2f(__uint_as_float((bits & 0x7fffffu) | 0x3f800000u))) * 0.6931471805599453f;
-    return sum == 0.f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
-}
+// Beside such scales O is in units of this where a block's four warps add it up and in the parts: their sums may come to 8, and the
+// numbers of V to the end of fp32's range.  The join divides its parts' weights first, and not its O in the end, for the same reason.
+constexpr int kScaledUnitLog = 4;
+constexpr float kScaledUnit = 16.f;
+constexpr uint32_t kOneBits = 0x3f800000u, kInfBits = 0x7f800000u;
+// LSE of a row from its base (log2 units) and sum.
+__device__ __forceinline__ float lse_of(float base, float sum) { return sum == 0.f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f; }
 
 // BS: a scale for each block of rows (the members of DecodeParams from ks on), for FP8.  SEL: heads with a past read chosen blocks of
 // it and what their own segment and tail show them (from choice_log on); WM = 1.
@@ -425,6 +426,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
     __shared__ int warp_sum[4];
     __shared__ uint32_t there[ST][4];  // which of a warp's 16 KG slots were loaded, per stage
     __shared__ float2 end_ml[4][8];    // an item's end: base and sum of eight rows of each warp
+    __shared__ float2 end_power[BS ? 4 : 1][8];  // and the power of two that their O is in units of, as a product
     __shared__ __align__(16) float block_scale[(BS ? ST : 1) * 16];  // of K and V, for each of a warp's blocks of 16 slots: [ST][4][2][2]
     const uint32_t ring = (smem_u32(smem_raw) + 127u) & ~127u;
     uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
@@ -601,7 +603,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     const int to = s * 16 + warp * 4 + 2 * k + lane;
                     const long long* st = lane == 0 ? p.ks_stride : p.vs_stride;
                     if ((unsigned)page < (unsigned)p.c.n_pages) cp_async4(smem_u32(block_scale) + to * 4, s_item + page * st[0] + (prow >> p.scale_log) * st[1]);
-                    else block_scale[to] = 1.f;  // none of the 16 is there
+                    else block_scale[to] = 0.f;  // none of the 16 is there
                 }
             }
             if (lane == 0) there[s][warp] = loaded;
@@ -631,7 +633,7 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
     const uint32_t v_lane = 16 * RB + (FP8 ? swizzled<RB>(lane & 15, lane >> 4) : swizzled<RB>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1));
 
     float o[MT][NT][4];        // O^T: (dim l4, row 2 q4), (dim l4, row 2 q4 + 1), (dim l4 + 8, ...) of 16-dim tiles
-    // A row's weights are exp2(score - base) so far: the base (0, or a scale's exponent, until the row has seen a key), the sum over this lane's slots,
+    // A row's weights are exp2(score - base) so far: the base (0, or the scales' exponent, until the row has seen a key), the sum over this lane's slots,
     // and how far over the base a score has to be for the base to move (-inf until the row has seen a key).
     float base[NT][2], l[NT][2], slack[NT][2];
     uint32_t qf[KS][NT][2];
@@ -715,7 +717,8 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
         float* scores = p.scores;
         if (scores) scores += (((long long)get.b * p.c.Hkv + head) * p.g * p.c.Lq + get.rb * MB + wrow * WR) * p.pitch;
 
-        bool fresh = BS;  // no scale of the piece has been seen
+        uint32_t ref_bits = kInfBits;  // the bits of 2^ref; infinity: no scale of the piece has been seen that has an exponent
+
         for (int left = count; left > 0; --left) {
             cp_async_wait<ST - 2>();
             if (WM == 1) __syncwarp();
@@ -741,6 +744,9 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) s2[x][k][nt][e] = 0.f;
+                // the scales of K and V in each of the two blocks of slots; asked for in front of the products, which they are needed behind
+                float4 sc = make_float4(1.f, 1.f, 1.f, 1.f);
+                if (BS) sc = *reinterpret_cast<const float4*>(block_scale + stage * 16 + from * 4);
                 if (FP8) {
 #pragma unroll
                     for (int v = 0; v < D / 64; ++v) {
@@ -779,28 +785,58 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[k][nt][e] = CH == 1 ? s2[0][k][nt][e] : s2[0][k][nt][e] + s2[CH - 1][k][nt][e];
-                // score scales of the rows in each block of slots; m, e and 2^-e of V's scales
+                // score scales of the rows in each block of slots; m, e and 2^(ref - e) of V's scales
                 float qs[KP][NT][2], vsc[KP], vexp[KP], vinv[KP];
+                // Scales that are read in the plain way: positive, with exponents from ref to ref + 126.
+                const uint32_t span = min(126u << 23, kInfBits - ref_bits);
+                bool plain = true;
 #pragma unroll
                 for (int k = 0; k < KP; ++k) {
-                    float2 sc = make_float2(1.f, 1.f);
+                    const float ks = k == 0 ? sc.x : sc.z, vs = k == 0 ? sc.y : sc.w;
                     if (BS) {
-                        sc = *reinterpret_cast<const float2*>(block_scale + stage * 16 + from * 4 + 2 * k);
-                        const uint32_t bits = __float_as_uint(sc.y);
-                        const int e = min(max((int)((bits >> 23) & 0xffu) - 127, -126), 126);
-                        vsc[k] = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
-                        vexp[k] = (float)e;
-                        vinv[k] = __uint_as_float((uint32_t)(127 - e) << 23);
+                        const uint32_t bits = __float_as_uint(vs);
+                        plain = plain && bits - ref_bits < span;
+                        vsc[k] = __uint_as_float((bits & 0x7fffffu) | kOneBits);
+                        vexp[k] = __uint_as_float(0x4b000000u | (bits >> 23)) - 8388735.f;  // 2^23 + 127
+                        vinv[k] = __uint_as_float(ref_bits + kOneBits - (bits & kInfBits));
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) qs[k][nt][e] = BS ? qscale[nt][e] * sc.x : qscale[nt][e];
+                        for (int e = 0; e < 2; ++e) qs[k][nt][e] = BS ? qscale[nt][e] * ks : qscale[nt][e];
                 }
-                if (fresh) {  // bases begin where the scales are: a score is not rounded by how far that is from zero
+                if (BS && !plain) {
+                    const bool first = ref_bits == kInfBits;
+                    int ref = first ? 127 : (int)(ref_bits >> 23), low = 255, ve[KP];  // exponents as they stand in a number's bits
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) base[nt][0] = base[nt][1] = vexp[0];
-                    fresh = false;
+                    for (int k = 0; k < KP; ++k) {
+                        const float vs = k == 0 ? sc.y : sc.w;
+                        const uint32_t size = __float_as_uint(vs) & 0x7fffffffu;
+                        ve[k] = size == 0 ? 255 : max((int)(size >> 23), 1);
+                        vsc[k] = size == 0 || size >= kInfBits ? vs
+                                 : size < 1u << 23 ? vs * 0x1p126f : __uint_as_float((__float_as_uint(vs) & 0x807fffffu) | kOneBits);
+                        low = min(low, ve[k]);
+                    }
+                    if (low < (first ? 255 : ref)) {
+                        // Bases begin where the scales are: a score is not rounded by how far that is from zero.  Scales without an exponent in
+                        // front of the first may have moved them: from there, with nothing in O that depends on it.  Later ref only falls.
+                        const float f = __uint_as_float((uint32_t)max(127 + low - ref, 0) << 23);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                if (first) base[nt][e] += (float)(low - ref);
+                                else l[nt][e] *= f;
+                            }
+                        ref = low;
+                        ref_bits = (uint32_t)ref << 23;
+                    }
+#pragma unroll
+                    for (int k = 0; k < KP; ++k) {
+                        if (ve[k] == 255) ve[k] = ref;
+                        vexp[k] = (float)(ve[k] - 127);
+                        vinv[k] = __uint_as_float((uint32_t)max(127 + ref - ve[k], 0) << 23);
+                    }
                 }
                 // element e of s[k][nt]: slot 16 k + js[e >> 1], row 2 q4 + (e & 1) of the warp's eight; log2 units over the base
                 const bool edge_range = slot0 < all_lo || slot0 + 16 * KP > all_hi;
@@ -879,17 +915,27 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     }
                 }
                 uint32_t pf[KP][NT][2];
-                const bool fractions = BS && (vsc[0] != 1.f || vsc[KP - 1] != 1.f);  // scales that are no powers of two
 #pragma unroll
                 for (int k = 0; k < KP; ++k)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             s[k][nt][e] = ex2(s[k][nt][e]);
                             l[nt][e & 1] = BS ? fmaf(s[k][nt][e], vinv[k], l[nt][e & 1]) : l[nt][e & 1] + s[k][nt][e];
-                            if (BS && fractions) s[k][nt][e] *= vsc[k];
                         }
+                if (BS && (vsc[0] != 1.f || vsc[KP - 1] != 1.f)) {  // scales that are no (positive) powers of two
+#pragma unroll
+                    for (int k = 0; k < KP; ++k)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[k][nt][e] = s[k][nt][e] == 0.f ? 0.f : s[k][nt][e] * vsc[k];  // hidden: not 0 times NaN
+                }
+#pragma unroll
+                for (int k = 0; k < KP; ++k)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
                         pf[k][nt][0] = movm_t(pack16<FP8>(s[k][nt][0], s[k][nt][1]));
                         pf[k][nt][1] = movm_t(pack16<FP8>(s[k][nt][2], s[k][nt][3]));
                     }
@@ -1035,8 +1081,29 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
 #pragma unroll
                 for (int e = 0; e < 4; ++e) mine[(2 * q4 + (e & 1)) * D + ((k2 * 16 + l4 + 8 * (e >> 1)) ^ (q4 << 3))] = o[k2][nt][e];
             if (l4 == 0) {
-                end_ml[warp][2 * q4] = make_float2(slack[nt][0] == -INFINITY ? -INFINITY : base[nt][0], l[nt][0]);
-                end_ml[warp][2 * q4 + 1] = make_float2(slack[nt][1] == -INFINITY ? -INFINITY : base[nt][1], l[nt][1]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float m = slack[nt][e] == -INFINITY ? -INFINITY : base[nt][e], sum = l[nt][e];
+                    if (BS) {
+                        // The true sum is sum 2^(base - ref) and O in units of 2^(base - ref) 2^ref.  The sum is brought to [1, 2): whole
+                        // numbers are added up first, and the LSE is not rounded by how far the scales are from one.
+                        const uint32_t bits = __float_as_uint(sum);
+                        int power = ref_bits == kInfBits ? 0 : (int)(ref_bits >> 23) - 127;
+                        m -= (float)power;
+                        if (bits - 0x00800000u < 0x7f000000u) {  // a normal number
+                            const int up = (int)(bits >> 23) - 127;
+                            m += (float)up;
+                            sum = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
+                            power -= up;
+                        }
+                        // in two factors, as their product may be out of range
+                        power -= kScaledUnitLog;
+                        const int half = power >> 1;
+                        end_power[warp][2 * q4 + e] =
+                            make_float2(__uint_as_float((uint32_t)max(127 + half, 0) << 23), __uint_as_float((uint32_t)max(127 + power - half, 0) << 23));
+                    }
+                    end_ml[warp][2 * q4 + e] = make_float2(m, sum);
+                }
             }
             __syncthreads();
             constexpr int TPR = D / 4;  // threads to a row
@@ -1048,17 +1115,25 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                 int t, hq;
                 if (!row_of<MB, SEL>(p, get.rows, get.rb, (WM == 1 ? 0 : w0 * WR) + nt * 8 + r8, &t, &hq)) continue;
                 const int h = p.head_order[get.first_head + (WM == 1 ? w0 : 0)];
-                const float vs = FP8 && !BS ? p.v_scale[h] : 1.f;
+                const float vs = BS ? kScaledUnit : FP8 ? p.v_scale[h] : 1.f;
                 float mm = -INFINITY, ll = 0.f;
                 float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
                 for (int w = w0; w < 4; w += side) mm = fmaxf(mm, end_ml[w][r8].x);
                 const float top = mm == -INFINITY ? 0.f : mm;
                 for (int w = w0; w < 4; w += side) {
                     const float2 ml = end_ml[w][r8];
-                    const float f = ex2(ml.x - top);
-                    const float4 y = *reinterpret_cast<const float4*>(
+                    float f = ex2(ml.x - top);
+                    float4 y = *reinterpret_cast<const float4*>(
                         ring_ptr + (size_t)(free_stage * 4 + w) * Sh::kWarpStage + (r8 * D + (d0 ^ ((r8 >> 1) << 3))) * 4);
                     ll += ml.y * f;
+                    if (BS) {
+                        const float2 power = end_power[w][r8];
+                        f *= power.x;
+                        y.x *= power.y;
+                        y.y *= power.y;
+                        y.z *= power.y;
+                        y.w *= power.y;
+                    }
                     x.x += y.x * f;
                     x.y += y.y * f;
                     x.z += y.z * f;
@@ -1070,11 +1145,11 @@ __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, FP8, NT, WM, BS, S
                     *reinterpret_cast<uint2*>(p.O + get.b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + d0) =
                         make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
                     if (d0 == 0)
-                        p.LSE[((long long)get.b * p.Hq + qh) * p.c.Lq + t] = lse_of(mm, ll, BS);
+                        p.LSE[((long long)get.b * p.Hq + qh) * p.c.Lq + t] = lse_of(mm, ll);
                 } else {
                     // a part: slot 0 where the block's range begins inside the item, else slot 1
                     const long long at = ((long long)blockIdx.x * 2 + (first == 0 ? 1 : 0)) * Sh::kPartRows + w0 * WR + nt * 8 + r8;
-                    *reinterpret_cast<float4*>(p.part_o + at * D + d0) = make_float4(x.x * vs, x.y * vs, x.z * vs, x.w * vs);
+                    *reinterpret_cast<float4*>(p.part_o + at * D + d0) = BS ? x : make_float4(x.x * vs, x.y * vs, x.z * vs, x.w * vs);
                     if (d0 == 0) p.part_ml[at] = make_float2(mm, ll);
                 }
             }
@@ -1119,6 +1194,7 @@ __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ 
 #pragma unroll
     for (int k = 0; k < D / 32; ++k) m = fmaxf(m, red[0][k]);
     const float base = m == -INFINITY ? 0.f : m;
+    const bool scaled = p.ks != nullptr;
     float l = 0.f;
     for (int k = tid; k < n; k += D) {
         const float2 ml = p.part_ml[at(k)];
@@ -1133,14 +1209,15 @@ __global__ void __launch_bounds__(D) decode_join_kernel(const __grid_constant__ 
 #pragma unroll
     for (int k = 0; k < D / 32; ++k) l += red[1][k];
     float o = 0.f;
+    const float share = scaled ? kScaledUnit / l : 1.f;
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k)
-        if (k < n) o += ahead[k] * weight[k];
+        if (k < n) o += ahead[k] * (weight[k] * share);
 #pragma unroll 8
-    for (int k = AHEAD; k < n; ++k) o += p.part_o[at(k) * D + tid] * weight[k];
+    for (int k = AHEAD; k < n; ++k) o += p.part_o[at(k) * D + tid] * (weight[k] * share);
     const int t = SEL ? rb / p.head_blocks : (int)fdiv((uint32_t)r, p.f_g), qh = h * p.g + (SEL ? rb % p.head_blocks * MB + rl : r - t * p.g);
-    p.O[b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + tid] = __float2bfloat16(l == 0.f ? 0.f : o / l);
-    if (tid == 0) p.LSE[((long long)b * p.Hq + qh) * p.c.Lq + t] = lse_of(m, l, p.ks != nullptr);
+    p.O[b * p.o_stride[0] + t * p.o_stride[1] + qh * p.o_stride[2] + tid] = __float2bfloat16(l == 0.f ? 0.f : scaled ? o : o / l);
+    if (tid == 0) p.LSE[((long long)b * p.Hq + qh) * p.c.Lq + t] = lse_of(m, l);
 }
 
 // Attention weight of every slot, from the scores and the finished LSE: a block takes 256 slots of one (sequence, KV head), a
