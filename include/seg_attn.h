@@ -481,6 +481,8 @@ typedef struct {
     int32_t block;
 } seg_block_means;
 /* Means of every block that holds one of the sequence's newest q_len (NULL: Lq) rows and is full; other blocks' are left as they were.
+ * With `scales` of more rows than a mean's block: of every full block in a scale's block that holds one, up to the sequence's end, since the
+ * append that brought them may have raised that scale and rounded all its rows anew.
  * The cache's V is not read; `scales` is NULL or its blocks' (of which only those of K are read).  One kernel. */
 segattn_status seg_blocks_summarise(const seg_kv_cache* c, const seg_block_scales* scales, int32_t Lq, const seg_block_means* means, void* stream);
 /* The choice of each new row t and KV head.  For a head of class PAST, with lo the lowest slot that a head of class LOCAL would show

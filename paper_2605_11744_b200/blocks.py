@@ -72,7 +72,8 @@ def _means(sums, sum_scale, page_size: int, dev: int):
 
 @_on_stream
 def blocks_summarise(K_pages, block_table, kv_len, Lq: int, sums, sum_scale, q_len: Optional[torch.Tensor] = None, k_scale=None, stream=None):
-    """Mean keys of the blocks that hold one of the newest q_len (None: Lq) rows of a sequence and are full, into sums (int8
+    """Mean keys of the blocks that hold one of the newest q_len (None: Lq) rows of a sequence and are full (and of those that share a
+    scale's block with such a row, whose rows the append may have rounded anew), into sums (int8
     [n_pages, page_size / block, Hkv, d]) times sum_scale (fp32 [n_pages, page_size / block, Hkv]) - the C entry point
     `seg_blocks_summarise`.  kv_len counts the new rows already; to rebuild all means, pass Lq = max_pages * page_size."""
     dev = K_pages.get_device()

@@ -291,7 +291,7 @@ struct SummariseParams {
     int ks_log;
     int8_t* sums;               // [n_pages][blocks of a page][Hkv][D]
     float* sum_scale;           // [n_pages][blocks of a page][Hkv]
-    FastDiv f_heads, f_blocks;  // Hkv; blocks that the new rows of a sequence can touch
+    FastDiv f_heads, f_blocks;  // Hkv; blocks whose means the new rows of a sequence can change
     uint32_t units;             // B * blocks * Hkv
     int log, per_page;          // log2 of a block's rows; blocks of a page
 };
@@ -305,7 +305,7 @@ __device__ __forceinline__ void add_halves(float& lo, float& hi, uint32_t x) {
     asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.f32.f16 %0, a, %0;\n\tadd.f32.f16 %1, b, %1;\n\t}" : "+f"(lo), "+f"(hi) : "r"(x));
 }
 
-// A warp takes one head's block of rows, if the new rows have filled it, 16 rows (which have one scale) at a time: the mean of its
+// A warp takes one head's block of rows, if it is full and the new rows may have changed it, 16 rows (which have one scale) at a time: the mean of its
 // keys in double, then c = max |mean| / 127 and the mean in steps of c.  HBM is to bound it, so a value costs few instructions and
 // hardly any of them in double precision, where a conversion alone takes the time of a dozen others: values of an 8-bit cache are
 // multiples of 2^-9, of which a lane adds up 32 at most in fp32, and the lanes their sums as integers, exactly; bf16 numbers are put
@@ -324,7 +324,8 @@ __global__ void __launch_bounds__(32 * kSumWarps, 6) summarise_kernel(const __gr
     const int h = (int)(unit - bk * p.f_heads.d), k = (int)(bk - b * p.f_blocks.d);
     const int rows = new_rows(p.c, b), n = seq_len(p.c, b);
     if (rows == 0) return;
-    const int start = ((max(n - rows, 0) >> p.log) + k) << p.log;
+    // from the block that the first new row lies in, or all of its scale's block: an append may have raised that, with all its rows
+    const int whole = max(p.log, p.ks_log), start = (max(n - rows, 0) >> whole << whole) + (k << p.log);
     if ((long long)start + (1 << p.log) > n) return;
     int prow;
     const int page = page_of(p.c, b, start, &prow);

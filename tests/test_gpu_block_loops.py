@@ -1,0 +1,86 @@
+"""What a decoding loop relies on from one call to the next: means that follow rescaled rows, free lists of empty batches, scales that
+are carried along or refused, numbers at the ends of their types."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import blocks_ref as br
+import paged_ref as ref
+import paper_2605_11744_b200 as sa
+
+pytestmark = pytest.mark.gpu
+E4M3 = torch.float8_e4m3fn
+
+
+def ints(x, kind=torch.int32):
+    return torch.tensor(x, dtype=kind, device="cuda")
+
+
+def rand(*shape, seed=0):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(300 + seed)).bfloat16().cuda()
+
+
+def refused():
+    with pytest.raises(sa.SegAttnError) as e:
+        sa.poll_status()
+    assert e.value.status == 1
+
+
+def fresh_means(c, block):
+    n_pages, page, Hkv, d = c.K.shape
+    return torch.full((n_pages, page // block, Hkv, d), 9, dtype=torch.int8, device="cuda"), torch.full((n_pages, page // block, Hkv), 7.0, device="cuda")
+
+
+def same_means(c, block, got, lens):
+    """The means of all full blocks are those of the rows that the cache holds now."""
+    X = br.dequantised(c.K, c.scales["k_scale"])
+    for b, n in enumerate(lens):
+        for j in range(n // block):
+            at, row = int(c.table[b, j * block // c.page]), j * block % c.page
+            q, s = br.means(X[at, row:row + block], block)
+            assert np.array_equal(got[0][at, row // block].cpu().numpy(), q) and np.array_equal(got[1][at, row // block].cpu().numpy(), s), (b, j)
+
+
+@pytest.mark.parametrize("d,page,rows,block", [(64, 64, 64, 16), (128, 128, 128, 32), (128, 128, 64, 32), (64, 128, 32, 16), (64, 128, 64, 128), (128, 96, 32, 32)])
+def test_means_follow_rows_that_an_append_rescales(d, page, rows, block):
+    # keys grow along the sequence, so that tokens raise the scales of half-filled blocks again and again; steps of one token are captured
+    # and replayed, those of several run as they come, and idle sequences stay as they are
+    lens, Hkv = [0, 0, 0], 2
+    c = br.ScaledCache([300] * 3, Hkv, d, page, rows, seed=1)
+    means = fresh_means(c, block)
+    n = ints(lens)
+    kw = dict(block_table=c.dev["block_table"], kv_len=n)
+
+    def step(K, V, q):
+        sa.kv_append(K, V, c.K, c.V, q_len=q, **kw, **c.scales)
+        sa.blocks_summarise(c.K, c.dev["block_table"], n, K.shape[1], *means, q_len=q, k_scale=c.scales["k_scale"])
+
+    graphs = {}
+    for Lq in (1, 9):
+        K, V, q = rand(3, Lq, Hkv, d), rand(3, Lq, Hkv, d), ints([0] * 3)
+        step(K, V, q)
+        torch.cuda.synchronize()
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            step(K, V, q)
+        graphs[Lq] = gr, K, V, q
+    for k in range(40):
+        Lq = 1 if k % 4 else 9
+        gr, K, V, q = graphs[Lq]
+        new = [min(Lq, 300 - x) if (k + b) % 5 else 0 for b, x in enumerate(lens)]
+        lens = [x + y for x, y in zip(lens, new)]
+        for t, s in ((K, 2 * k), (V, 2 * k + 1)):
+            t.copy_(rand(*t.shape, seed=s) * 2.0 ** (k // 3))
+        n.copy_(ints(lens))
+        q.copy_(ints(new))
+        gr.replay()
+    same_means(c, block, means, lens)
+    for k, Lq in enumerate((70, 33, 5)):
+        new = [min(Lq, 300 - x) for x in lens]
+        lens = [x + y for x, y in zip(lens, new)]
+        n.copy_(ints(lens))
+        step(rand(3, Lq, Hkv, d, seed=90 + k) * 2.0 ** (14 + 2 * k), rand(3, Lq, Hkv, d, seed=95 + k), ints(new))
+        same_means(c, block, means, lens)
+    sa.poll_status()
