@@ -461,8 +461,8 @@ segattn_status seg_blocks_append(const seg_kv_cache* c, const seg_block_scales* 
                                  const int64_t q_stride[3], void* Q_out, const int64_t qo_stride[3], const float* table,
                                  int32_t n_pos, int32_t rot_dim, int32_t layout, void* stream);
 
-/* seg_kv_evict (same arguments, same rows kept) for such a cache: the kept rows' new blocks take the largest of their rows' scales, and
- * a row whose scale was smaller is brought to it as above.  Scales must not share elements, neither here nor in the append (a zero stride
+/* seg_kv_evict (same arguments, same rows kept) for such a cache: the kept rows' new blocks take the largest magnitude of their rows' finite
+ * scales (2^-40 where that is zero), and a row of another scale is brought to it as above (one whose scale is not finite becomes NaN or saturates).  Scales must not share elements, neither here nor in the append (a zero stride
  * is SEGATTN_ERR_INVALID).  (seg_kv_evict itself moves rows as they are, without their blocks' scales.)  Two kernels. */
 segattn_status seg_blocks_evict(const seg_kv_cache* c, const seg_block_scales* scales, const float* weights, int32_t W, int32_t sink,
                                 int32_t recent, int32_t heavy, const int32_t* dst_table, int32_t dst_max_pages, int32_t dst_stride,

@@ -206,8 +206,8 @@ struct EvictBlocksParams {
 };
 
 // A warp writes one block of the compacted cache for one head: its rows come from blocks of all kinds, so it takes the largest of their
-// scales, and a row whose scale was smaller is brought to it (exactly but at the lowest octave, as in an append; no row's largest value
-// has to be looked for).  Runs after evict_select_kernel; the lengths and shifts are written here as in evict_move_kernel.
+// scales in magnitude, and a row of another scale is brought to it (exactly but at the lowest octave where both are powers of two, as in an
+// append; no row's largest value has to be looked for).  A scale that is not finite has no say: its row becomes NaN, or saturates.  Runs after evict_select_kernel; the lengths and shifts are written here as in evict_move_kernel.
 template <int D>
 __global__ void __launch_bounds__(256) evict_move_blocks_kernel(const __grid_constant__ EvictBlocksParams p) {
     const EvictParams& prm = p.e;
@@ -243,8 +243,9 @@ __global__ void __launch_bounds__(256) evict_move_blocks_kernel(const __grid_con
                 vs[j] = p.vs[page[j] * p.vs_stride[0] + (row[j] >> p.log) * p.vs_stride[1] + h * p.vs_stride[2]];
             }
         }
-        k_top = fmaxf(k_top, ks[j]);
-        v_top = fmaxf(v_top, vs[j]);
+        const float k_size = fabsf(ks[j]), v_size = fabsf(vs[j]);
+        if (k_size <= FLT_MAX) k_top = fmaxf(k_top, k_size);
+        if (v_size <= FLT_MAX) v_top = fmaxf(v_top, v_size);
     }
     if (!__any_sync(0xffffffffu, any)) return;
     const int entry = (int)fdiv((uint32_t)r0, prm.c.f_page), first = r0 - entry * (int)prm.c.f_page.d;
@@ -253,9 +254,10 @@ __global__ void __launch_bounds__(256) evict_move_blocks_kernel(const __grid_con
         if (lane == 0) refuse_input(36);
         return;
     }
-    constexpr float kLeast = 9.094947017729282e-13f;  // 2^-40, where no row had a page
-    k_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(k_top))), kLeast);
-    v_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v_top))), kLeast);
+    k_top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(k_top)));
+    v_top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v_top)));
+    if (k_top == 0.f) k_top = 0x1p-40f;  // no row had a page, or a scale to go by
+    if (v_top == 0.f) v_top = 0x1p-40f;
     if (lane == 0) {
         p.ks[to * p.ks_stride[0] + (first >> p.log) * p.ks_stride[1] + h * p.ks_stride[2]] = k_top;
         p.vs[to * p.vs_stride[0] + (first >> p.log) * p.vs_stride[1] + h * p.vs_stride[2]] = v_top;

@@ -1,4 +1,4 @@
-"""Scales of blocks that no append writes: zero, negative, not finite, and small or large throughout, in the attention,
+"""Scales of blocks that no append writes: zero, negative, not finite, and small or large throughout, in the attention and the eviction,
 against the definition (a stored element x stands for x times its block's scale) in 64 bits."""
 import math
 
@@ -185,3 +185,38 @@ def test_scales_that_drift_along_parts_of_a_long_sequence():
                     at = j if up else k - 1 - j
                     put(c, b, [j], 0.0 if j % 7 == 2 or (seed and j < 40) else 2.0 ** (98 * at // (k - 1) - 49) * (1.0 if seed else 1.375))
             compare(c, query(2, 1, 4, d, seed=seed, size=0.3), 1 << 30, 0, [1, 1])
+
+
+@pytest.mark.parametrize("unit", [1.0, 2.0 ** -70, 2.0 ** 80])
+@pytest.mark.parametrize("d,page,rows", [(64, 32, 16), (128, 64, 64)])
+def test_evicted_rows_keep_values_of_any_scale(d, page, rows, unit):
+    # the new block's scale is the largest magnitude of its rows' finite ones; what a row stood for, it stands for afterwards
+    n, Hkv, sink, recent, heavy = 300, 2, 3, 40, 50
+    budget = sink + recent + heavy
+    need = -(-budget // page)
+    c = br.ScaledCache([n], Hkv, d, page, rows, seed=d, spare=3 + need)
+    c.K.copy_((4 * torch.randn(c.K.shape, generator=torch.Generator().manual_seed(2))).clamp(-400, 400).cuda().to(E4M3))
+    c.V.copy_((4 * torch.randn(c.K.shape, generator=torch.Generator().manual_seed(3))).clamp(-400, 400).cuda().to(E4M3))
+    for x, shift in (("k_scale", 0), ("v_scale", 1)):
+        for j in range(-(-n // rows)):
+            put(c, 0, [j], unit * (0.5, -4.0, 0.0, -0.25, math.nan, 2.0)[(j + shift) % 6], which=x)
+    dst = torch.tensor(c.spare[:need], dtype=torch.int32).view(1, need)
+    W = c.max_pages * page
+    w = torch.rand(1, Hkv, max(W, budget), generator=torch.Generator().manual_seed(1)).cuda()
+    before = [x.cpu().clone() for x in (c.K, c.V, c.scales["k_scale"], c.scales["v_scale"])]
+    idx, *_ = sa.kv_evict(w, c.K, c.V, dst_table=dst.cuda(), sink=sink, recent=recent, heavy=heavy, **c.dev, **c.scales)
+    sa.poll_status()
+    for x, s, pages, scales in ((0, 2, c.K, c.scales["k_scale"]), (1, 3, c.V, c.scales["v_scale"])):
+        for h in range(Hkv):
+            keep = idx[0, h].tolist()
+            for r0 in range(0, budget, rows):
+                at = [(int(c.table[0, j // page]), j % page) for j in keep[r0:r0 + rows]]
+                src = torch.stack([before[s][p, q // rows, h] for p, q in at])
+                fine = src[torch.isfinite(src)].abs()
+                top = (fine.max().item() if len(fine) else 0.0) or 2.0 ** -40
+                to, first = int(dst[0, r0 // page]), r0 % page
+                assert scales[to, first // rows, h].item() == top
+                want = torch.stack([before[x][p, q, h].float() for p, q in at]) * (src / top)[:, None]
+                got = pages[to, first:first + len(at), h].cpu()
+                same = lambda a: torch.where(br.bits(a) & 0x7f == 0x7f, 0x7f, br.bits(a))
+                assert torch.equal(same(got), same(want.to(E4M3)))
