@@ -426,7 +426,7 @@ segattn_status seg_kv_evict(const seg_kv_cache* c, const float* weights, int32_t
  * share are not given back by a call of this kind.
  *   block_table     [B][max_pages], row stride table_stride: new entries are written, others are left as they were
  *   kv_len_out      int32 [B]: want[b] or, where the sequence stayed as it is, kv_len[b]; may be kv_len or want
- *   free_count_out  int32 [1]; may be free_count
+ *   free_count_out  int32 [1]; may be free_count (else it is written for B = 0 too)
  *   q_len           int32 [B]: max(0, kv_len_out - kv_len), the new rows as the calls below take them
  *   slots           int64 [B][Lq]: page * page_size + row of new row t, -1 from q_len[b] on (8-byte aligned)
  *   positions       int32 [B][Lq]: kv_len + t + pos_shift (NULL: 0) of new row t, 0 from q_len[b] on: what seg_rope_rotate takes

@@ -85,7 +85,7 @@ __device__ __forceinline__ void plan_pages(const ResizeParams& p, PagePlan* plan
         count = min(max(count, 0), p.n_pages);
     }
     auto pages = [&](int rows) { return rows < 0 ? 0 : pages_for(p, rows); };
-    long long there = 0;  // pages on the list, those given back among them
+    long long there = count;  // pages on the list, those given back among them
     if (p.B > threads) {  // else one scan gives their number as well
         Pair back{0, 0}, total;
         for (int b = tid; b < p.B; b += threads) {

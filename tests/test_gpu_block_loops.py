@@ -84,3 +84,19 @@ def test_means_follow_rows_that_an_append_rescales(d, page, rows, block):
         step(rand(3, Lq, Hkv, d, seed=90 + k) * 2.0 ** (14 + 2 * k), rand(3, Lq, Hkv, d, seed=95 + k), ints(new))
         same_means(c, block, means, lens)
     sa.poll_status()
+
+
+def test_an_empty_batch_keeps_its_free_list():
+    e, none = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, 4, dtype=torch.int32, device="cuda")
+    free = ints([1, 2, 7, 5, 3])
+    for Lq in (0, 4, 5000):
+        out = ints([-77])
+        got = sa.pages_resize(e, none, e, free, ints([2]), 16, Lq, free_count_out=out)
+        assert got[1] is out and out.item() == 2 and got[0].numel() == 0 and got[3].shape == (0, Lq)
+        for count, want in ((-3, 0), (6, 5)):      # cut, and reported, as in a batch with sequences
+            assert sa.pages_resize(e, none, e, free, ints([count]), 16, Lq, free_count_out=out)[1].item() == want
+            refused()
+    count = ints([2])
+    sa.pages_resize(e, none, e, free, count, 16, 4, free_count_out=count)
+    assert count.item() == 2 and free.tolist() == [1, 2, 7, 5, 3]
+    sa.poll_status()
