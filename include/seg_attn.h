@@ -473,7 +473,7 @@ segattn_status seg_blocks_evict(const seg_kv_cache* c, const seg_block_scales* s
  * segment at a time over keys that lie in one piece; this one is for rows of the paged cache, each with a choice of its own.)
  * Blocks are `block` slots (16, 32, 64 or 128; a divisor of page_size), block j the slots [j block, (j + 1) block) of a sequence.
  *   means   of a full block's keys: with m = their mean in double, rounded to fp32, and scale = max |m| times 1/127 (in fp32), q = m / scale
- *           (fp32) rounded to the nearest integer.  A block with an infinite or NaN mean gets q = 0 and a NaN scale.
+ *           (fp32) rounded to the nearest integer, -127 to 127.  A block with an infinite or NaN mean gets q = 0 and a NaN scale.
  *           q is int8 contiguous [n_pages][page_size / block][Hkv][d], 16-byte aligned, scale fp32 [n_pages][page_size / block][Hkv]. */
 typedef struct {
     int8_t* q;      /* DEVICE */

@@ -445,9 +445,10 @@ __global__ void __launch_bounds__(32 * kSumWarps, 6) summarise_kernel(const __gr
     const bool fine = most < 0x7f800000u && !__any_sync(0xffffffffu, odd);
     const float step = fine ? __fmul_rn(__uint_as_float(most), kOver127) : __uint_as_float(0x7fffffffu);
     const long long at = ((long long)page * p.per_page + (prow >> p.log)) * p.c.Hkv + h;
-    uint32_t q = 0;
+    uint32_t q = 0;  // cut to +-127: a subnormal step is rounded so coarsely that the largest mean comes to more of them
 #pragma unroll
-    for (int e = 0; e < KEEP; ++e) q |= (fine && step > 0.f ? (uint32_t)__float2int_rn(__fdiv_rn(mean[e], step)) & 0xffu : 0u) << (8 * e);
+    for (int e = 0; e < KEEP; ++e)
+        q |= (fine && step > 0.f ? (uint32_t)min(max(__float2int_rn(__fdiv_rn(mean[e], step)), -127), 127) & 0xffu : 0u) << (8 * e);
     int8_t* out = p.sums + at * D + dim;
     if (KEEP == 4) *reinterpret_cast<uint32_t*>(out) = q;
     else *reinterpret_cast<uint16_t*>(out) = (uint16_t)q;

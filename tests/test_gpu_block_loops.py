@@ -100,3 +100,19 @@ def test_an_empty_batch_keeps_its_free_list():
     sa.pages_resize(e, none, e, free, count, 16, 4, free_count_out=count)
     assert count.item() == 2 and free.tolist() == [1, 2, 7, 5, 3]
     sa.poll_status()
+
+
+@pytest.mark.parametrize("units", [1, 2, 3, 5, 11, 100])
+def test_means_of_the_smallest_numbers(units):
+    # a mean of a few fp32 subnormal steps: the step of the mean's 8 bits is rounded so coarsely that the largest comes to more than 127 of them
+    for d, block in ((64, 16), (128, 128)):
+        K = torch.zeros(2, 128, 1, d, dtype=torch.bfloat16, device="cuda")
+        K[1, 3, 0, 7], K[1, 5, 0, 11] = units * 2.0 ** -133, -units * 2.0 ** -133
+        sums, scale = torch.full((2, 128 // block, 1, d), 9, dtype=torch.int8, device="cuda"), torch.full((2, 128 // block, 1), 7.0, device="cuda")
+        sa.blocks_summarise(K, ints([[1]]), ints([128]), 128, sums, scale)
+        sa.poll_status()
+        mean = np.float32(units * 2.0 ** -133 / block)
+        step = np.float32(mean * (np.float32(1) / np.float32(127)))
+        q = min(127, int(np.rint(np.float32(mean / step))))
+        assert scale[1, 0, 0].item() == step and sums[1, 0, 0, 7].item() == q and sums[1, 0, 0, 11].item() == -q
+        assert sums[1, 0, 0].abs().sum().item() == 2 * q
