@@ -332,6 +332,13 @@ def kv_evict(weights, K_pages, V_pages, block_table, kv_len, dst_table, sink: in
     the evicted cache, whose block table is dst_table; kv_len_out may be kv_len and pos_shift_out pos_shift."""
     c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, None, pos_shift, None, None, reads_values=False)
     sc = _block_scales(k_scale, v_scale, K_pages, dev)
+    if sc is None and (k_scale is not None or v_scale is not None):  # one to a head: the same for every row
+        if K_pages.dtype is not _E4M3:
+            raise ValueError("scales belong to an 8-bit cache")
+        if k_scale is None or v_scale is None:
+            raise ValueError("an 8-bit cache has k_scale and v_scale")
+        _flat(k_scale, _F32, (Hkv,), "k_scale", dev)
+        _flat(v_scale, _F32, (Hkv,), "v_scale", dev)
     _, dst_pages, dst_stride = _pages(dst_table, B, "dst_table", dev)
     W = weights.shape[-1] if weights.dim() == 3 else 0
     _flat(weights, _F32, (B, Hkv, W), "weights", dev)

@@ -116,3 +116,23 @@ def test_means_of_the_smallest_numbers(units):
         q = min(127, int(np.rint(np.float32(mean / step))))
         assert scale[1, 0, 0].item() == step and sums[1, 0, 0, 7].item() == q and sums[1, 0, 0, 11].item() == -q
         assert sums[1, 0, 0].abs().sum().item() == 2 * q
+
+
+def test_scales_an_eviction_cannot_use_are_refused():
+    c = br.ScaledCache([200], 2, 64, 32, 16, seed=1, spare=5)
+    dst = ints([c.spare[:3]])
+    w = torch.rand(1, 2, c.max_pages * 32, device="cuda")
+    k, v = c.scales["k_scale"], c.scales["v_scale"]
+    call = lambda **kw: sa.kv_evict(w, c.K, c.V, dst_table=dst, sink=1, recent=30, heavy=40, **c.dev, **kw)
+    before = [br.bits(x).clone() for x in (c.K, c.V)]
+    for kw in (dict(v_scale=v), dict(k_scale=k), dict(k_scale=k[0], v_scale=v[0]), dict(k_scale=k[0, 0], v_scale=v), dict(k_scale=k, v_scale=v[0, 0]),
+               dict(k_scale=k[0, 0].double(), v_scale=v[0, 0].double()), dict(k_scale=k[0, 0])):
+        with pytest.raises(ValueError):
+            call(**kw)
+    assert all(torch.equal(br.bits(x), y) for x, y in zip((c.K, c.V), before))
+    one = torch.ones(2, device="cuda")
+    call(k_scale=one, v_scale=one)      # one to a head goes with every row: nothing to carry
+    b = ref.Cache([200], 2, 64, 32, seed=1, spare=5)
+    with pytest.raises(ValueError):
+        sa.kv_evict(w, b.K, b.V, dst_table=ints([b.spare[:3]]), sink=1, recent=30, heavy=40, k_scale=one, v_scale=one, **b.dev)
+    sa.poll_status()
