@@ -463,7 +463,8 @@ segattn_status seg_blocks_append(const seg_kv_cache* c, const seg_block_scales* 
 
 /* seg_kv_evict (same arguments, same rows kept) for such a cache: the kept rows' new blocks take the largest magnitude of their rows' finite
  * scales (2^-40 where that is zero), and a row of another scale is brought to it as above (one whose scale is not finite becomes NaN or saturates).  Scales must not share elements, neither here nor in the append (a zero stride
- * is SEGATTN_ERR_INVALID).  (seg_kv_evict itself moves rows as they are, without their blocks' scales.)  Two kernels. */
+ * is SEGATTN_ERR_INVALID).  (seg_kv_evict itself moves rows as they are, without their blocks' scales.)  Neither moves means of blocks (see
+ * below): those of the new pages are to be taken anew, by seg_blocks_summarise with Lq = max_pages * page_size.  Two kernels. */
 segattn_status seg_blocks_evict(const seg_kv_cache* c, const seg_block_scales* scales, const float* weights, int32_t W, int32_t sink,
                                 int32_t recent, int32_t heavy, const int32_t* dst_table, int32_t dst_max_pages, int32_t dst_stride,
                                 int32_t* idx, int32_t* kv_len_out, int32_t* pos_shift_out, float* weights_out, void* stream);

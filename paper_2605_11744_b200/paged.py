@@ -327,7 +327,8 @@ def kv_evict(weights, K_pages, V_pages, block_table, kv_len, dst_table, sink: in
     `recent` and the `heavy` rows of largest accumulated weight between them, copied in order to the pages of dst_table (int32
     [B, pages], none of them a page the sequence has now) - the C entry point `seg_kv_evict`.  Rows are moved as they are: an
     8-bit cache's scales are not needed, unless it has one for each block of rows and head: those go with the rows (`k_scale`,
-    `v_scale`; the C entry point `seg_blocks_evict`).  weights is fp32 [B, Hkv, W] as
+    `v_scale`; the C entry point `seg_blocks_evict`).  Means of blocks (blocks_summarise) do not go with them: those of the new pages
+    are to be taken anew, with Lq = max_pages * page_size.  weights is fp32 [B, Hkv, W] as
     seg_attn_decode gathers it.  Returns (idx int32 [B, Hkv, budget] (the slots kept, then -1), kv_len, pos_shift, weights) of
     the evicted cache, whose block table is dst_table; kv_len_out may be kv_len and pos_shift_out pos_shift."""
     c, B, Hkv, d, _, _, dev = _cache(K_pages, V_pages, block_table, kv_len, None, pos_shift, None, None, reads_values=False)

@@ -136,3 +136,27 @@ def test_scales_an_eviction_cannot_use_are_refused():
     with pytest.raises(ValueError):
         sa.kv_evict(w, b.K, b.V, dst_table=ints([b.spare[:3]]), sink=1, recent=30, heavy=40, k_scale=one, v_scale=one, **b.dev)
     sa.poll_status()
+
+
+def test_means_are_taken_anew_after_an_eviction():
+    # the new pages' means are none of the old ones', and a choice goes by those of the rows that are there
+    lens, Hkv, d, page, rows, block = [300, 260], 2, 64, 32, 16, 16
+    budget, S, T, n = 160, 32, 8, 4
+    need = -(-budget // page)
+    c = br.ScaledCache(lens, Hkv, d, page, rows, seed=4, spare=2 * need)
+    dst = ints(c.spare[:2 * need]).view(2, need)
+    means = fresh_means(c, block)
+    sa.blocks_summarise(c.K, c.dev["block_table"], c.dev["kv_len"], c.max_pages * page, *means, k_scale=c.scales["k_scale"])
+    w = torch.rand(2, Hkv, c.max_pages * page, generator=torch.Generator().manual_seed(1)).cuda()
+    _, kept, shift, _ = sa.kv_evict(w, c.K, c.V, dst_table=dst, sink=2, recent=60, heavy=budget - 62, **c.dev, **c.scales)
+    assert (means[0][dst[0, 0].long()] == 9).all()      # as they were
+    sa.blocks_summarise(c.K, dst, kept, need * page, *means, k_scale=c.scales["k_scale"])
+    Q = rand(2, 1, 4, d)
+    got = sa.blocks_select(Q, *means, dst, kept, page, S, T, n, head_past_mask=[1, 1], pos_shift=shift)
+    sa.poll_status()
+    c.table = dst.cpu()
+    same_means(c, block, means, kept.tolist())
+    for b in range(2):
+        want = br.select(Q[b].float().cpu().double().numpy(), means[0].cpu().numpy(), means[1].cpu().numpy(), dst[b].tolist(), budget, 1, S, T, [1, 1], page, block, n, 0,
+                         shift=int(shift[b]))
+        assert np.array_equal(got[b].cpu().numpy(), want)
