@@ -432,7 +432,8 @@ segattn_status seg_kv_evict(const seg_kv_cache* c, const float* weights, int32_t
  *   positions       int32 [B][Lq]: kv_len + t + pos_shift (NULL: 0) of new row t, 0 from q_len[b] on: what seg_rope_rotate takes
  * A sequence grows by at most Lq rows.  One out of range (want < 0 or past max_pages * page_size, a larger growth, a kv_len out of
  * range) stays as it is, a free_count outside [0, n_pages] is cut, a page number outside [0, n_pages) comes out as -1 in the table
- * and the slots: each makes the next seg_attn_poll_status return SEGATTN_ERR_INVALID.  B <= 65535, max_pages * page_size <= 2^30.
+ * and the slots, a pos_shift below 0, or one that brings a position past 2^31 - 1, counts as 0: each makes the next
+ * seg_attn_poll_status return SEGATTN_ERR_INVALID.  B <= 65535, max_pages * page_size <= 2^30.
  * `workspace`: DEVICE, 256-byte aligned, seg_pages_workspace_bytes(B) bytes (0: invalid B), scratch (calls that may run
  * at the same time, captured ones too, need one each); not looked at, and may be NULL, where B <= 1024 and B * Lq <= 4096 (one kernel; two elsewhere). */
 size_t seg_pages_workspace_bytes(int32_t B);

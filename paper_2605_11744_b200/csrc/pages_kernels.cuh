@@ -161,7 +161,7 @@ __device__ __forceinline__ void fill_sequence(const ResizeParams& p, const PageP
     }
     const int grown = q.n_new - q.n_old;
     int shift = p.pos_shift ? p.pos_shift[b] : 0;
-    if (shift < 0) {
+    if (shift < 0 || (grown > 0 && shift > 0x7fffffff - (q.n_new - 1))) {  // or one that brings a position past its type
         if (i0 == 0) refuse_input(32);
         shift = 0;
     }

@@ -160,3 +160,16 @@ def test_means_are_taken_anew_after_an_eviction():
         want = br.select(Q[b].float().cpu().double().numpy(), means[0].cpu().numpy(), means[1].cpu().numpy(), dst[b].tolist(), budget, 1, S, T, [1, 1], page, block, n, 0,
                          shift=int(shift[b]))
         assert np.array_equal(got[b].cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("Lq", [4, 3000])
+def test_positions_past_their_type_are_refused(Lq):
+    # a shift that brings a new row's position past 2^31 - 1 counts as one out of range: the sequence's positions are its slots
+    page, top = 16, 2 ** 31 - 1
+    lens, want = [40, 33, 7], [43, 33, 8]
+    table = ints([[3 * b + i for i in range(3)] + [-1] * 300 for b in range(3)])
+    for shift, bad in (([top - 42, top, 5], False), ([top - 41, 3, 5], True), ([top, 3, 5], True)):
+        got = sa.pages_resize(ints(want), table.clone(), ints(lens), ints(list(range(20, 60))), ints([40]), page, Lq, pos_shift=ints(shift))
+        refused() if bad else sa.poll_status()
+        assert got[4][0, :4].tolist() == [(0 if bad else shift[0]) + 40 + t for t in range(3)] + [0]
+        assert got[4][2, :2].tolist() == [12, 0] and got[4][1].eq(0).all() and got[0].tolist() == want
