@@ -21,8 +21,9 @@ struct AppendBlocksParams {
     int log;                               // log2 of a block's rows
 };
 
-// The exponent of the scale of a block whose largest value is `top`: 2^e >= top / 448, the smallest such, cut to [-40, 119] (2^119
-// times 448 is bf16's range; 2^-40 lies below every value that matters and keeps the scales of a cache within reach of each other).
+// The exponent of the scale of a block whose largest value is `top`: 2^e >= top / 448, the smallest such, cut to [-40, 119].  (2^119 times
+// 448 is 1.75 * 2^127: what lies between that and bf16's end at 1.99 * 2^127 saturates, as infinities do.  2^-40 lies below every
+// value that matters and keeps the scales of a cache within reach of each other.)
 __device__ __forceinline__ int scale_exponent(float top) {
     const uint32_t bits = __float_as_uint(top);
     const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);  // 448 = 1.75 * 2^8

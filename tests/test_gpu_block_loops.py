@@ -173,3 +173,17 @@ def test_positions_past_their_type_are_refused(Lq):
         refused() if bad else sa.poll_status()
         assert got[4][0, :4].tolist() == [(0 if bad else shift[0]) + 40 + t for t in range(3)] + [0]
         assert got[4][2, :2].tolist() == [12, 0] and got[4][1].eq(0).all() and got[0].tolist() == want
+
+
+@pytest.mark.parametrize("top", [448 * 2.0 ** 119, 3.3895313892515355e38])
+def test_the_largest_numbers_saturate(top):
+    # scales end at 2^119: finite magnitudes past 448 * 2^119 (bf16 goes to 1.99 * 2^127) saturate like infinities
+    c = br.ScaledCache([16], 1, 64, 16, 16, seed=1)
+    K, V = torch.zeros(1, 16, 1, 64, dtype=torch.bfloat16, device="cuda"), rand(1, 16, 1, 64)
+    K[0, 3, 0, 5], K[0, 4, 0, 6] = top, -top
+    assert K[0, 3, 0, 5].item() == top
+    sa.kv_append(K, V, c.K, c.V, **c.dev, **c.scales)
+    sa.poll_status()
+    at = c.table[0, 0].long()
+    x = c.K[at].float()
+    assert c.scales["k_scale"][at, 0, 0].item() == 2.0 ** 119 and x[3, 0, 5].item() == 448 and x[4, 0, 6].item() == -448 and x.abs().sum().item() == 896
