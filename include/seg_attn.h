@@ -428,7 +428,8 @@ segattn_status seg_kv_evict(const seg_kv_cache* c, const float* weights, int32_t
  *   kv_len_out      int32 [B]: want[b] or, where the sequence stayed as it is, kv_len[b]; may be kv_len or want
  *   free_count_out  int32 [1]; may be free_count (else it is written for B = 0 too)
  *   q_len           int32 [B]: max(0, kv_len_out - kv_len), the new rows as the calls below take them
- *   slots           int64 [B][Lq]: page * page_size + row of new row t, -1 from q_len[b] on (8-byte aligned)
+ *   slots           int64 [B][Lq]: page * page_size + row of new row t, -1 from q_len[b] on (8-byte aligned); for kernels that keep something
+ *                   of their own beside the cache's rows: no call here needs it
  *   positions       int32 [B][Lq]: kv_len + t + pos_shift (NULL: 0) of new row t, 0 from q_len[b] on: what seg_rope_rotate takes
  * A sequence grows by at most Lq rows.  One out of range (want < 0 or past max_pages * page_size, a larger growth, a kv_len out of
  * range) stays as it is, a free_count outside [0, n_pages] is cut, a page number outside [0, n_pages) comes out as -1 in the table

@@ -27,7 +27,8 @@ def pages_resize(want, block_table, kv_len, free_pages, free_count, page_size: i
     enough: those stay as they are - the C entry point `seg_pages_resize`.  block_table [B, max_pages] gets the new entries.
     Returns (kv_len_out, free_count_out, q_len, slots, positions): the lengths (kv_len_out may be kv_len or want), the list's new length (may be
     free_count), the new rows of every sequence, and for each of them, [B, Lq], its row in the pages taken as one (int64, -1: not there) and
-    its position (int32, pos_shift added), as kv_append and rope_rotate take them."""
+    its position (int32, pos_shift added).  kv_append takes the lengths and the new rows (kv_len, q_len) and finds their places by itself;
+    rope_rotate takes the positions; the slot map is for kernels of a program's own that write beside the cache."""
     dev = want.get_device()
     if dev < 0:
         raise ValueError("pages are handed out on a CUDA device: want and the others lie there")
