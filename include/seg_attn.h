@@ -455,7 +455,8 @@ typedef struct {
 /* seg_kv_append (same arguments, same rows left out) into such a cache.  With m the largest finite magnitude that the call adds
  * to a block (of keys after their rotation), the block's scale becomes the smallest power of two 2^e >= m / 448, -40 <= e <= 119, or stays
  * where the block has rows of its sequence already and their scale is larger; where it grows those rows are brought to it (times
- * old / new, rounded to nearest even: exact, but for values below 2^-6 times the new scale).  Stored is x times the scale's inverse,
+ * old / new, rounded to nearest even: exact, but for values below 2^-6 times the new scale).  (Of a scale that another program has left
+ * there the magnitude counts; rows of one that is not finite become NaN or saturate.)  Stored is x times the scale's inverse,
  * rounded to nearest even and saturated at +-448; infinities saturate, and magnitudes past 448 * 2^119 = 2.98e38, a NaN stays one.  Scales of blocks that are written into for the
  * first time may hold anything before.  One kernel. */
 segattn_status seg_blocks_append(const seg_kv_cache* c, const seg_block_scales* scales, int32_t Lq, const void* K_new,

@@ -168,10 +168,13 @@ __global__ void __launch_bounds__(256) append_blocks_kernel(const __grid_constan
         __syncthreads();
         most = __reduce_max_sync(0xffffffffu, red[tid & 7]);
     }
-    const float scale = fmaxf(old, __uint_as_float((uint32_t)(127 + scale_exponent(__uint_as_float(most))) << 23));
+    // An append's own scales are positive; of others the magnitude counts, and one that is not finite has no say (its rows become NaN, or
+    // saturate).
+    const float size = fabsf(old), need = __uint_as_float((uint32_t)(127 + scale_exponent(__uint_as_float(most))) << 23);
+    const float scale = size <= FLT_MAX ? fmaxf(size, need) : need;
     char* dst = val ? a.c.V + page * a.c.v_stride[0] + prow * dst_row + h * a.c.v_stride[2]
                     : a.c.K + page * a.c.k_stride[0] + prow * dst_row + h * a.c.k_stride[2];
-    if (start < lo && scale > old) {
+    if (start < lo && scale != old) {
         const float r = __fdiv_rn(old, scale);
         for (int row = rr; row < lo - start; row += RP) {
             uint4* at = reinterpret_cast<uint4*>(dst + row * dst_row + u * 16);

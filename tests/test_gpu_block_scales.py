@@ -1,5 +1,5 @@
-"""Scales of blocks that no append writes: zero, negative, not finite, and small or large throughout, in the attention and the eviction,
-against the definition (a stored element x stands for x times its block's scale) in 64 bits."""
+"""Scales of blocks that no append writes: zero, negative, not finite, and small or large throughout, in the attention, the eviction and the
+append itself, against the definition (a stored element x stands for x times its block's scale) in 64 bits."""
 import math
 
 import numpy as np
@@ -220,3 +220,34 @@ def test_evicted_rows_keep_values_of_any_scale(d, page, rows, unit):
                 got = pages[to, first:first + len(at), h].cpu()
                 same = lambda a: torch.where(br.bits(a) & 0x7f == 0x7f, 0x7f, br.bits(a))
                 assert torch.equal(same(got), same(want.to(E4M3)))
+
+
+@pytest.mark.parametrize("old", [-0.5, -64.0, 0.0, 3.0, 2.0 ** -60, -(2.0 ** 100), math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("d,rows", [(64, 16), (128, 64)])
+def test_rows_appended_to_a_block_of_any_scale(d, rows, old):
+    # what the rows there stood for, they stand for afterwards: they are brought to the larger magnitude of the old scale and the new rows'
+    n, Hkv, page = rows + rows // 2 + 3, 2, 2 * rows
+    c = br.ScaledCache([n], Hkv, d, page, rows, seed=d)
+    pages = [(4 * torch.randn(c.K.shape, generator=torch.Generator().manual_seed(k))).clamp(-400, 400).to(E4M3) for k in (1, 2)]
+    c.K.copy_(pages[0].cuda()), c.V.copy_(pages[1].cuda())
+    for x in ("k_scale", "v_scale"):
+        put(c, 0, [0, 1], old, which=x)
+    for Lq in (1, rows // 2):
+        K, V = query(1, Lq, Hkv, d, seed=Lq, size=3.0), query(1, Lq, Hkv, d, seed=Lq + 1, size=100.0)
+        before = [x.cpu().clone() for x in (c.K, c.V, c.scales["k_scale"], c.scales["v_scale"])]
+        sa.kv_append(K, V, c.K, c.V, **c.dev, **c.scales)
+        sa.poll_status()
+        at = int(c.table[0, 0])
+        for new, was, s0, stored, scales in ((K, before[0], before[2], c.K, c.scales["k_scale"]), (V, before[1], before[3], c.V, c.scales["v_scale"])):
+            first = n - Lq
+            for h in range(Hkv):
+                x = new[0, :, h].float().cpu()
+                s = s0[at, 1, h].item()
+                want = max(br.scale_of(x.abs().max().item()), abs(s) if math.isfinite(s) else 0.0)
+                assert scales[at, 1, h].item() == want
+                there = (was[at, rows:first, h].float() * (torch.tensor(s) / want)).clamp(-448, 448)
+                fresh = (x * (1 / torch.tensor(want))).clamp(-448, 448)
+                same = lambda a: torch.where(br.bits(a) & 0x7f == 0x7f, 0x7f, br.bits(a))
+                assert torch.equal(same(stored[at, rows:first, h].cpu()), same(there.to(E4M3)))
+                assert torch.equal(same(stored[at, first:n, h].cpu()), same(fresh.to(E4M3)))
+                assert torch.equal(br.bits(stored)[at, :rows, h].cpu(), br.bits(was)[at, :rows, h])
