@@ -316,7 +316,8 @@ __device__ __forceinline__ void add_halves(float& lo, float& hi, uint32_t x) {
 // hardly any of them in double precision, where a conversion alone takes the time of a dozen others: values of an 8-bit cache are
 // multiples of 2^-9, of which a lane adds up 32 at most in fp32, and the lanes their sums as integers, exactly; bf16 numbers are put
 // into doubles bit by bit.  8 sequences of 16-65K rows, 8 heads in 8 bits: 79 us for 384 MB (4.9 TB/s; 317 us with every value made a
-// double), 1080 instructions to a block of 64 rows, half of them the additions.  Small thread blocks: a step's few blocks spread out.
+// double), 1080 instructions to a block of 64 rows, half of them the additions; issue slots and DRAM are both at 57%, as a warp looks up and
+// loads one block alone and waits for it.  Small thread blocks: a step's few blocks spread out.
 constexpr int kSumWarps = 4;
 template <int D, bool FP8>
 __global__ void __launch_bounds__(32 * kSumWarps, 6) summarise_kernel(const __grid_constant__ SummariseParams p) {

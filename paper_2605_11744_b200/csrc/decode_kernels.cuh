@@ -22,10 +22,10 @@
 // convert (453 instructions per 16 slots at first, 240 now) and by DRAM pieces of 64 or 128 bytes.
 //
 // Two more forms of the same kernel: with a scale for each block of rows (BS: 8 sequences of 100-131K slots, every second of 8 heads,
-// 172 us for 1.04 GB, 6.0 TB/s), and with chosen blocks in the place of the far past (SEL; with scales, 16 sequences of 90-131K slots,
-// four rows each of 64 blocks and 2-3K slots of their own: 125 us for the 595 MB that they cannot do without).  The latter is
-// held up by the instructions of a row's 16 slots (half of the issue slots, 5.7 cycles to one of a warp): four query heads leave
-// half of each product empty, and a start of 7 us (length, list, page, rows) weighs more.
+// 168-181 us on different cards for 1.04 GB, 5.8-6.2 TB/s), and with chosen blocks in the place of the far past (SEL; with scales, 16 sequences of 90-131K slots,
+// four rows each of 64 blocks and 2-3K slots of their own: 123-129 us for the 595 MB that they cannot do without).  The latter
+// waits: three warps to a scheduler leave half of the issue slots empty (5.7 cycles to an instruction of a warp) and DRAM at 58%.  Four query
+// heads leave half of each product empty, and a start of 7 us (length, list, page, rows) weighs more.
 #pragma once
 #include <cstdint>
 #include <cuda_bf16.h>
